@@ -124,6 +124,58 @@ int32_t chiron_append_kv(chiron_kvpool *p, int32_t layer, const void *k, const v
 int32_t chiron_gather_kv(const chiron_kvpool *p, int32_t layer, const int32_t *block_table_row, int32_t len,
                          void *k_out, void *v_out, void *stream);
 
+/* Rotate and append (drafting and prefill outside chiron_decode_step): request i brings the rows
+ * row_starts[i] .. row_starts[i+1]-1 of q, k and v, its tokens at the positions seq_lens[i], seq_lens[i]+1, ...
+ *     q_out[r][a] = rot(q[r][a]);  slot(i, pos) of layer `layer` = bf16(rot(k[r])), bf16(v[r])
+ * where rot turns the pairs (j, j+head_dim/2) by the row's angles: (a cos - b sin, b cos + a sin), in fp32, rounded once
+ * (to nearest, ties to even) when stored as bf16.
+ *   in           host, read during the call: dtype CHIRON_F32 or CHIRON_BF16; q, k, v dev [rows][heads][head_dim] with
+ *                the row strides given (elements, any; heads and dims contiguous); q and q_out may both be null
+ *   cos, sin     dev fp32 [rows, head_dim/2] (chiron_op_rope_table)
+ *   q_out        dev fp32 [rows, n_q_heads, head_dim], contiguous, not overlapping the inputs
+ *   row_starts   dev int32 [batch+1], ascending from 0 to rows;  seq_lens dev int32 [batch]: tokens ALREADY cached
+ *   block_table  dev int32 [batch, max_blocks_per_seq]; a written page must belong to one request only
+ *   index        optional: the records of every written page are brought up to date from all its tokens (old and new)
+ * A request may bring no row.  Tokens whose page is not one of the pool, or behind the table's last column, are not
+ * written.  rows == 0 is a no-op.  No other slot of a page is touched. */
+enum { CHIRON_F32 = 2 };
+typedef struct chiron_kvindex chiron_kvindex;
+typedef struct {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    int32_t dtype, n_q_heads;
+    const float *cos, *sin;
+    float *q_out;
+} chiron_new_rows;
+int32_t chiron_append_kv_rope(chiron_kvpool *p, chiron_kvindex *index, int32_t layer, const chiron_new_rows *in,
+                              const int32_t *block_table, int32_t max_blocks_per_seq, const int32_t *row_starts,
+                              const int32_t *seq_lens, int32_t batch, int32_t rows, void *stream);
+
+/* ---- page index (what block-sparse attention scores pages by) -------------------------------------------------
+ *
+ * One record per layer, page and KV head: for each key dimension a bound from above and one from below over the page's
+ * tokens, as whole multiples of a power of two that the record's dimensions share:
+ *     2^e = the smallest power of two, e >= -126, with  max |k| <= 127 * 2^e   (e = 0 where all keys are 0)
+ *     hi  = ceil(max_t k_t / 2^e),  lo = floor(min_t k_t / 2^e)                 in -127 .. 127
+ * NaN keys count as 0 and infinite ones as the largest finite bf16.  Everything is exact, so a record does not depend on
+ * the order in which tokens came.
+ * The index is a descriptor over CALLER-owned device memory beside a pool's, `bytes` >= chiron_kv_index_bytes(p),
+ * 256-byte aligned.  Memory is not cleared: a page's records hold nothing meaningful until the page was written with
+ * chiron_append_kv_rope(index) or named in chiron_kv_index_update.  The layout:
+ *     per layer  int8 [num_blocks][n_kv_heads][hi, lo][head_dim], then int8 e [num_blocks][n_kv_heads], the layer's
+ *     total padded to 256 bytes. */
+int64_t chiron_kv_index_bytes(const chiron_kvpool *p);
+int32_t chiron_kv_index_create(const chiron_kvpool *p, void *dev_mem, uint64_t bytes, chiron_kvindex **out);
+int32_t chiron_kv_index_destroy(chiron_kvindex *x); /* does not free dev_mem */
+
+/* Recomputes, for the layers layer .. layer+n_layers-1, the records of the pages that hold the positions
+ * from[i] .. to[i]-1 of each request, from the tokens 0 .. to[i]-1 that the pool holds (after a step, an append or a
+ * swap-in that did not know the index).  from, to dev int32 [batch]; max_new >= every to[i]-from[i] (a request with more
+ * is done for the pages of its first max_new positions). */
+int32_t chiron_kv_index_update(chiron_kvindex *x, const chiron_kvpool *p, int32_t layer, int32_t n_layers,
+                               const int32_t *block_table, int32_t max_blocks_per_seq, const int32_t *from,
+                               const int32_t *to, int32_t batch, int32_t max_new, void *stream);
+
 /* Eviction support (Design: a mixed instance evicts a batch request when an interactive one arrives, and
  * saves its KV cache by migrating it to CPU memory so that it can restart fast).
  * chiron_kv_swap_out copies the first n_pages pages of one request (every layer, K and V) into `image`;

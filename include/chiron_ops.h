@@ -74,6 +74,84 @@ int32_t chiron_op_paged_attention(chiron_model *m, const chiron_kvpool *p, int32
                                   const int32_t *block_table, const int32_t *ctx_lens, int32_t batch, float *out,
                                   void *stream);
 
+/* cos/sin [rows, d/2] dev fp32 of the angles pos[r]*base^(-2j/d), evaluated in fp64: the table that chiron_append_kv_rope
+ * takes, one for all layers of a step. */
+int32_t chiron_op_rope_table(const int32_t *pos, int32_t rows, int32_t d, float base, float *cos, float *sin, void *stream);
+
+/* ---- block-sparse attention of new tokens: select pages by a cheap score, attend over those only --------------
+ *
+ * Row r is one new token: of request row_seq[r] (dev int32 [rows], null: of request r), seeing the first ctx_lens[r]
+ * (dev int32 [rows], >= 0) positions of it, its own among them.  q dev fp32 [rows, n_q_heads*head_dim], rotated.
+ *
+ * Selection, for each row and KV head c, over the pages 0 .. ceil(ctx_lens[r]/16)-1:
+ *     q8[h]    = round(q[h] / 2^f), ties to even, 2^f as an index record's 2^e over the G query heads of c
+ *     score(p) = 2^e(p) * max_h sum_j (q8[h][j] > 0 ? q8[h][j]*hi(p)[j] : q8[h][j]*lo(p)[j])
+ * which (but for the rounding of q) bounds q . k from above for every token of the page.  The first n_first and the last
+ * n_last pages are always taken, then the pages of the highest scores, equal ones by the lower page, `top` in all.  Whole
+ * number arithmetic: a selection does not depend on the batch or on how the work was split.  NaN in q counts as 0 and
+ * infinities as the largest finite value.
+ *   pages   dev int32 [rows, n_kv_heads, top]: page indices of the request (columns of its block table), ascending, then -1
+ *   counts  dev int32 [rows] (optional): min(top, pages of the row)
+ * n_first, n_last >= 0, n_first + n_last <= top. */
+int32_t chiron_op_select_pages(chiron_model *m, const chiron_kvpool *p, const chiron_kvindex *x, int32_t layer, const float *q,
+                               const int32_t *block_table, const int32_t *row_seq, const int32_t *ctx_lens, int32_t rows,
+                               int32_t top, int32_t n_first, int32_t n_last, int32_t *pages, int32_t *counts, void *stream);
+
+/* out[r][a] = softmax_t(q[r][a] . K_t / sqrt(d)) . V_t over the tokens t < ctx_lens[r] of the pages listed for (r, a / G)
+ * in pages[r][a / G][0 .. counts[r]-1] (counts null: all `top` entries).  Lists may be any, in any order, without an
+ * entry twice; entries that name no page of the row (negative, or behind ctx_lens[r]) count for nothing; a row that sees
+ * no token gets zeros.  out dev fp32 [rows, n_q_heads*head_dim]. */
+int32_t chiron_op_sparse_attention(chiron_model *m, const chiron_kvpool *p, int32_t layer, const float *q,
+                                   const int32_t *block_table, const int32_t *row_seq, const int32_t *ctx_lens, int32_t rows,
+                                   const int32_t *pages, const int32_t *counts, int32_t top, float *out, void *stream);
+/* Both use the model's attention workspace (rows <= max_batch; calls on one model must not overlap). */
+
+/* ---- verification of drafted tokens ---------------------------------------------------------------------------
+ *
+ * Request i drafted n_i = draft_lens[i] (0 .. max_draft; null: max_draft) tokens x_t = tokens[i][t]; logits[i][t] are the
+ * target's after the token before x_t (chiron_decode_step_multi fed with the last token and the drafts), draft_logits[i][t]
+ * the draft's at the same place.  With p, q the softmax of logits / temperature[i] (null: 1) over the vocabulary:
+ *     prob[i][t] = min(1, p_t(x_t) / q_t(x_t))         (q(x) = 0: 1 if p(x) > 0, else 0; t >= n_i: 0)
+ *     a          = the first t < n_i with uniforms[i][t] >= prob[i][t], or n_i: the number of accepted tokens
+ *     new token  = argmax_x r(x) / noise[i][x],  r = max(p_a - q_a, 0) if a < n_i (p_a where that is 0 everywhere), else p_a
+ *     out_tokens[i] = x_0 .. x_{a-1}, new token, -1, ...
+ * With uniforms uniform in [0,1) and noise from the unit exponential distribution the tokens are distributed as the target's
+ * own samples.  draft_logits null: drafts that were not sampled (q is 1 at x_t).  temperature 0 (or no number above it): the greedy choice:
+ * prob is 1 where x_t has the highest logit (of equal ones the lowest token), else 0, and the new token has the highest.
+ * NaN logits count as -inf, +inf as the largest finite value; in a row without any logit above -inf every p is 0 and the new token -1.
+ * A drafted token outside 0 .. vocab-1 has prob 0.
+ *   logits        dev fp32 [batch][max_draft+1][vocab], row (i,t) at logits + (i*(max_draft+1)+t)*logits_stride
+ *   draft_logits  dev fp32 [batch][max_draft][vocab], row stride draft_stride, or null
+ *   tokens        dev int32 [batch, max_draft];  uniforms dev fp32 [batch, max_draft];  noise dev fp32 [batch][vocab] (contiguous)
+ *   out_tokens    dev int32 [batch, max_draft+1];  accepted dev int32 [batch];  prob dev fp32 [batch, max_draft] (optional)
+ *   workspace     dev, chiron_verify_workspace_bytes() bytes, 16-byte aligned, caller-owned, in use until the stream has passed
+ * 0 <= max_draft <= 127. */
+int64_t chiron_verify_workspace_bytes(int32_t batch, int32_t max_draft, int32_t vocab);
+typedef struct {
+    const float *logits, *draft_logits;
+    int64_t logits_stride, draft_stride;
+    const int32_t *tokens, *draft_lens;
+    const float *uniforms, *noise, *temperature;
+} chiron_draft_batch;
+int32_t chiron_op_verify_drafts(const chiron_draft_batch *in /* host */, int32_t batch, int32_t max_draft, int32_t vocab,
+                                int32_t *out_tokens, int32_t *accepted, float *prob, void *workspace, void *stream);
+
+/* ---- products with 4-bit weights ------------------------------------------------------------------------------
+ *
+ * W[n][k] = (w4[n][k] - z[n][k/group]) * scale[n][k/group], w4 in 0 .. 15, z in 0 .. 15 (null: 8 everywhere).
+ *   w4      dev uint8 [N, K/2]: k even in the low four bits, k odd in the high four
+ *   scales  dev bf16 [N, K/group];  zeros dev uint8 [N, K/group] or null
+ * group 32, 64 or 128, K a multiple of group, any N >= 1.  The library keeps its own repacked copy. */
+typedef struct chiron_linear4 chiron_linear4;
+int32_t chiron_linear4_create(const void *w4, const void *scales, const void *zeros, int32_t N, int32_t K, int32_t group,
+                              void *stream, chiron_linear4 **out);
+int32_t chiron_linear4_destroy(chiron_linear4 *l);
+
+/* y[M,N] = x[M,K] * W^T, or y += (accumulate != 0).  x, y dev fp32 row-major, not overlapping.  Per row and group, x enters
+ * as whole multiples of a power of two, 2^22 at the group's largest value (an error of at most 2^-23 of it), in three 8-bit
+ * digits whose products are exact; groups are added in fp32.  A NaN or an infinity in a row of x makes that row of y NaN. */
+int32_t chiron_op_linear4(const chiron_linear4 *l, const float *x, int32_t M, float *y, int32_t accumulate, void *stream);
+
 /* Performance knobs of the kernels, process-wide (0 restores the built-in heuristic where one exists):
  *   linear_nf (1|2|4), linear_mt (1|2|3|4), linear_xcd_remap (0|1), linear_ksplit, linear_target_blocks,
  *   linear_big_min_m (rows from which the gate/up projection hands the down projection tiled bf16 terms; <0 never),

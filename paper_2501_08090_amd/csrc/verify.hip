@@ -1,0 +1,300 @@
+// Verification of drafted tokens: acceptance against the target's probabilities and the token that replaces the first rejected one.
+// gfx950, wave64.
+//
+// Three launches.  (1) Every logit row's maximum, its index, and sum of exponentials, in pieces over the vocabulary: the only pass
+// over all rows, bounded by reading them.  (2) A workgroup per request and piece joins the pieces of its request's rows, decides how
+// many drafts are taken (every workgroup of a request comes to the same answer from the same numbers), and races what is left of the
+// vocabulary in its piece; the two or three rows it needs again come from the caches.  (3) Joins the pieces' winners.
+// The race argmax r(x)/noise(x) instead of a running sum over the vocabulary: it is one pass in any order, and which token wins does
+// not depend on the order of any sum.
+#include <new>
+
+#include "draft_ops.h"
+
+namespace chiron {
+
+constexpr float kTopF32 = 3.4028234663852886e38f;
+constexpr int kMaxDrafts = 127;
+constexpr int kVerifyThreads = 256;
+constexpr int kVerifyPiece = 4096;  // logits of a row per workgroup
+
+struct RowStat {
+    float m, z;  // maximum; sum of exp((x - m) / T)
+    int best;    // lowest index of the maximum, -1: nothing above -inf
+    int pad;
+};
+struct Winner {
+    float rest, all;  // best r/noise with the draft taken off, and without
+    int rest_at, all_at;
+};
+struct VerifyArgs {
+    chiron_draft_batch in;
+    int batch, max_draft, vocab, pieces;
+    RowStat* stats;  // [batch][2*max_draft+1][pieces]: target rows, then draft rows
+    Winner* winners; // [batch][pieces]
+    int32_t *out_tokens, *accepted;
+    float* prob;
+};
+
+__device__ __forceinline__ float logit_of(float x) { return x != x ? -INFINITY : fminf(x, kTopF32); }
+__device__ __forceinline__ float inv_temperature(const VerifyArgs& a, int i) {
+    if (!a.in.temperature) return 1.f;
+    const float t = a.in.temperature[i];
+    return t > 0.f ? fminf(1.f / t, kTopF32) : 0.f;  // 0: greedy
+}
+__device__ __forceinline__ int drafts_of(const VerifyArgs& a, int i) {
+    return a.in.draft_lens ? min(max(a.in.draft_lens[i], 0), a.max_draft) : a.max_draft;
+}
+// joins two statistics of one row; of equal maxima the lower index
+__device__ __forceinline__ void join(float& m, float& z, int& best, float m2, float z2, int best2, float inv_t) {
+    if (m2 == -INFINITY) return;
+    if (m == -INFINITY) {
+        m = m2; z = z2; best = best2;
+        return;
+    }
+    if (m2 > m) {
+        z = z * expf((m - m2) * inv_t) + z2;
+        m = m2;
+        best = best2;
+    } else {
+        z += z2 * expf((m2 - m) * inv_t);
+        if (m2 == m) best = min(best, best2);
+    }
+}
+__device__ __forceinline__ void join_wave(float& m, float& z, int& best, float inv_t) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const float m2 = __shfl_xor(m, o), z2 = __shfl_xor(z, o);
+        const int b2 = __shfl_xor(best, o);
+        join(m, z, best, m2, z2, b2, inv_t);
+    }
+}
+
+__global__ __launch_bounds__(kVerifyThreads) void verify_stats_kernel(VerifyArgs a) {
+    __shared__ float s_m[4], s_z[4];
+    __shared__ int s_b[4];
+    const int rows = 2 * a.max_draft + 1;
+    const int i = blockIdx.y / rows, r = blockIdx.y % rows, piece = blockIdx.x;
+    const int n = drafts_of(a, i);
+    const float inv_t = inv_temperature(a, i);
+    const bool draft = r > a.max_draft;
+    const int t = draft ? r - a.max_draft - 1 : r;
+    if (draft ? (t >= n || !a.in.draft_logits || inv_t == 0.f) : t > n) return;  // nobody asks for this row
+    const float* row = draft ? a.in.draft_logits + ((int64_t)i * a.max_draft + t) * a.in.draft_stride
+                             : a.in.logits + ((int64_t)i * (a.max_draft + 1) + t) * a.in.logits_stride;
+    const int x0 = piece * kVerifyPiece, x1 = min(a.vocab, x0 + kVerifyPiece);
+    constexpr int VPT = kVerifyPiece / kVerifyThreads;
+    float v[VPT];
+    float m = -INFINITY, z = 0.f;
+    int best = -1;
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+        const int x = x0 + j * kVerifyThreads + threadIdx.x;
+        v[j] = x < x1 ? logit_of(row[x]) : -INFINITY;
+    }
+#pragma unroll
+    for (int j = 0; j < VPT; ++j)
+        if (v[j] > m) {
+            m = v[j];
+            best = x0 + j * kVerifyThreads + threadIdx.x;
+        }
+    if (m > -INFINITY)
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) z += expf((v[j] - m) * inv_t);
+    join_wave(m, z, best, inv_t);
+    if ((threadIdx.x & 63) == 0) {
+        s_m[threadIdx.x >> 6] = m;
+        s_z[threadIdx.x >> 6] = z;
+        s_b[threadIdx.x >> 6] = best;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kVerifyThreads / 64; ++w) join(m, z, best, s_m[w], s_z[w], s_b[w], inv_t);
+        a.stats[(int64_t)blockIdx.y * a.pieces + piece] = RowStat{m, z, best, 0};
+    }
+}
+
+// p(x) of a row
+__device__ __forceinline__ float share(float x, float m, float z, float inv_t) {
+    return z > 0.f ? expf((logit_of(x) - m) * inv_t) / z : 0.f;
+}
+
+__global__ __launch_bounds__(kVerifyThreads) void verify_race_kernel(VerifyArgs a) {
+    __shared__ RowStat s_row[2 * kMaxDrafts + 1];
+    __shared__ float s_prob[kMaxDrafts];
+    __shared__ Winner s_win[4];
+    __shared__ int s_took;
+    const int i = blockIdx.y, piece = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n = drafts_of(a, i), rows = 2 * a.max_draft + 1;
+    const float inv_t = inv_temperature(a, i);
+    const bool greedy = inv_t == 0.f, with_draft = a.in.draft_logits != nullptr && !greedy;
+    const int need = n + 1 + (with_draft ? n : 0);
+    for (int w = wave; w < need; w += kVerifyThreads / 64) {
+        const int r = w <= n ? w : a.max_draft + w - n;  // target rows 0..n, then the draft's 0..n-1
+        const RowStat* st = a.stats + ((int64_t)i * rows + r) * a.pieces;
+        float m = -INFINITY, z = 0.f;
+        int best = -1;
+        for (int p = lane; p < a.pieces; p += 64) {
+            const RowStat s = st[p];
+            join(m, z, best, s.m, s.z, s.best, inv_t);
+        }
+        join_wave(m, z, best, inv_t);
+        if (lane == 0) s_row[w] = RowStat{m, z, best, 0};
+    }
+    __syncthreads();
+    const float* target = a.in.logits + (int64_t)i * (a.max_draft + 1) * a.in.logits_stride;
+    const float* draft = with_draft ? a.in.draft_logits + (int64_t)i * a.max_draft * a.in.draft_stride : nullptr;
+    const int32_t* tok = a.in.tokens + (int64_t)i * a.max_draft;
+    for (int t = threadIdx.x; t < n; t += kVerifyThreads) {
+        const int x = tok[t];
+        float pr = 0.f;
+        if (x >= 0 && x < a.vocab) {
+            const RowStat p = s_row[t];
+            if (greedy) pr = x == p.best ? 1.f : 0.f;
+            else {
+                const float px = share(target[t * a.in.logits_stride + x], p.m, p.z, inv_t);
+                if (with_draft) {
+                    const RowStat q = s_row[n + 1 + t];
+                    const float qx = share(draft[t * a.in.draft_stride + x], q.m, q.z, inv_t);
+                    pr = qx > 0.f ? fminf(1.f, px / qx) : px > 0.f ? 1.f : 0.f;
+                } else pr = px;
+            }
+        }
+        s_prob[t] = pr;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        int took = 0;
+        while (took < n && a.in.uniforms[(int64_t)i * a.max_draft + took] < s_prob[took]) ++took;
+        s_took = took;
+    }
+    __syncthreads();
+    const int took = s_took;
+    if (piece == 0) {
+        if (a.prob)
+            for (int t = threadIdx.x; t < a.max_draft; t += kVerifyThreads) a.prob[(int64_t)i * a.max_draft + t] = t < n ? s_prob[t] : 0.f;
+        for (int t = threadIdx.x; t <= a.max_draft; t += kVerifyThreads)
+            if (t != took) a.out_tokens[(int64_t)i * (a.max_draft + 1) + t] = t < took ? tok[t] : -1;
+        if (threadIdx.x == 0) a.accepted[i] = took;
+    }
+    const RowStat p = s_row[took];
+    Winner win{-1.f, -1.f, -1, -1};
+    if (greedy) {
+        win.all = win.rest = 1.f;
+        win.all_at = win.rest_at = p.best;
+    } else if (p.z > 0.f) {
+        const bool rejected = took < n;
+        const float* prow = target + took * a.in.logits_stride;
+        const float* qrow = rejected && with_draft ? draft + took * a.in.draft_stride : nullptr;
+        const float* noise = a.in.noise + (int64_t)i * a.vocab;
+        const RowStat q = qrow ? s_row[n + 1 + took] : RowStat{0.f, 0.f, -1, 0};
+        const int without = rejected && !with_draft ? tok[took] : -1;
+        const int x0 = piece * kVerifyPiece, x1 = min(a.vocab, x0 + kVerifyPiece);
+        for (int x = x0 + threadIdx.x; x < x1; x += kVerifyThreads) {
+            const float ps = share(prow[x], p.m, p.z, inv_t), e = noise[x];
+            float rest = ps;
+            if (qrow) rest = fmaxf(ps - share(qrow[x], q.m, q.z, inv_t), 0.f);
+            else if (x == without) rest = 0.f;
+            if (ps > 0.f) {
+                const float f = ps / e;
+                if (f > win.all) {
+                    win.all = f;
+                    win.all_at = x;
+                }
+            }
+            if (rest > 0.f) {
+                const float f = rest / e;
+                if (f > win.rest) {
+                    win.rest = f;
+                    win.rest_at = x;
+                }
+            }
+        }
+    }
+    auto better = [](float& v, int& at, float v2, int at2) {
+        if (at2 >= 0 && (at < 0 || v2 > v || (v2 == v && at2 < at))) {
+            v = v2;
+            at = at2;
+        }
+    };
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        better(win.rest, win.rest_at, __shfl_xor(win.rest, o), __shfl_xor(win.rest_at, o));
+        better(win.all, win.all_at, __shfl_xor(win.all, o), __shfl_xor(win.all_at, o));
+    }
+    if (lane == 0) s_win[wave] = win;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kVerifyThreads / 64; ++w) {
+            better(win.rest, win.rest_at, s_win[w].rest, s_win[w].rest_at);
+            better(win.all, win.all_at, s_win[w].all, s_win[w].all_at);
+        }
+        a.winners[(int64_t)i * a.pieces + piece] = win;
+    }
+}
+
+// one wave per request
+__global__ __launch_bounds__(64) void verify_finish_kernel(VerifyArgs a) {
+    const int i = blockIdx.x, lane = threadIdx.x;
+    Winner win{-1.f, -1.f, -1, -1};
+    auto better = [](float& v, int& at, float v2, int at2) {
+        if (at2 >= 0 && (at < 0 || v2 > v || (v2 == v && at2 < at))) {
+            v = v2;
+            at = at2;
+        }
+    };
+    for (int p = lane; p < a.pieces; p += 64) {
+        const Winner w = a.winners[(int64_t)i * a.pieces + p];
+        better(win.rest, win.rest_at, w.rest, w.rest_at);
+        better(win.all, win.all_at, w.all, w.all_at);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        better(win.rest, win.rest_at, __shfl_xor(win.rest, o), __shfl_xor(win.rest_at, o));
+        better(win.all, win.all_at, __shfl_xor(win.all, o), __shfl_xor(win.all_at, o));
+    }
+    if (lane == 0) a.out_tokens[(int64_t)i * (a.max_draft + 1) + a.accepted[i]] = win.rest_at >= 0 ? win.rest_at : win.all_at;
+}
+
+static int verify_pieces(int vocab) { return (vocab + kVerifyPiece - 1) / kVerifyPiece; }
+
+}  // namespace chiron
+
+using namespace chiron;
+
+extern "C" {
+
+int64_t chiron_verify_workspace_bytes(int32_t batch, int32_t max_draft, int32_t vocab) {
+    if (batch < 0 || max_draft < 0 || max_draft > kMaxDrafts || vocab < 1) return 0;
+    return (int64_t)batch * verify_pieces(vocab) * ((2 * max_draft + 1) * (int64_t)sizeof(RowStat) + (int64_t)sizeof(Winner));
+}
+
+int32_t chiron_op_verify_drafts(const chiron_draft_batch* in, int32_t batch, int32_t max_draft, int32_t vocab, int32_t* out_tokens,
+                                int32_t* accepted, float* prob, void* workspace, void* stream) {
+    if (!in) return fail(CHIRON_ERR_INVALID_ARG, "verify: the batch is null");
+    if (batch < 0 || max_draft < 0 || vocab < 1) return fail(CHIRON_ERR_INVALID_ARG, "verify: bad sizes");
+    if (max_draft > kMaxDrafts) return fail(CHIRON_ERR_SHAPE, "verify: %d drafted tokens, at most %d", max_draft, kMaxDrafts);
+    if (batch == 0) return CHIRON_OK;
+    if (!in->logits || !in->noise || !out_tokens || !accepted || !workspace || (max_draft > 0 && (!in->tokens || !in->uniforms)))
+        return fail(CHIRON_ERR_INVALID_ARG, "verify: a pointer is null");
+    if (in->logits_stride < vocab || (in->draft_logits && in->draft_stride < vocab))
+        return fail(CHIRON_ERR_INVALID_ARG, "verify: a row stride is smaller than the vocabulary");
+    if ((uintptr_t)workspace & 15) return fail(CHIRON_ERR_INVALID_ARG, "verify: the workspace must be 16-byte aligned");
+    const int pieces = verify_pieces(vocab);
+    const int64_t rows = (int64_t)batch * (2 * max_draft + 1);
+    if (rows > 65535) return fail(CHIRON_ERR_BATCH_TOO_LARGE, "verify: %d requests of %d drafts are too many for one call", batch, max_draft);
+    VerifyArgs a;
+    a.in = *in;
+    a.batch = batch; a.max_draft = max_draft; a.vocab = vocab; a.pieces = pieces;
+    a.stats = (RowStat*)workspace;
+    a.winners = (Winner*)((char*)workspace + rows * pieces * (int64_t)sizeof(RowStat));
+    a.out_tokens = out_tokens; a.accepted = accepted; a.prob = prob;
+    hipStream_t st = (hipStream_t)stream;
+    launch(verify_stats_kernel, dim3(pieces, (unsigned)rows), dim3(kVerifyThreads), st, a);
+    launch(verify_race_kernel, dim3(pieces, batch), dim3(kVerifyThreads), st, a);
+    launch(verify_finish_kernel, dim3(batch), dim3(64), st, a);
+    CHIRON_HIP(hipGetLastError());
+    return CHIRON_OK;
+}
+
+}  // extern "C"
