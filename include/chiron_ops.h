@@ -147,10 +147,14 @@ int32_t chiron_linear4_create(const void *w4, const void *scales, const void *ze
                               void *stream, chiron_linear4 **out);
 int32_t chiron_linear4_destroy(chiron_linear4 *l);
 
-/* y[M,N] = x[M,K] * W^T, or y += (accumulate != 0).  x, y dev fp32 row-major, not overlapping.  Per row and group, x enters
- * as whole multiples of a power of two, 2^22 at the group's largest value (an error of at most 2^-23 of it), in three 8-bit
- * digits whose products are exact; groups are added in fp32.  A NaN or an infinity in a row of x makes that row of y NaN. */
-int32_t chiron_op_linear4(const chiron_linear4 *l, const float *x, int32_t M, float *y, int32_t accumulate, void *stream);
+/* y[M,N] = x[M,K] * W^T, or y += (accumulate != 0).  x, y dev fp32 row-major, not overlapping.  Per row and 128 inputs, x
+ * enters as whole multiples of a power of two, at most 2^22 of them (an error of at most 2^-23 of the largest value, or
+ * 2^-128), in three 8-bit digits whose products are exact; groups are added in fp32.  A NaN or an infinity in a row of x makes that row of y NaN. */
+int32_t chiron_op_linear4(const chiron_linear4 *l, const float *x, int32_t M, float *y, int32_t accumulate, void *workspace,
+                          void *stream);
+/* workspace: dev, that many bytes, 16-byte aligned, caller-owned, in use until the stream has passed; 0 (null
+ * will do) for few rows of few inputs. */
+int64_t chiron_linear4_workspace_bytes(const chiron_linear4 *l, int32_t M);
 
 /* Performance knobs of the kernels, process-wide (0 restores the built-in heuristic where one exists):
  *   linear_nf (1|2|4), linear_mt (1|2|3|4), linear_xcd_remap (0|1), linear_ksplit, linear_target_blocks,

@@ -31,6 +31,7 @@ SYMBOLS = [
     "chiron_append_kv_rope", "chiron_kv_index_bytes", "chiron_kv_index_create", "chiron_kv_index_destroy", "chiron_kv_index_update",
     "chiron_op_rope_table", "chiron_op_select_pages", "chiron_op_sparse_attention", "chiron_verify_workspace_bytes",
     "chiron_op_verify_drafts", "chiron_linear4_create", "chiron_linear4_destroy", "chiron_op_linear4",
+    "chiron_linear4_workspace_bytes",
 ]
 
 
@@ -75,7 +76,7 @@ _HOT = {"chiron_decode_step": "pppppipp", "chiron_decode_step_multi": "pppppiipp
         "chiron_op_gate_up_swiglu": "ppipp", "chiron_op_swiglu_ffn": "pppipip", "chiron_op_paged_attention": "ppipppipp",
         "chiron_append_kv_rope": "ppippippiip", "chiron_kv_index_update": "ppiipippiip", "chiron_op_select_pages": "pppippppiiiippp",
         "chiron_op_sparse_attention": "ppippppippipp", "chiron_verify_workspace_bytes": "iii", "chiron_op_verify_drafts": "piiippppp",
-        "chiron_op_linear4": "ppipip"}
+        "chiron_op_linear4": "ppipipp", "chiron_linear4_workspace_bytes": "pi"}
 _TYPES = {"p": C.c_void_p, "i": C.c_int32, "l": C.c_int64}
 
 
@@ -91,6 +92,7 @@ def load():
         lib.chiron_kv_block_bytes.restype = C.c_int64
         lib.chiron_kv_index_bytes.restype = C.c_int64
         lib.chiron_verify_workspace_bytes.restype = C.c_int64
+        lib.chiron_linear4_workspace_bytes.restype = C.c_int64
         for name, types in _HOT.items():
             getattr(lib, name).argtypes = [_TYPES[t] for t in types]
         _lib = lib
@@ -650,8 +652,10 @@ class Linear4:
             y = torch.empty((M, self.N), dtype=torch.float32, device=x.device)
         elif y.numel() != M * self.N:
             raise ValueError("y must be [%d, %d], got %s" % (M, self.N, tuple(y.shape)))
+        need = load().chiron_linear4_workspace_bytes(self._h, M)
+        work = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
         _check(load().chiron_op_linear4(self._h, _address(x, torch.float32), M, _address(y, torch.float32), 1 if accumulate else 0,
-                                        _stream_number()))
+                                        _address(work), _stream_number()))
         return y
 
     def close(self):

@@ -49,10 +49,7 @@ __device__ __forceinline__ int row_move(int v) {
 }
 constexpr int kRor1 = 0x121, kRor2 = 0x122, kRor4 = 0x124, kRor8 = 0x128;  // row_ror:n, rotation within 16 lanes
 
-// scratch of a call on `st`, from the pool that the handles of device `dev` keep (api.hip); freed with hipFreeAsync
-int32_t scratch_alloc(int dev, void** out, size_t bytes, hipStream_t st);
-int scratch_pool_enter();
-void scratch_pool_leave(int dev);
+// device memory of a handle (api.hip)
 int32_t dev_alloc(void** p, size_t bytes);
 
 }  // namespace chiron

@@ -36,6 +36,9 @@ struct VerifyArgs {
     float* prob;
 };
 
+// exp(d / T) with c = log2(e) / T, for sums: |d / T| 2^-24 off, where that is much the term is small
+__device__ __forceinline__ float weight(float d, float c) { return __builtin_amdgcn_exp2f(d * c); }
+__device__ __forceinline__ float log2e_over(float inv_t) { return fminf(inv_t * 1.44269504088896341f, kTopF32); }
 __device__ __forceinline__ float logit_of(float x) { return x != x ? -INFINITY : fminf(x, kTopF32); }
 __device__ __forceinline__ float inv_temperature(const VerifyArgs& a, int i) {
     if (!a.in.temperature) return 1.f;
@@ -46,62 +49,77 @@ __device__ __forceinline__ int drafts_of(const VerifyArgs& a, int i) {
     return a.in.draft_lens ? min(max(a.in.draft_lens[i], 0), a.max_draft) : a.max_draft;
 }
 // joins two statistics of one row; of equal maxima the lower index
-__device__ __forceinline__ void join(float& m, float& z, int& best, float m2, float z2, int best2, float inv_t) {
+__device__ __forceinline__ void join(float& m, float& z, int& best, float m2, float z2, int best2, float c) {
     if (m2 == -INFINITY) return;
     if (m == -INFINITY) {
         m = m2; z = z2; best = best2;
         return;
     }
     if (m2 > m) {
-        z = z * expf((m - m2) * inv_t) + z2;
+        z = z * weight(m - m2, c) + z2;
         m = m2;
         best = best2;
     } else {
-        z += z2 * expf((m2 - m) * inv_t);
+        z += z2 * weight(m2 - m, c);
         if (m2 == m) best = min(best, best2);
     }
 }
-__device__ __forceinline__ void join_wave(float& m, float& z, int& best, float inv_t) {
+// joins over LANES neighbouring lanes
+template <int LANES>
+__device__ __forceinline__ void join_lanes(float& m, float& z, int& best, float c) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
+    for (int o = LANES / 2; o > 0; o >>= 1) {
         const float m2 = __shfl_xor(m, o), z2 = __shfl_xor(z, o);
         const int b2 = __shfl_xor(best, o);
-        join(m, z, best, m2, z2, b2, inv_t);
+        join(m, z, best, m2, z2, b2, c);
     }
 }
 
+// Rows of any length begin at any multiple of 4 bytes: a piece is 1024 vectors of 16 bytes counted from the 16-byte boundary at or
+// before the row's start, and only vectors that lie wholly within the row are loaded as such.
 __global__ __launch_bounds__(kVerifyThreads) void verify_stats_kernel(VerifyArgs a) {
     __shared__ float s_m[4], s_z[4];
     __shared__ int s_b[4];
     const int rows = 2 * a.max_draft + 1;
     const int i = blockIdx.y / rows, r = blockIdx.y % rows, piece = blockIdx.x;
     const int n = drafts_of(a, i);
-    const float inv_t = inv_temperature(a, i);
+    const float inv_t = inv_temperature(a, i), c = log2e_over(inv_t);
     const bool draft = r > a.max_draft;
     const int t = draft ? r - a.max_draft - 1 : r;
     if (draft ? (t >= n || !a.in.draft_logits || inv_t == 0.f) : t > n) return;  // nobody asks for this row
     const float* row = draft ? a.in.draft_logits + ((int64_t)i * a.max_draft + t) * a.in.draft_stride
                              : a.in.logits + ((int64_t)i * (a.max_draft + 1) + t) * a.in.logits_stride;
-    const int x0 = piece * kVerifyPiece, x1 = min(a.vocab, x0 + kVerifyPiece);
-    constexpr int VPT = kVerifyPiece / kVerifyThreads;
-    float v[VPT];
+    const int shift = (int)((uintptr_t)row >> 2 & 3);
+    constexpr int VPT = kVerifyPiece / kVerifyThreads / 4;
+    float4 v[VPT];
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+        const int x = (piece * (kVerifyPiece / 4) + j * kVerifyThreads + threadIdx.x) * 4 - shift;
+        if (x >= 0 && x + 4 <= a.vocab) v[j] = *reinterpret_cast<const float4*>(row + x);
+        else {
+            float* p = &v[j].x;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) p[k] = x + k >= 0 && x + k < a.vocab ? row[x + k] : -INFINITY;
+        }
+    }
     float m = -INFINITY, z = 0.f;
     int best = -1;
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
-        const int x = x0 + j * kVerifyThreads + threadIdx.x;
-        v[j] = x < x1 ? logit_of(row[x]) : -INFINITY;
-    }
+        float* p = &v[j].x;
 #pragma unroll
-    for (int j = 0; j < VPT; ++j)
-        if (v[j] > m) {
-            m = v[j];
-            best = x0 + j * kVerifyThreads + threadIdx.x;
+        for (int k = 0; k < 4; ++k) {
+            p[k] = logit_of(p[k]);
+            if (p[k] > m) {
+                m = p[k];
+                best = (piece * (kVerifyPiece / 4) + j * kVerifyThreads + threadIdx.x) * 4 - shift + k;
+            }
         }
+    }
     if (m > -INFINITY)
 #pragma unroll
-        for (int j = 0; j < VPT; ++j) z += expf((v[j] - m) * inv_t);
-    join_wave(m, z, best, inv_t);
+        for (int j = 0; j < VPT; ++j) z += (weight(v[j].x - m, c) + weight(v[j].y - m, c)) + (weight(v[j].z - m, c) + weight(v[j].w - m, c));
+    join_lanes<64>(m, z, best, c);
     if ((threadIdx.x & 63) == 0) {
         s_m[threadIdx.x >> 6] = m;
         s_z[threadIdx.x >> 6] = z;
@@ -109,7 +127,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_stats_kernel(VerifyArgs
     }
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kVerifyThreads / 64; ++w) join(m, z, best, s_m[w], s_z[w], s_b[w], inv_t);
+        for (int w = 1; w < kVerifyThreads / 64; ++w) join(m, z, best, s_m[w], s_z[w], s_b[w], c);
         a.stats[(int64_t)blockIdx.y * a.pieces + piece] = RowStat{m, z, best, 0};
     }
 }
@@ -124,46 +142,66 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_race_kernel(VerifyArgs 
     __shared__ float s_prob[kMaxDrafts];
     __shared__ Winner s_win[4];
     __shared__ int s_took;
-    const int i = blockIdx.y, piece = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int n = drafts_of(a, i), rows = 2 * a.max_draft + 1;
-    const float inv_t = inv_temperature(a, i);
-    const bool greedy = inv_t == 0.f, with_draft = a.in.draft_logits != nullptr && !greedy;
+    const int i = blockIdx.y, piece = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t0 = threadIdx.x;
+    const int rows = 2 * a.max_draft + 1;
+    const float* target = a.in.logits + (int64_t)i * (a.max_draft + 1) * a.in.logits_stride;
+    const float* draft = a.in.draft_logits ? a.in.draft_logits + (int64_t)i * a.max_draft * a.in.draft_stride : nullptr;
+    const int32_t* tok = a.in.tokens + (int64_t)i * a.max_draft;
+    // A chain of loads, each a microsecond, is what this kernel takes with few requests: what does not wait for the rows' sums and the
+    // decision is on its way first.
+    const int x0 = piece * kVerifyPiece + t0;
+    constexpr int VPT = kVerifyPiece / kVerifyThreads;
+    float noise[VPT];
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) noise[j] = x0 + j * kVerifyThreads < a.vocab ? a.in.noise[(int64_t)i * a.vocab + x0 + j * kVerifyThreads] : 1.f;
+    int my_tok = -1;
+    float my_target = 0.f, my_draft = 0.f;
+    if (t0 < a.max_draft) {
+        my_tok = tok[t0];
+        if (my_tok >= 0 && my_tok < a.vocab) {
+            my_target = target[t0 * a.in.logits_stride + my_tok];
+            if (draft) my_draft = draft[t0 * a.in.draft_stride + my_tok];
+        } else my_tok = -1;
+    }
+    const int n = drafts_of(a, i);
+    const float inv_t = inv_temperature(a, i), c = log2e_over(inv_t);
+    const bool greedy = inv_t == 0.f, with_draft = draft && !greedy;
     const int need = n + 1 + (with_draft ? n : 0);
-    for (int w = wave; w < need; w += kVerifyThreads / 64) {
+    // 16 lanes join a row's pieces
+    for (int w = t0 / 16; w - t0 / 16 < need; w += kVerifyThreads / 16) {
         const int r = w <= n ? w : a.max_draft + w - n;  // target rows 0..n, then the draft's 0..n-1
-        const RowStat* st = a.stats + ((int64_t)i * rows + r) * a.pieces;
         float m = -INFINITY, z = 0.f;
         int best = -1;
-        for (int p = lane; p < a.pieces; p += 64) {
-            const RowStat s = st[p];
-            join(m, z, best, s.m, s.z, s.best, inv_t);
+        if (w < need) {
+            const RowStat* st = a.stats + ((int64_t)i * rows + r) * a.pieces;
+            for (int p = t0 % 16; p < a.pieces; p += 16) {
+                const RowStat s = st[p];
+                join(m, z, best, s.m, s.z, s.best, c);
+            }
         }
-        join_wave(m, z, best, inv_t);
-        if (lane == 0) s_row[w] = RowStat{m, z, best, 0};
+        join_lanes<16>(m, z, best, c);
+        if (w < need && t0 % 16 == 0) s_row[w] = RowStat{m, z, best, 0};
     }
     __syncthreads();
-    const float* target = a.in.logits + (int64_t)i * (a.max_draft + 1) * a.in.logits_stride;
-    const float* draft = with_draft ? a.in.draft_logits + (int64_t)i * a.max_draft * a.in.draft_stride : nullptr;
-    const int32_t* tok = a.in.tokens + (int64_t)i * a.max_draft;
-    for (int t = threadIdx.x; t < n; t += kVerifyThreads) {
-        const int x = tok[t];
+    static_assert(kMaxDrafts <= kVerifyThreads, "a thread per draft");
+    if (t0 < n) {
         float pr = 0.f;
-        if (x >= 0 && x < a.vocab) {
-            const RowStat p = s_row[t];
-            if (greedy) pr = x == p.best ? 1.f : 0.f;
+        if (my_tok >= 0) {
+            const RowStat p = s_row[t0];
+            if (greedy) pr = my_tok == p.best ? 1.f : 0.f;
             else {
-                const float px = share(target[t * a.in.logits_stride + x], p.m, p.z, inv_t);
+                const float px = share(my_target, p.m, p.z, inv_t);
                 if (with_draft) {
-                    const RowStat q = s_row[n + 1 + t];
-                    const float qx = share(draft[t * a.in.draft_stride + x], q.m, q.z, inv_t);
+                    const RowStat q = s_row[n + 1 + t0];
+                    const float qx = share(my_draft, q.m, q.z, inv_t);
                     pr = qx > 0.f ? fminf(1.f, px / qx) : px > 0.f ? 1.f : 0.f;
                 } else pr = px;
             }
         }
-        s_prob[t] = pr;
+        s_prob[t0] = pr;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
+    if (t0 == 0) {
         int took = 0;
         while (took < n && a.in.uniforms[(int64_t)i * a.max_draft + took] < s_prob[took]) ++took;
         s_took = took;
@@ -172,10 +210,10 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_race_kernel(VerifyArgs 
     const int took = s_took;
     if (piece == 0) {
         if (a.prob)
-            for (int t = threadIdx.x; t < a.max_draft; t += kVerifyThreads) a.prob[(int64_t)i * a.max_draft + t] = t < n ? s_prob[t] : 0.f;
-        for (int t = threadIdx.x; t <= a.max_draft; t += kVerifyThreads)
+            for (int t = t0; t < a.max_draft; t += kVerifyThreads) a.prob[(int64_t)i * a.max_draft + t] = t < n ? s_prob[t] : 0.f;
+        for (int t = t0; t <= a.max_draft; t += kVerifyThreads)
             if (t != took) a.out_tokens[(int64_t)i * (a.max_draft + 1) + t] = t < took ? tok[t] : -1;
-        if (threadIdx.x == 0) a.accepted[i] = took;
+        if (t0 == 0) a.accepted[i] = took;
     }
     const RowStat p = s_row[took];
     Winner win{-1.f, -1.f, -1, -1};
@@ -186,28 +224,32 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_race_kernel(VerifyArgs 
         const bool rejected = took < n;
         const float* prow = target + took * a.in.logits_stride;
         const float* qrow = rejected && with_draft ? draft + took * a.in.draft_stride : nullptr;
-        const float* noise = a.in.noise + (int64_t)i * a.vocab;
         const RowStat q = qrow ? s_row[n + 1 + took] : RowStat{0.f, 0.f, -1, 0};
         const int without = rejected && !with_draft ? tok[took] : -1;
-        const int x0 = piece * kVerifyPiece, x1 = min(a.vocab, x0 + kVerifyPiece);
-        for (int x = x0 + threadIdx.x; x < x1; x += kVerifyThreads) {
-            const float ps = share(prow[x], p.m, p.z, inv_t), e = noise[x];
+        float pv[VPT], qv[VPT];
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) pv[j] = x0 + j * kVerifyThreads < a.vocab ? prow[x0 + j * kVerifyThreads] : -INFINITY;
+        if (qrow)
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) qv[j] = x0 + j * kVerifyThreads < a.vocab ? qrow[x0 + j * kVerifyThreads] : -INFINITY;
+        // exponentials and quotients of the machine's own precision: 2 to 3 units in the last place, as far as who wins a race goes
+        const float rp = 1.f / p.z, rq = q.z > 0.f ? 1.f / q.z : 0.f;
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int x = x0 + j * kVerifyThreads;
+            const float inv = __builtin_amdgcn_rcpf(noise[j]);
+            const float ps = weight(logit_of(pv[j]) - p.m, c) * rp;
             float rest = ps;
-            if (qrow) rest = fmaxf(ps - share(qrow[x], q.m, q.z, inv_t), 0.f);
+            if (qrow) rest = fmaxf(ps - (rq > 0.f ? weight(logit_of(qv[j]) - q.m, c) * rq : 0.f), 0.f);
             else if (x == without) rest = 0.f;
-            if (ps > 0.f) {
-                const float f = ps / e;
-                if (f > win.all) {
-                    win.all = f;
-                    win.all_at = x;
-                }
+            const float all = ps * inv, some = rest * inv;
+            if (ps > 0.f && all > win.all) {
+                win.all = all;
+                win.all_at = x;
             }
-            if (rest > 0.f) {
-                const float f = rest / e;
-                if (f > win.rest) {
-                    win.rest = f;
-                    win.rest_at = x;
-                }
+            if (rest > 0.f && some > win.rest) {
+                win.rest = some;
+                win.rest_at = x;
             }
         }
     }
@@ -256,7 +298,7 @@ __global__ __launch_bounds__(64) void verify_finish_kernel(VerifyArgs a) {
     if (lane == 0) a.out_tokens[(int64_t)i * (a.max_draft + 1) + a.accepted[i]] = win.rest_at >= 0 ? win.rest_at : win.all_at;
 }
 
-static int verify_pieces(int vocab) { return (vocab + kVerifyPiece - 1) / kVerifyPiece; }
+static int verify_pieces(int vocab) { return (int)(((int64_t)vocab + 3 + kVerifyPiece - 1) / kVerifyPiece); }  // up to 3 values before an aligned start
 
 }  // namespace chiron
 

@@ -4,8 +4,8 @@ attention over listed pages, verification of drafts, 4-bit products.  Needs a re
 Tolerances.  Whole numbers (index records, page lists, tokens) are equal.  Stored bf16 keys: half a unit in the last place of the
 exact value plus the fp32 rounding of two products.  Attention: a softmax whose logits are off by at most s moves an average of
 values by at most 2 s max|v|, with s from the products' own magnitudes, plus 2^-20 max|v| for the exponentials and the sums.
-Probabilities: 2^-16 relative (logits up to 100 in an fp32 exponential).  4-bit products: 2^-23 of a group's largest |x| per product
-of the group, and the fp32 additions over the groups."""
+Probabilities: 2^-16 relative (logits up to 100 in an fp32 exponential).  4-bit products: 2^-23 of the largest |x| of its 128 inputs per
+product, and the fp32 additions over the groups."""
 import numpy as np
 import pytest
 import torch
@@ -553,8 +553,9 @@ def check_linear4(lin, w, s, x, group, y0=None, accumulate=False):
     xk = np.where(ok[:, None], xd, 0.0)
     want = xk @ w.T + (y0.double().numpy() if accumulate else 0)
     groups = K // group
-    top = abs(xk).reshape(M, groups, group).max(2)
-    # the rounding of x: 2^-23 of the group's largest value for each of its products; sums over the groups in fp32
+    blocks = -(-K // 128)
+    top = np.abs(np.pad(xk, ((0, 0), (0, blocks * 128 - K)))).reshape(M, blocks, 128).max(2).repeat(128 // group, 1)[:, :groups]
+    # the rounding of x: 2^-23 of the largest value of its 128 for each product; sums over the groups in fp32
     digits = (top[:, None, :] * 2.0 ** -23 * abs(w).reshape(1, lin.N, groups, group).sum(3)).sum(2)
     parts = abs(np.einsum("mgk,ngk->mng", xk.reshape(M, groups, group), w.reshape(lin.N, groups, group)))
     sums = (groups + 6) * 2.0 ** -24 * (parts.sum(2) + (abs(y0.double().numpy()) if accumulate else 0))
@@ -606,6 +607,15 @@ def test_linear4_larger(N, K, group, M, zeros):
         def __call__(self, x, y, accumulate):
             return sub
     check_linear4(Rows(), w, sk, x, group)
+
+
+@pytest.mark.parametrize("M", (3, 7, 12, 20))
+def test_linear4_rows_that_are_not_aligned(M):
+    w4, s, z = weights(40, 384, 128, False, 5)
+    lin = B.Linear4(w4.cuda(), s.cuda())
+    flat = torch.randn(M * 384 + 3, generator=torch.Generator().manual_seed(6)).cuda()
+    for shift in (1, 2, 3):
+        assert torch.equal(lin(flat[shift:shift + M * 384].view(M, 384)), lin(flat[shift:shift + M * 384].view(M, 384).clone()))
 
 
 @pytest.mark.parametrize("M", (2, 6, 40))
