@@ -140,6 +140,9 @@ def _stream_number():
     return _raw_stream(torch._C._cuda_getDevice())
 
 
+_ROW_TYPES = {torch.float32: CHIRON_F32, torch.bfloat16: CHIRON_BF16}
+
+
 def _rows_of(t, rows, heads, d, dtype):
     """address and row stride of t [rows, heads, d], heads and dims contiguous"""
     if not t.is_cuda:
@@ -148,9 +151,12 @@ def _rows_of(t, rows, heads, d, dtype):
         raise TypeError("expected %s, got %s" % (dtype, t.dtype))
     if t.shape != (rows, heads, d):
         raise ValueError("expected [%d, %d, %d], got %s" % (rows, heads, d, tuple(t.shape)))
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d) or (rows > 1 and t.stride(0) < heads * d):
+    s0, s1, s2 = t.stride()
+    if rows < 2:
+        s0 = heads * d
+    if s2 != 1 or (s1 != d and heads > 1) or s0 < heads * d:
         raise TypeError("heads and dims of a row must be contiguous")
-    return t.data_ptr(), t.stride(0) if rows > 1 else heads * d
+    return t.data_ptr(), s0
 
 
 def make_config(m, max_batch, max_blocks_per_seq):
@@ -209,6 +215,7 @@ class KVPool:
                                             C.c_int32(block_size), C.byref(self._h), C.byref(nb)))
         self.num_blocks = nb.value
         self.block_size = block_size
+        self._views = {}  # layer -> torch views of the memory
 
     def append(self, layer, k, v, block_table, seq_idx, pos):
         n = seq_idx.numel()
@@ -231,44 +238,47 @@ class KVPool:
         projection's rows, for one); cos, sin fp32 [rows, head_dim/2] (rope_table); request i brings the rows row_starts[i] ..
         row_starts[i+1]-1 at the positions from seq_lens[i] on.  index: a KVIndex to bring up to date.  Returns the rotated q, fp32."""
         cfg = self.model.cfg
-        rows, batch = k.shape[0], seq_lens.numel()
-        if k.dtype not in (torch.float32, torch.bfloat16):
-            raise TypeError("expected torch.float32 or torch.bfloat16, got %s" % k.dtype)
-        if block_table.dim() != 2 or block_table.shape[0] < batch or row_starts.numel() != batch + 1:
+        rows, batch, d, dtype = k.shape[0], seq_lens.numel(), cfg.head_dim, k.dtype
+        if dtype not in _ROW_TYPES:
+            raise TypeError("expected torch.float32 or torch.bfloat16, got %s" % dtype)
+        width = block_table.shape[1] if block_table.dim() == 2 else -1
+        if width < 0 or block_table.shape[0] < batch or row_starts.numel() != batch + 1:
             raise ValueError("%d requests need %d row starts and as many rows of the block table, got %d and %s" % (
                 batch, batch + 1, row_starts.numel(), tuple(block_table.shape)))
-        for t in (cos, sin):
-            if t.numel() != rows * (cfg.head_dim // 2):
-                raise ValueError("cos and sin must be [%d, %d], got %s" % (rows, cfg.head_dim // 2, tuple(t.shape)))
-        r = NewRows()
-        r.k, r.k_stride = _rows_of(k, rows, cfg.n_kv_heads, cfg.head_dim, k.dtype)
-        r.v, r.v_stride = _rows_of(v, rows, cfg.n_kv_heads, cfg.head_dim, k.dtype)
-        r.dtype = CHIRON_F32 if k.dtype == torch.float32 else CHIRON_BF16
-        r.cos, r.sin = _address(cos, torch.float32), _address(sin, torch.float32)
+        if cos.numel() != rows * (d // 2) or sin.numel() != cos.numel():
+            raise ValueError("cos and sin must be [%d, %d], got %s and %s" % (rows, d // 2, tuple(cos.shape), tuple(sin.shape)))
+        kp, ks = _rows_of(k, rows, cfg.n_kv_heads, d, dtype)
+        vp, vs = _rows_of(v, rows, cfg.n_kv_heads, d, dtype)
+        qp = qs = heads = out = 0
         if q is not None:
-            r.n_q_heads = q.shape[1]
-            r.q, r.q_stride = _rows_of(q, rows, q.shape[1], cfg.head_dim, k.dtype)
+            heads = q.shape[1]
+            qp, qs = _rows_of(q, rows, heads, d, dtype)
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+                q_out = torch.empty((rows, heads, d), dtype=torch.float32, device=q.device)
             elif q_out.shape != q.shape:
                 raise ValueError("q_out must have q's shape %s, got %s" % (tuple(q.shape), tuple(q_out.shape)))
-            r.q_out = _address(q_out, torch.float32)
+            out = _address(q_out, torch.float32)
+        r = NewRows(qp, kp, vp, qs, ks, vs, _ROW_TYPES[dtype], heads, _address(cos, torch.float32), _address(sin, torch.float32), out)
         _check(load().chiron_append_kv_rope(self._h, index._h if index is not None else None, _whole(layer), C.addressof(r),
-                                            _address(block_table, torch.int32), block_table.shape[1], _address(row_starts, torch.int32),
+                                            _address(block_table, torch.int32), width, _address(row_starts, torch.int32),
                                             _address(seq_lens, torch.int32), batch, rows, _stream_number()))
         return q_out
 
     def layer_views(self, layer):
         """The pool's memory of one layer as torch views without a copy: K [page, token, head, d/8, 8] and V [page, 4, 4 (token),
         head, d/32, 2, 16]; reshape either to [page, 16, head, d] for a copy in logical order."""
+        layer = index(layer)
+        if layer in self._views:
+            return self._views[layer]
         cfg, nb = self.model.cfg, self.num_blocks
-        n, d, layer = cfg.n_kv_heads, cfg.head_dim, index(layer)
+        n, d = cfg.n_kv_heads, cfg.head_dim
         if not 0 <= layer < cfg.n_layers:
             raise IndexError("layer %d out of range" % layer)
         size = nb * n * 2 * 16 * d
         t = self.memory.view(torch.uint8).view(-1)[layer * size * 2:(layer + 1) * size * 2].view(torch.bfloat16).view(nb, n, 2, 16 * d)
         k = t[:, :, 0].unflatten(2, (d // 8, 16, 8)).permute(0, 3, 1, 2, 4)
         v = t[:, :, 1].unflatten(2, (d // 32, 4, 16, 2, 4)).permute(0, 3, 6, 1, 2, 5, 4)
+        self._views[layer] = (k, v)
         return k, v
 
     def swap_out(self, block_table_row, n_pages, image):
@@ -638,6 +648,7 @@ class Linear4:
         if scales.shape[0] != self.N or groups < 1 or self.K % groups != 0 or (zeros is not None and zeros.shape != scales.shape):
             raise ValueError("w4 %s, scales %s and zeros %s do not fit" % (tuple(w4.shape), tuple(scales.shape), None if zeros is None else tuple(zeros.shape)))
         self.group = self.K // groups
+        self._work = {}  # rows -> bytes of workspace
         self._h = C.c_void_p()
         _check(load().chiron_linear4_create(_ptr(w4, torch.uint8), _ptr(scales, torch.bfloat16), _ptr(zeros, torch.uint8), C.c_int32(self.N),
                                             C.c_int32(self.K), C.c_int32(self.group), _stream(), C.byref(self._h)))
@@ -652,7 +663,9 @@ class Linear4:
             y = torch.empty((M, self.N), dtype=torch.float32, device=x.device)
         elif y.numel() != M * self.N:
             raise ValueError("y must be [%d, %d], got %s" % (M, self.N, tuple(y.shape)))
-        need = load().chiron_linear4_workspace_bytes(self._h, M)
+        need = self._work.get(M)
+        if need is None:
+            need = self._work[M] = load().chiron_linear4_workspace_bytes(self._h, M)
         work = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
         _check(load().chiron_op_linear4(self._h, _address(x, torch.float32), M, _address(y, torch.float32), 1 if accumulate else 0,
                                         _address(work), _stream_number()))

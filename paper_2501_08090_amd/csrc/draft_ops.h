@@ -49,6 +49,12 @@ __device__ __forceinline__ int row_move(int v) {
 }
 constexpr int kRor1 = 0x121, kRor2 = 0x122, kRor4 = 0x124, kRor8 = 0x128;  // row_ror:n, rotation within 16 lanes
 
+// a launch with dynamic LDS
+template <typename... P, typename... A>
+inline void launch_lds(void (*kernel)(P...), dim3 grid, dim3 block, size_t lds, hipStream_t st, A... args) {
+    kernel<<<grid, block, lds, st>>>(static_cast<P>(args)...);
+}
+
 // device memory of a handle (api.hip)
 int32_t dev_alloc(void** p, size_t bytes);
 

@@ -24,37 +24,29 @@ struct SelectArgs {
     int layer, max_blocks, rows, top, n_first, n_last;
 };
 
-template <int D, int G>
-__global__ __launch_bounds__(256) void page_scores_kernel(SelectArgs a) {
-    constexpr int KS = D / 32;  // steps of 64 codes: the first half meets the bounds from above, the second those from below
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int n_kv = a.pool.n_kv, row = blockIdx.x / n_kv, c = blockIdx.x % n_kv;
-    const int ctx = a.ctx_lens[row];
-    const int n = min((int)(((int64_t)ctx + kBlockSize - 1) / kBlockSize), a.max_blocks);
-    if (n <= a.top) return;  // every page is taken: nobody reads the scores
-    const int seq = a.row_seq ? a.row_seq[row] : row;
-    const int32_t* btrow = a.bt + (size_t)seq * a.max_blocks;
-    const int col = lane & 15, g = lane >> 4;
+constexpr float kTop = 3.4028234663852886e38f;
 
-    // q8 in operand layout: column = head, 16 consecutive dims per lane group and step of 64
-    const float* qp = a.q + ((size_t)row * n_kv + c) * (G * D) + (col % G) * D + g * 16;
+// q8 of one (row, KV head) as B operand: column = head, 16 consecutive dims per lane group and step of 64; the positive ones first
+template <int D, int G>
+__device__ __forceinline__ void load_q8(const float* q, intx4 (&b)[D / 32]) {
+    const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+    const float* qp = q + (col % G) * D + g * 16;
     float x[D / 64][16], amax = 0.f;
 #pragma unroll
     for (int s = 0; s < D / 64; ++s)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const float4 v = *reinterpret_cast<const float4*>(qp + s * 64 + i);
-            x[s][i] = finite_or(v.x, 3.4028234663852886e38f);
-            x[s][i + 1] = finite_or(v.y, 3.4028234663852886e38f);
-            x[s][i + 2] = finite_or(v.z, 3.4028234663852886e38f);
-            x[s][i + 3] = finite_or(v.w, 3.4028234663852886e38f);
+            x[s][i] = finite_or(v.x, kTop);
+            x[s][i + 1] = finite_or(v.y, kTop);
+            x[s][i + 2] = finite_or(v.z, kTop);
+            x[s][i + 3] = finite_or(v.w, kTop);
 #pragma unroll
             for (int u = 0; u < 4; ++u) amax = fmaxf(amax, fabsf(x[s][i + u]));
         }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
     const float up = two_to(-power_of(amax));
-    intx4 b[KS];
 #pragma unroll
     for (int s = 0; s < D / 64; ++s)
 #pragma unroll
@@ -69,21 +61,32 @@ __global__ __launch_bounds__(256) void page_scores_kernel(SelectArgs a) {
             b[s][w] = (int)pos;
             b[s + D / 64][w] = (int)neg;
         }
+}
 
-    float* out = a.scores + ((size_t)row * n_kv + c) * a.max_blocks;
-    for (int p0 = (blockIdx.y * 4 + wave) * 16; p0 < n; p0 += gridDim.y * 64) {
-        const int page = min(p0 + col, n - 1);  // A operand: row = lane % 16
-        int block = btrow[page];
-        const bool bad = block < 0 || block >= a.pool.num_blocks;
-        block = bad ? 0 : block;
-        const int8_t* rec = index_codes(a.index, a.layer, block, c) + g * 16;
+// The scores of the 64 pages from p0 on, by one wave: the page that lane l's result belongs to is p0 + score_page(l).  All records
+// (16 KiB at d = 128) are on their way before the first product.  block: lane l's is the pool's page of p0 + l, or of the last one.
+__device__ __forceinline__ int score_page(int lane) { return (lane & 15) / 4 * 16 + (lane >> 4) * 4 + (lane & 3); }
+template <int D>
+__device__ __forceinline__ float score_64(const SelectArgs& a, int c, int block, const intx4 (&b)[D / 32]) {
+    constexpr int KS = D / 32;  // steps of 64 codes: the first half meets the bounds from above, the second those from below
+    const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+    const bool bad = block < 0 || block >= a.pool.num_blocks;
+    block = bad ? 0 : block;
+    intx4 rec[4][KS];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const int8_t* p = index_codes(a.index, a.layer, __shfl(block, 16 * t + col), c) + g * 16;  // A operand: row = lane % 16
+#pragma unroll
+        for (int s = 0; s < KS; ++s) rec[t][s] = *reinterpret_cast<const intx4*>(p + s * 64);
+    }
+    const int e = bad ? -1000 : *index_exp(a.index, a.layer, block, c);
+    int mine = 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
         intx4 acc = {0, 0, 0, 0};
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
-            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const intx4*>(rec + s * 64), b[s], acc, 0, 0, 0);
-        const int e = bad ? -1000 : *index_exp(a.index, a.layer, block, c);
-        // accumulator: column = lane % 16, page 4g + r in register r; the maximum over the columns, then lane r of the group stores
-        float v = 0.f;
+        for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(rec[t][s], b[s], acc, 0, 0, 0);
+        // accumulator: column = lane % 16, page 16t + 4g + r in register r; the maximum over the columns, in all 16 lanes
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             int m = acc[r];
@@ -91,101 +94,224 @@ __global__ __launch_bounds__(256) void page_scores_kernel(SelectArgs a) {
             m = max(m, row_move<kRor4>(m));
             m = max(m, row_move<kRor2>(m));
             m = max(m, row_move<kRor1>(m));
-            const int er = __shfl(e, 4 * g + r);
-            const float f = er == -1000 ? -3.4028234663852886e38f : finite_or((float)m * two_to(er), 3.4028234663852886e38f);
-            v = col == r ? f : v;
+            mine = col == 4 * t + r ? m : mine;
         }
-        if (col < 4 && p0 + 4 * g + col < n) out[p0 + 4 * g + col] = v;
     }
+    const int em = __shfl(e, score_page(lane));
+    return em == -1000 ? -kTop : finite_or((float)mine * two_to(em), kTop);
+}
+
+// Workgroup b works for list list_at(b): the lists of one row, one behind the other, run on one XCD (workgroups go to the eight in
+// turn), whose L2 then serves the row's exponents, eight heads to a line, and page ids to all of them.
+__device__ __forceinline__ int list_at(int b, int lists) {
+    const int xcd = b & 7, each = lists >> 3, more = lists & 7;
+    return xcd * each + min(xcd, more) + (b >> 3);
+}
+// what both forms of the selection begin with
+struct ListOf {
+    int n, c;
+    const int32_t* btrow;
+    const float* q;
+};
+template <int D, int G>
+__device__ __forceinline__ ListOf list_of(const SelectArgs& a, int list) {
+    ListOf l;
+    const int row = list / a.pool.n_kv, ctx = a.ctx_lens[row], seq = a.row_seq ? a.row_seq[row] : row;
+    l.c = list - row * a.pool.n_kv;
+    l.n = ctx <= 0 ? 0 : (int)min(((int64_t)ctx + kBlockSize - 1) / kBlockSize, (int64_t)a.max_blocks);
+    l.btrow = a.bt + (size_t)seq * a.max_blocks;
+    l.q = a.q + (size_t)list * (G * D);
+    return l;
 }
 
 // ---- the `top` best pages of a list, ascending -------------------------------------------------------------------
-// A workgroup per (row, KV head).  Scores become order-preserving 32-bit keys (forced pages the highest); the key of the top-th is
-// found 8 bits at a time from histograms in LDS; then every wave counts and writes what its run of pages holds.
+// By a workgroup.  Scores are order-preserving 32-bit keys.  Of the pages that are not forced, the key of the last one taken is found
+// 8 bits at a time, from the first bit in which the list's keys differ on, with histograms in LDS; it ends early where a bin is taken
+// whole.  Then every wave counts and writes what its run of pages holds.
 __device__ __forceinline__ uint32_t score_key(float f) {
     const uint32_t u = __float_as_uint(f);
     return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
-
-constexpr int kSelectThreads = 512;
-__global__ __launch_bounds__(kSelectThreads) void select_pages_kernel(SelectArgs a) {
-    constexpr int WAVES = kSelectThreads / 64;
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t s_prefix, s_left;
-    __shared__ int s_gt[WAVES], s_eq[WAVES];
+constexpr int kSelectThreads = 512, kSelectWaves = kSelectThreads / 64;
+struct SelectShared {
+    uint32_t hist[256];
+    uint32_t lo[kSelectWaves], hi[kSelectWaves];
+    uint32_t bin, before, inside;
+    int gt[kSelectWaves], eq[kSelectWaves];
+};
+template <typename Key>
+__device__ __forceinline__ void select_top(const SelectArgs& a, int n, const Key& key_of, SelectShared& sh, int32_t* out) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int n_kv = a.pool.n_kv, row = blockIdx.x / n_kv, c = blockIdx.x % n_kv;
-    const int ctx = a.ctx_lens[row];
-    const int n = ctx <= 0 ? 0 : min((int)(((int64_t)ctx + kBlockSize - 1) / kBlockSize), a.max_blocks);
-    const int count = min(n, a.top);
-    int32_t* out = a.pages + (size_t)blockIdx.x * a.top;
-    if (a.counts && c == 0 && threadIdx.x == 0) a.counts[row] = count;
-    if (n <= a.top) {
-        for (int i = threadIdx.x; i < a.top; i += kSelectThreads) out[i] = i < n ? i : -1;
-        return;
-    }
-    const float* scores = a.scores + (size_t)blockIdx.x * a.max_blocks;
-    auto key_of = [&](int p) { return p < a.n_first || p >= n - a.n_last ? 0xffffffffu : score_key(scores[p]); };
-    uint32_t prefix = 0, left = a.top;  // the keys that begin with `prefix` hold the left-th highest
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = threadIdx.x; i < 256; i += kSelectThreads) hist[i] = 0;
-        __syncthreads();
-        for (int p = threadIdx.x; p < n; p += kSelectThreads) {
+    const int f0 = a.n_first, f1 = n - a.n_last;  // the pages f0 .. f1-1 compete
+    uint32_t left = a.top - a.n_first - a.n_last;
+    uint32_t from = 0xffffffffu, equal = 0xffffffffu;  // taken: keys >= from, and the first `left` at `equal` (no score has that key)
+    if (left > 0) {
+        uint32_t lo = 0xffffffffu, hi = 0;
+        for (int p = f0 + threadIdx.x; p < f1; p += kSelectThreads) {
             const uint32_t k = key_of(p);
-            if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1u);
+            lo = min(lo, k);
+            hi = max(hi, k);
         }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
+            hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
+        }
+        if (lane == 0) {
+            sh.lo[wave] = lo;
+            sh.hi[wave] = hi;
+        }
+        if (threadIdx.x < 256) sh.hist[threadIdx.x] = 0;
         __syncthreads();
-        if (wave == 0) {
-            // lane l holds the bins 255-4l .. 252-4l, from the top; the bin in which the running count reaches `left`
-            uint32_t h[4], sum = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                h[i] = hist[255 - 4 * lane - i];
-                sum += h[i];
+        for (int w = 0; w < kSelectWaves; ++w) {
+            lo = min(lo, sh.lo[w]);
+            hi = max(hi, sh.hi[w]);
+        }
+        int bits = lo == hi ? 0 : 32 - __clz(lo ^ hi);  // the keys agree above them
+        uint32_t prefix = hi;
+        if (bits == 0) equal = hi, from = hi + 1;
+        while (bits > 0) {
+            const int shift = max(0, bits - 8);
+            const uint32_t mask = (1u << (bits - shift)) - 1;
+            for (int p = f0 + threadIdx.x; p < f1; p += kSelectThreads) {
+                const uint32_t k = key_of(p);
+                if (bits == 32 || k >> bits == prefix >> bits) atomicAdd(&sh.hist[k >> shift & mask], 1u);
             }
-            uint32_t before = (uint32_t)wave_scan((int)sum) - sum;
+            __syncthreads();
+            if (wave == 0) {
+                // lane l holds the bins 255-4l .. 252-4l, from the top; the bin in which the running count reaches `left`
+                uint32_t h[4], sum = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (before < left && before + h[i] >= left) {
-                    s_prefix = prefix | (uint32_t)(255 - 4 * lane - i) << shift;
-                    s_left = left - before;
+                for (int i = 0; i < 4; ++i) {
+                    h[i] = sh.hist[255 - 4 * lane - i];
+                    sum += h[i];
                 }
-                before += h[i];
+                uint32_t before = (uint32_t)wave_scan((int)sum) - sum;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (before < left && before + h[i] >= left) {
+                        sh.bin = 255 - 4 * lane - i;
+                        sh.before = before;
+                        sh.inside = h[i];
+                    }
+                    before += h[i];
+                }
             }
+            __syncthreads();
+            const uint32_t inside = sh.inside;
+            prefix = (bits == 32 ? 0 : prefix >> bits << bits) | sh.bin << shift;
+            left -= sh.before;
+            if (inside == left) {
+                from = prefix;
+                left = 0;
+                break;
+            }
+            bits = shift;
+            if (bits == 0) {
+                equal = prefix;
+                from = prefix + 1;
+                break;
+            }
+            if (threadIdx.x < 256) sh.hist[threadIdx.x] = 0;
+            __syncthreads();
         }
-        __syncthreads();
-        prefix = s_prefix;
-        left = s_left;
-        __syncthreads();
     }
-    // pages above the key all go, of those at it the first `left`; wave w has the pages [w0, w1)
-    const int run = (n + WAVES * 64 - 1) / (WAVES * 64) * 64, w0 = min(n, wave * run), w1 = min(n, w0 + run);
-    int gt = 0, eq = 0;
+    // wave w has the pages [w0, w1)
+    auto test = [&](int p, int w1, bool& gt, bool& eq) {
+        const bool forced = p < f0 || p >= f1;
+        const uint32_t k = p < w1 && !forced ? key_of(p) : 0;
+        gt = p < w1 && (forced || k >= from);
+        eq = p < w1 && !forced && k == equal;
+    };
+    const int run = (n + kSelectThreads - 1) / kSelectThreads * 64, w0 = min(n, wave * run), w1 = min(n, w0 + run);
+    int n_gt = 0, n_eq = 0;
     for (int p = w0 + lane; p - lane < w1; p += 64) {
-        const uint32_t k = p < w1 ? key_of(p) : 0;
-        gt += __popcll(__ballot(p < w1 && k > prefix));
-        eq += __popcll(__ballot(p < w1 && k == prefix));
+        bool gt, eq;
+        test(p, w1, gt, eq);
+        n_gt += __popcll(__ballot(gt));
+        n_eq += __popcll(__ballot(eq));
     }
     if (lane == 0) {
-        s_gt[wave] = gt;
-        s_eq[wave] = eq;
+        sh.gt[wave] = n_gt;
+        sh.eq[wave] = n_eq;
     }
     __syncthreads();
     int gt0 = 0, eq0 = 0;
     for (int w = 0; w < wave; ++w) {
-        gt0 += s_gt[w];
-        eq0 += s_eq[w];
+        gt0 += sh.gt[w];
+        eq0 += sh.eq[w];
     }
     const uint64_t below = ((uint64_t)1 << lane) - 1;
     for (int p = w0 + lane; p - lane < w1; p += 64) {
-        const uint32_t k = p < w1 ? key_of(p) : 0;
-        const bool is_gt = p < w1 && k > prefix, is_eq = p < w1 && k == prefix;
-        const uint64_t bg = __ballot(is_gt), be = __ballot(is_eq);
-        const int eqs = eq0 + __popcll(be & below);  // pages at the key before this one
-        if (is_gt || (is_eq && eqs < (int)left)) out[gt0 + __popcll(bg & below) + min(eqs, (int)left)] = p;
+        bool gt, eq;
+        test(p, w1, gt, eq);
+        const uint64_t bg = __ballot(gt), be = __ballot(eq);
+        const int eqs = eq0 + __popcll(be & below);  // pages at `equal` before this one
+        if (gt || (eq && eqs < (int)left)) out[gt0 + __popcll(bg & below) + min(eqs, (int)left)] = p;
         gt0 += __popcll(bg);
         eq0 += __popcll(be);
     }
+}
+// lists that take every page, and the counts
+__device__ __forceinline__ bool select_all(const SelectArgs& a, int list, int n, int32_t* out) {
+    if (a.counts && list % a.pool.n_kv == 0 && threadIdx.x == 0) a.counts[list / a.pool.n_kv] = min(n, a.top);
+    if (n > a.top) return false;
+    for (int i = threadIdx.x; i < a.top; i += kSelectThreads) out[i] = i < n ? i : -1;
+    return true;
+}
+
+// One launch, a workgroup per (row, KV head) that scores its pages into LDS and selects: as long as one CU can take in a list's records
+// in about the time of the second launch, or there are lists for half the CUs.
+constexpr int kSelectPages = 15360;  // keys that fit 64 KiB of LDS beside the rest
+template <int D, int G>
+__global__ __launch_bounds__(kSelectThreads, 2) void select_pages_kernel(SelectArgs a) {
+    __shared__ SelectShared sh;
+    extern __shared__ uint32_t s_keys[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, list = list_at(blockIdx.x, gridDim.x);
+    const ListOf l = list_of<D, G>(a, list);
+    int32_t* out = a.pages + (size_t)list * a.top;
+    if (select_all(a, list, l.n, out)) return;
+    intx4 b[D / 32];
+    int block = l.btrow[min(wave * 64 + lane, l.n - 1)];  // one step ahead
+    load_q8<D, G>(l.q, b);
+    for (int p0 = wave * 64; p0 < l.n; p0 += kSelectThreads) {
+        const int next = l.btrow[min(p0 + kSelectThreads + lane, l.n - 1)];
+        const float f = score_64<D>(a, l.c, block, b);
+        block = next;
+        s_keys[p0 + score_page(lane)] = score_key(f);  // (the places up to the next multiple of 64 are there)
+    }
+    __syncthreads();
+    select_top(a, l.n, [&](int p) { return s_keys[p]; }, sh, out);
+}
+
+// Two launches: few and long lists are scored by many workgroups, through memory
+template <int D, int G>
+__global__ __launch_bounds__(256) void page_scores_kernel(SelectArgs a) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, list = list_at(blockIdx.x, gridDim.x);
+    const ListOf l = list_of<D, G>(a, list);
+    if (l.n <= a.top) return;  // every page is taken: nobody reads the scores
+    intx4 b[D / 32];
+    const int first = (blockIdx.y * 4 + wave) * 64, step = gridDim.y * 256;
+    int block = l.btrow[min(first + lane, l.n - 1)];  // one step ahead
+    load_q8<D, G>(l.q, b);
+    float* out = a.scores + (size_t)list * a.max_blocks;
+    for (int p0 = first; p0 < l.n; p0 += step) {
+        const int next = l.btrow[min(p0 + step + lane, l.n - 1)];
+        const float f = score_64<D>(a, l.c, block, b);
+        block = next;
+        const int p = p0 + score_page(lane);
+        if (p < l.n) out[p] = f;
+    }
+}
+__global__ __launch_bounds__(kSelectThreads) void select_scored_kernel(SelectArgs a) {
+    __shared__ SelectShared sh;
+    const int list = blockIdx.x, ctx = a.ctx_lens[list / a.pool.n_kv];
+    const int n = ctx <= 0 ? 0 : (int)min(((int64_t)ctx + kBlockSize - 1) / kBlockSize, (int64_t)a.max_blocks);
+    int32_t* out = a.pages + (size_t)list * a.top;
+    if (select_all(a, list, n, out)) return;
+    const float* scores = a.scores + (size_t)list * a.max_blocks;
+    select_top(a, n, [&](int p) { return score_key(scores[p]); }, sh, out);
 }
 
 // ---- attention over listed pages -----------------------------------------------------------------------------------
@@ -471,23 +597,34 @@ int32_t chiron_op_select_pages(chiron_model* m, const chiron_kvpool* p, const ch
     if ((uintptr_t)q & 15) return fail(CHIRON_ERR_INVALID_ARG, "select: q must be 16-byte aligned");
     const int n_kv = p->d.n_kv, G = m->cfg.n_q_heads / n_kv, mb = m->cfg.max_blocks_per_seq;
     const int64_t lists = (int64_t)rows * n_kv;
-    // the scores lie in the attention workspace
-    if (lists * mb > (int64_t)m->aws.cap_items * m->cfg.n_q_heads * p->d.d)
-        return fail(CHIRON_ERR_BATCH_TOO_LARGE, "select: scores of %d rows x %d heads x %d pages exceed the model's workspace", rows, n_kv, mb);
     if (lists > 0x7fffffff) return fail(CHIRON_ERR_BATCH_TOO_LARGE, "select: %lld lists are too many", (long long)lists);
     SelectArgs a;
     a.pool = p->d; a.index = x->d; a.q = q; a.bt = block_table; a.row_seq = row_seq; a.ctx_lens = ctx_lens; a.scores = m->aws.part_o;
     a.pages = pages; a.counts = counts; a.layer = layer; a.max_blocks = mb; a.rows = rows; a.top = top; a.n_first = n_first; a.n_last = n_last;
     hipStream_t st = (hipStream_t)stream;
-    if (mb > top) {
-        const int chunks = (int)std::min<int64_t>((mb + 63) / 64, std::max<int64_t>(1, 8 * kNumCU / lists));
+    const int d = p->d.d;
+    // us of a CU for a whole list's records at 45 B/ns, against some 5 us for the second launch
+    const bool one = mb <= kSelectPages && (lists * 2 >= kNumCU || (double)mb * 2 * d / 45e3 <= 5.0);
+    if (one) {
+        const size_t lds = ((size_t)mb + 63) / 64 * 64 * 4;
+#define CHIRON_SELECT(D_, G_) launch_lds(select_pages_kernel<D_, G_>, dim3((unsigned)lists), dim3(kSelectThreads), lds, st, a)
+        if (d == 128) CHIRON_BY_HEADS(CHIRON_SELECT, 128)
+        else CHIRON_BY_HEADS(CHIRON_SELECT, 64)
+#undef CHIRON_SELECT
+    } else {
+        // the scores lie in the attention workspace
+        if (lists * mb > (int64_t)m->aws.cap_items * m->cfg.n_q_heads * d)
+            return fail(CHIRON_ERR_BATCH_TOO_LARGE, "select: scores of %d rows x %d heads x %d pages exceed the model's workspace", rows, n_kv, mb);
+        const int chunks = (int)std::min<int64_t>((mb + 255) / 256, std::max<int64_t>(1, 4 * kNumCU / lists));
         const dim3 grid((unsigned)lists, chunks);
+        if (mb > top) {
 #define CHIRON_SCORES(D_, G_) launch(page_scores_kernel<D_, G_>, grid, dim3(256), st, a)
-        if (p->d.d == 128) CHIRON_BY_HEADS(CHIRON_SCORES, 128)
-        else CHIRON_BY_HEADS(CHIRON_SCORES, 64)
+            if (d == 128) CHIRON_BY_HEADS(CHIRON_SCORES, 128)
+            else CHIRON_BY_HEADS(CHIRON_SCORES, 64)
 #undef CHIRON_SCORES
+        }
+        launch(select_scored_kernel, dim3((unsigned)lists), dim3(kSelectThreads), st, a);
     }
-    launch(select_pages_kernel, dim3((unsigned)lists), dim3(kSelectThreads), st, a);
     CHIRON_HIP(hipGetLastError());
     return CHIRON_OK;
 }
