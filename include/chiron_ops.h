@@ -141,15 +141,16 @@ int32_t chiron_op_verify_drafts(const chiron_draft_batch *in /* host */, int32_t
  * W[n][k] = (w4[n][k] - z[n][k/group]) * scale[n][k/group], w4 in 0 .. 15, z in 0 .. 15 (null: 8 everywhere).
  *   w4      dev uint8 [N, K/2]: k even in the low four bits, k odd in the high four
  *   scales  dev bf16 [N, K/group];  zeros dev uint8 [N, K/group] or null
- * group 32, 64 or 128, K a multiple of group, any N >= 1.  The library keeps its own repacked copy. */
+ * group 32, 64 or 128, K a multiple of group below 2^23, any N >= 1.  The library keeps its own repacked copy. */
 typedef struct chiron_linear4 chiron_linear4;
 int32_t chiron_linear4_create(const void *w4, const void *scales, const void *zeros, int32_t N, int32_t K, int32_t group,
                               void *stream, chiron_linear4 **out);
 int32_t chiron_linear4_destroy(chiron_linear4 *l);
 
 /* y[M,N] = x[M,K] * W^T, or y += (accumulate != 0).  x, y dev fp32 row-major, not overlapping.  Per row and 128 inputs, x
- * enters as whole multiples of a power of two, at most 2^22 of them (an error of at most 2^-23 of the largest value, or
- * 2^-128), in three 8-bit digits whose products are exact; groups are added in fp32.  A NaN or an infinity in a row of x makes that row of y NaN. */
+ * enters with an error of at most 2^-23 of its largest value, or 2^-128: up to 16 rows as whole multiples of a power
+ * of two in three 8-bit digits, more rows as two fp16 terms.  Sums over the groups are fp32.  A NaN or an infinity in a
+ * row of x makes that row of y NaN.  M <= 65535. */
 int32_t chiron_op_linear4(const chiron_linear4 *l, const float *x, int32_t M, float *y, int32_t accumulate, void *workspace,
                           void *stream);
 /* workspace: dev, that many bytes, 16-byte aligned, caller-owned, in use until the stream has passed; 0 (null

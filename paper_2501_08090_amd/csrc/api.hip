@@ -72,58 +72,6 @@ int32_t dev_alloc(void** p, size_t bytes) {
     return CHIRON_OK;
 }
 
-// the device whose pool a new chiron_linear keeps, or -1 if there is none (its calls then use the default pool)
-int scratch_pool_enter() {
-    int dev = -1;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kScratchDevices) return -1;
-    std::lock_guard<std::mutex> lock(g_scratch_pool_mutex);
-    auto& g = g_scratch_pool[dev];
-    if (!g.pool) {
-        hipMemPoolProps props = {};
-        props.allocType = hipMemAllocationTypePinned;
-        props.location.type = hipMemLocationTypeDevice;
-        props.location.id = dev;
-        hipMemPool_t pool = nullptr;
-        uint64_t keep = kScratchKeep;
-        if (hipMemPoolCreate(&pool, &props) != hipSuccess || hipMemPoolSetAttribute(pool, hipMemPoolAttrReleaseThreshold, &keep) != hipSuccess) {
-            (void)hipGetLastError();
-            if (pool) (void)hipMemPoolDestroy(pool);
-            return -1;
-        }
-        g.pool = pool;
-    }
-    ++g.users;
-    return dev;
-}
-
-void scratch_pool_leave(int dev) {
-    if (dev < 0) return;
-    std::lock_guard<std::mutex> lock(g_scratch_pool_mutex);
-    auto& g = g_scratch_pool[dev];
-    if (--g.users == 0) (void)hipMemPoolTrimTo(g.pool, 0);
-}
-
-int32_t scratch_alloc(int dev, void** out, size_t bytes, hipStream_t st) {
-    *out = nullptr;
-    if (bytes == 0) return CHIRON_OK;
-    // (a stream that is being captured, or one of another device, takes the default pool as any allocation does)
-    if (dev >= 0) {
-        hipStreamCaptureStatus cap = hipStreamCaptureStatusActive;
-        int of_stream = -1;
-        hipError_t e = hipStreamIsCapturing(st, &cap);
-        if (e == hipSuccess && cap == hipStreamCaptureStatusNone) e = st ? hipStreamGetDevice(st, &of_stream) : hipGetDevice(&of_stream);
-        if (e == hipSuccess && of_stream == dev) {
-            e = hipMallocFromPoolAsync(out, bytes, g_scratch_pool[dev].pool, st);
-            if (e == hipSuccess) return CHIRON_OK;
-            (void)scratch_pool_trim(dev);  // the default pool may then find the memory
-            *out = nullptr;
-        }
-        if (e != hipSuccess) (void)hipGetLastError();
-    }
-    CHIRON_HIP(hipMallocAsync(out, bytes, st));
-    return CHIRON_OK;
-}
-
 static int32_t linear_alloc(Linear& L, int N, int K) {
     L.N = N;
     L.K = K;
@@ -652,6 +600,58 @@ int32_t chiron_op_rmsnorm(const float* h, const void* gain, int32_t rows, int32_
     if (rows == 0) return CHIRON_OK;
     if (!h || !gain || !out) return fail(CHIRON_ERR_INVALID_ARG, "rmsnorm: a pointer is null");
     return launch_rmsnorm(const_cast<float*>(h), nullptr, 0, (const uint16_t*)gain, rows, n, eps, out, (hipStream_t)stream);
+}
+
+// the device whose pool a new chiron_linear keeps, or -1 if there is none (its calls then use the default pool)
+static int scratch_pool_enter() {
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kScratchDevices) return -1;
+    std::lock_guard<std::mutex> lock(g_scratch_pool_mutex);
+    auto& g = g_scratch_pool[dev];
+    if (!g.pool) {
+        hipMemPoolProps props = {};
+        props.allocType = hipMemAllocationTypePinned;
+        props.location.type = hipMemLocationTypeDevice;
+        props.location.id = dev;
+        hipMemPool_t pool = nullptr;
+        uint64_t keep = kScratchKeep;
+        if (hipMemPoolCreate(&pool, &props) != hipSuccess || hipMemPoolSetAttribute(pool, hipMemPoolAttrReleaseThreshold, &keep) != hipSuccess) {
+            (void)hipGetLastError();
+            if (pool) (void)hipMemPoolDestroy(pool);
+            return -1;
+        }
+        g.pool = pool;
+    }
+    ++g.users;
+    return dev;
+}
+
+static void scratch_pool_leave(int dev) {
+    if (dev < 0) return;
+    std::lock_guard<std::mutex> lock(g_scratch_pool_mutex);
+    auto& g = g_scratch_pool[dev];
+    if (--g.users == 0) (void)hipMemPoolTrimTo(g.pool, 0);
+}
+
+static int32_t scratch_alloc(int dev, void** out, size_t bytes, hipStream_t st) {
+    *out = nullptr;
+    if (bytes == 0) return CHIRON_OK;
+    // (a stream that is being captured, or one of another device, takes the default pool as any allocation does)
+    if (dev >= 0) {
+        hipStreamCaptureStatus cap = hipStreamCaptureStatusActive;
+        int of_stream = -1;
+        hipError_t e = hipStreamIsCapturing(st, &cap);
+        if (e == hipSuccess && cap == hipStreamCaptureStatusNone) e = st ? hipStreamGetDevice(st, &of_stream) : hipGetDevice(&of_stream);
+        if (e == hipSuccess && of_stream == dev) {
+            e = hipMallocFromPoolAsync(out, bytes, g_scratch_pool[dev].pool, st);
+            if (e == hipSuccess) return CHIRON_OK;
+            (void)scratch_pool_trim(dev);  // the default pool may then find the memory
+            *out = nullptr;
+        }
+        if (e != hipSuccess) (void)hipGetLastError();
+    }
+    CHIRON_HIP(hipMallocAsync(out, bytes, st));
+    return CHIRON_OK;
 }
 
 int32_t chiron_linear_create(const void* w, int32_t N, int32_t K, void* stream, chiron_linear** out) {

@@ -1,12 +1,13 @@
 // Products of few rows with 4-bit weights: y = x W^T, W[n][k] = (w4 - z) * scale, a scale and a zero point for each row and group of
 // 32, 64 or 128 inputs.  gfx950, wave64.
 //
-// Within a group the product is whole-number arithmetic on the 8-bit matrix cores.  x enters, per row and 128 inputs, as whole
-// multiples of a power of two, |x| <= 2^22, in three signed 8-bit digits; a group's digit sums are exact, and are scaled and added
-// over the groups in fp32.  (The digits take the place of the two or three bf16 terms that the other projections split x into: whole numbers need no
-// correction for how a weight is unpacked, and the 8-bit matrix cores run at twice the rate.)  A weight without zero points enters as
-// 16 * (w4 - 8), which is its four bits, the highest inverted when the matrix is laid out, in the upper half of a byte: three
-// instructions for eight weights.  With zero points it enters as w4 - z: eight bytes, seven instructions.
+// x enters, per row and 128 inputs, with 22 bits of its largest value, on two ways:
+//  - up to 16 rows, where bringing x to the matrix cores costs most, as whole multiples of a power of two, |x| <= 2^22, in three signed
+//    8-bit digits: a group's digit sums are exact, and are scaled and added over the groups in fp32.  A weight without zero points is
+//    16 * (w4 - 8), which is its four bits, the highest inverted when the matrix is laid out, in the upper half of a byte: three
+//    instructions for eight weights.  With zero points it is w4 - z: eight bytes, seven instructions.
+//  - more rows as two fp16 terms, whose products with w4 - z, exact in fp16, meet in one fp32 sum.
+// (Scales multiply sums, not weights: w4 - z times a bf16 scale has 12 bits, one more than fp16.)
 //
 // Layout: tiles of 16 rows of W and 128 of K, 1 KiB each, a tile's blocks one behind the other: lane l holds row l % 16 and 32 values
 // of K in one 16-byte load, two dwords for each step of 64.  Within a step byte j of lane group g is k = 32 * (j / 8) + 8 g + j % 8,
@@ -201,7 +202,9 @@ __device__ __forceinline__ uint32_t block_top(const float (&v)[8]) {
 // one operand (column = 4 * digit + row), with up to 8 two operands (8 * digit + row), else three.  A slice of more than 8 NB blocks
 // goes in chunks, whose sums wait in LDS (for kFewTiles tiles at most): adding them up in y would put a load behind the weights on their
 // way, and what it waits for would be all of them.  The loops hold no branch that depends on a wave: blocks behind the slice's end
-// read the last one again and count with 0.
+// read the last one again and count with 0.  8 rows through 28672 x 4096: 17.7 us, 3.4 TB/s; one through 4096 x 4096: 5.
+// Bound by what stands before and beside the stream of weights: the launch, bringing x in (its conversion is a chain of loads, a maximum
+// over 16 lanes and LDS) and, with more rows, the scaling of the digits' sums.
 // Digits lie in LDS as the operands want them, 16 bytes a lane, column c of lane group g and step k in the place c ^ (4 g + k % 4) of its
 // 16: lanes that write consecutive runs of a row then meet in no bank.
 constexpr int kFewTiles = 12;
@@ -252,7 +255,7 @@ __global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const fl
             }
         };
         // All of the chunk's x is asked for before the first weights: loads come back in order, and x, which lies in the L2, need not
-        // wait for them (8 rows through 28672 x 4096: %s us).
+        // wait for them.
         constexpr int ROW = NB * 128, U = (ROWS * ROW + 511) / 512;  // runs of 8 in a row of the chunk, runs per thread
         float v[U][8];
 #pragma unroll
@@ -356,161 +359,333 @@ __global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const fl
 }
 
 // ---- more rows -------------------------------------------------------------------------------------------------
-// x as digits for the whole launch: digits [rows/16][Kpad/64][3][64 lanes][16 B], scales [rows/16][Kpad/128][16] fp32
-struct Digits {
+// x enters as two fp16 terms of x * 2^up, up to 2^15 of a block of 128; a group costs one multiplication and one fused multiply-add for
+// each result, where three digits cost five instructions.  64 rows through 8192 x 28672 with groups of 64 and zero points: 80 us, 70 of
+// them in the products, against 100 and 87 with digits (17 rows through 28672 x 4096: 31 and 28).  What bounds it is the matrix cores and
+// the vector units, which share issue and power: with no products 56 us are left of the 70, with no loads of weights or x 60.  Products
+// of 60 TFLOP take 24 us at the rate of the matrix cores, the weights 19.
+//
+// x for the whole launch: terms [rows/16][K/128][4 steps of 32][2][64 lanes][16 B], scales [rows/16][K/128][16] fp32.  A lane's eight
+// values of a step lie in the order in which masks take weights out of a dword: (4,6) (0,2) (5,7) (1,3).
+typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+struct Terms {
     uint8_t* d = nullptr;
     float* scale = nullptr;
 };
-// a thread per run of 8
-template <bool ZERO>
-__global__ __launch_bounds__(256) void digits_kernel(const float* __restrict__ x, int M, Linear4 l, Digits dg) {
-    const int kb = l.Kpad / 128, run = blockIdx.x * 256 + threadIdx.x;
-    const int64_t m = blockIdx.y;  // rows behind M: zeros
-    if (run >= kb * 16) return;
-    float v[8];
-    load_run(x + (m < M ? m : M - 1) * l.K, run * 8, l.K, v);
-    if (m >= M)
+__device__ __forceinline__ uint32_t pack_half(float a, float b) {
+    halfx2 h = {(_Float16)a, (_Float16)b};
+    return *reinterpret_cast<uint32_t*>(&h);
+}
+// a wave per tile of 16 rows and block: a lane holds 8 values of each of the four steps, reads them 128 bytes a row and writes them 1 KiB
+// a wave
+__global__ __launch_bounds__(256) void terms_kernel(const float* __restrict__ x, int M, Linear4 l, Terms tm) {
+    const int kb = l.Kpad / 128, b = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, row = lane & 15, g = lane >> 4;
+    const int64_t mt = blockIdx.y, m = mt * 16 + row;  // rows behind M: zeros
+    if (b >= kb) return;
+    float v[4][8];
+    uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    const uint32_t top = block_top(v);
-    const Run d = digits_of(v, top);
-    const int step = run / 8, half = run / 4 % 2, g = run % 4;
-    const int64_t mt = m / 16;
+    for (int step = 0; step < 4; ++step) load_run(x + (m < M ? m : M - 1) * l.K, b * 128 + step * 32 + g * 8, l.K, v[step]);
 #pragma unroll
-    for (int t = 0; t < 3; ++t)
-        *reinterpret_cast<uint2*>(dg.d + (((mt * kb * 2 + step) * 3 + t) * 64 + g * 16 + m % 16) * 16 + half * 8) = d.digit[t];
-    if (run % 16 == 0) dg.scale[(mt * kb + run / 16) * 16 + m % 16] = block_scale<ZERO>(top);
+    for (int step = 0; step < 4; ++step)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (m >= M) v[step][i] = 0.f;
+            top = max(top, __float_as_uint(v[step][i]) & 0x7fffffffu);
+        }
+    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+    const bool bad = top >= 0x7f800000u;  // infinity or NaN in the block: its scale is NaN
+    const int up = min(127, 15 - __builtin_amdgcn_frexp_expf(__uint_as_float(top)));
+    const float f = bad ? 0.f : ldexpf(1.f, up);
+    uint8_t* out = tm.d + (mt * kb + b) * 8192 + lane * 16;
+#pragma unroll
+    for (int step = 0; step < 4; ++step) {
+        float hi[8], lo[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float s = v[step][i] * f;
+            hi[i] = (float)(_Float16)s;
+            lo[i] = s - hi[i];
+        }
+        *reinterpret_cast<uint4*>(out + step * 2048) = make_uint4(pack_half(hi[4], hi[6]), pack_half(hi[0], hi[2]), pack_half(hi[5], hi[7]), pack_half(hi[1], hi[3]));
+        *reinterpret_cast<uint4*>(out + step * 2048 + 1024) = make_uint4(pack_half(lo[4], lo[6]), pack_half(lo[0], lo[2]), pack_half(lo[5], lo[7]), pack_half(lo[1], lo[3]));
+    }
+    if (g == 0) tm.scale[(mt * kb + b) * 16 + row] = bad ? __uint_as_float(0x7fc00000u) : ldexpf(1.f, -up);
 }
 
-// A workgroup of 8 waves owns 256 columns (two tiles a wave), MT tiles of 16 rows and a slice of K, whose digits and scales pass
-// through LDS block by block; slices go to `part` and are added by the caller's next launch.
+// Eight weights of a dword as fp16, nine instructions: a mask and the bits of 1024 make 1024 + w4 of the lower four bits of a byte and
+// 1024 + 16 w4 of the upper four; then minus 1024 + z, or over 16 and minus 64 + z, exactly.  (Without zero points the highest of the
+// four bits lies inverted.)
+struct Offsets {
+    halfx2 low, high;  // -(1024 + z), -(64 + z)
+};
+__device__ __forceinline__ halfx2 as_half(uint32_t w) { return *reinterpret_cast<halfx2*>(&w); }
+template <bool ZERO>
+__device__ __forceinline__ halfx8 unpack_half(uint32_t w, const Offsets& o, uint32_t bits) {
+    if (!ZERO) w ^= 0x88888888u;
+    const uint32_t v = w >> 8;
+    const halfx2 sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
+    const halfx2 r0 = as_half((w & 0x000f000fu) | bits) + o.low, r2 = as_half((v & 0x000f000fu) | bits) + o.low;
+    const halfx2 r1 = __builtin_elementwise_fma(as_half((w & 0x00f000f0u) | bits), sixteenth, o.high);
+    const halfx2 r3 = __builtin_elementwise_fma(as_half((v & 0x00f000f0u) | bits), sixteenth, o.high);
+    return halfx8{r0[0], r0[1], r1[0], r1[1], r2[0], r2[1], r3[0], r3[1]};
+}
+
+// A workgroup of 8 waves owns 256 columns, MT tiles of 16 rows and a slice of K; slices go to `part` and are added by the caller's next
+// launch.  Terms and scales pass through LDS block by block.  A wave owns 64 columns and one half of every block, so that all of x is
+// read from LDS four times and no weight is unpacked twice; the halves are joined at the end.
+//
+// A block goes in 2 MT phases, the products of a row tile with two of the wave's column tiles.  The waves go through a block together, so
+// what is to run beside the matrix cores has to come from the same wave: beside a phase's products run the scaling of the last phase's
+// sums, the reads of the next row tile's operands, in the first phase the unpacking of column tiles 2 and 3, and in the last, where 0 and
+// 1 have done their part, that of the next block's 0 and 1.  Weights are asked for again as soon as they are unpacked.  One barrier a
+// block: behind it the next block's x is there, and this one's is no longer read.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+// 2 GiB from p on, for loads with an offset of the lane and one of the wave; every offset stays inside what p points to
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffffff, 0x00027000);
+}
 template <int GROUP, bool ZERO, int MT>
-__global__ __launch_bounds__(512, 2) void linear4_kernel(Linear4 l, Digits dg, int mt0, int M, int slice_blocks, float* __restrict__ out, int add) {
-    constexpr int PER = 128 / GROUP, NT = 2, PIECES = MT * 384, NS = MT * 16;
-    __shared__ uint4 s_dig[2][PIECES];
+__global__ __launch_bounds__(512, 2) void linear4_kernel(Linear4 l, Terms tm, int M, int slice_blocks, float* __restrict__ out, int add) {
+    constexpr int PER = 128 / GROUP, PERW = PER == 4 ? 2 : 1, NS = MT * 16;  // groups in a block, in a wave's half of it
+    __shared__ u32x4 s_x[2][MT * 512];
     __shared__ float s_scale[2][NS];
     const int lane = threadIdx.x & 63, col = lane & 15, g4 = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = wave & 1, pair = wave >> 1;
     const int kb = l.Kpad / 128, tiles = (l.N + 15) / 16;
-    const int b0 = blockIdx.y * slice_blocks, b1 = min(kb, b0 + slice_blocks);
-    const int tile0 = (blockIdx.x * 8 + wave) * NT;
-    float acc[NT][MT][4];
+    const int b0 = blockIdx.y * slice_blocks, b1 = min(kb, b0 + slice_blocks), mt0 = blockIdx.z * MT;
+    const int tile0 = (blockIdx.x * 4 + pair) * 4;
+    floatx4 acc[4][MT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < 4; ++n)
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[n][m][r] = 0.f;
-    // block b of the MT row tiles, 6 KiB each, and their scales: three pieces of 16 bytes a thread or fewer
-    uint4 stage0, stage1 = make_uint4(0, 0, 0, 0), stage2 = make_uint4(0, 0, 0, 0);
-    float stage_s = 0.f;
-    const int tid = threadIdx.x;
-    const int j0 = min(tid, PIECES - 1), j1 = min(512 + tid, PIECES - 1), j2 = min(1024 + tid, PIECES - 1), js = min(tid, NS - 1);
-    const uint8_t* x0 = dg.d + (int64_t)(mt0 + j0 / 384) * kb * 6144 + j0 % 384 * 16;
-    const uint8_t* x1 = dg.d + (int64_t)(mt0 + j1 / 384) * kb * 6144 + j1 % 384 * 16;
-    const uint8_t* x2 = dg.d + (int64_t)(mt0 + j2 / 384) * kb * 6144 + j2 % 384 * 16;
-    const float* xs = dg.scale + (int64_t)(mt0 + js / 16) * kb * 16 + js % 16;
-    auto load_x = [&](int b) {
-        stage0 = *reinterpret_cast<const uint4*>(x0 + (int64_t)b * 6144);
-        if (PIECES > 512) stage1 = *reinterpret_cast<const uint4*>(x1 + (int64_t)b * 6144);
-        if (PIECES > 1024) stage2 = *reinterpret_cast<const uint4*>(x2 + (int64_t)b * 6144);
-        stage_s = xs[(int64_t)b * 16];
+        for (int m = 0; m < MT; ++m) acc[n][m] = floatx4{0.f, 0.f, 0.f, 0.f};
+    // what a column tile needs of a block, as it comes from memory
+    struct Raw {
+        u32x2 w;
+        uint32_t z, s[PERW == 2 ? 4 : PER == 2 ? 4 : 2];
     };
-    auto store_x = [&](int buf) {
-        s_dig[buf][tid] = stage0;
-        if (PIECES > 512 && (PIECES >= 1024 || tid < PIECES - 512)) s_dig[buf][512 + tid] = stage1;
-        if (PIECES > 1024 && (PIECES >= 1536 || tid < PIECES - 1024)) s_dig[buf][1024 + tid] = stage2;
-        if (tid < NS) s_scale[buf][tid] = stage_s;
-    };
-    static_assert(PIECES >= 512 && PIECES <= 1536, "two to four row tiles");
-    uint4 w[NT], wn[NT];
-    uint32_t z[NT], zn[NT];
-    Scales<GROUP> sc[NT], sn[NT];
-    auto load_w = [&](int b) {
+    Raw raw[4];
+    // the wave's column tiles: offsets of a lane, and of a tile (behind the last: the last)
+    int tile_at[4];
+    const int first = min(tile0, tiles - 1);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int64_t tb = (int64_t)min(tile0 + n, tiles - 1) * kb + b;
-            wn[n] = *reinterpret_cast<const uint4*>(l.w + (tb * 64 + lane) * 16);
-            sn[n].load(l.scale, tb, g4);
-            if (ZERO) zn[n] = load_zeros<GROUP>(l.zero, tb, col);
+    for (int n = 0; n < 4; ++n) tile_at[n] = (min(tile0 + n, tiles - 1) - first) * kb;
+    const auto w_rsrc = resource(l.w + (int64_t)first * kb * 1024), s_rsrc = resource(l.scale + (int64_t)first * kb * 16 * PER),
+               z_rsrc = resource(l.zero + (int64_t)first * kb * 16 * PER);
+    const int w_lane = lane * 16 + half * 8, s_lane = g4 * 8 * PER + (PER == 4 ? half * 4 : 0), z_lane = col * PER + (PER == 4 ? half * 2 : PER == 2 ? half : 0);
+    auto load_w = [&](Raw& r, int n, int b) __attribute__((always_inline)) {
+        const int t = tile_at[n] + b;
+        r.w = __builtin_amdgcn_raw_buffer_load_b64(w_rsrc, w_lane, t * 1024, 0);
+        if constexpr (PER == 4) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r.s[i] = __builtin_amdgcn_raw_buffer_load_b32(s_rsrc, s_lane, t * 128 + i * 8, 0);
+        } else if constexpr (PER == 2) {
+            const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(s_rsrc, s_lane, t * 64, 0);
+            r.s[0] = v.x; r.s[1] = v.y; r.s[2] = v.z; r.s[3] = v.w;
+        } else {
+            const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(s_rsrc, s_lane, t * 32, 0);
+            r.s[0] = v.x; r.s[1] = v.y;
+        }
+        if (ZERO) {
+            if constexpr (PER == 4) r.z = __builtin_amdgcn_raw_buffer_load_b16(z_rsrc, z_lane, t * 64, 0);
+            else r.z = __builtin_amdgcn_raw_buffer_load_b8(z_rsrc, z_lane, t * 16 * PER, 0);
         }
     };
-    load_w(b0);
+    uint32_t bits = 0x64006400u;
+    asm volatile("" : "+v"(bits));
+    halfx8 a[4][2];
+    float sc[4][PERW][4];
+    auto unpack = [&](int n) __attribute__((always_inline)) {
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+            const uint32_t z = ZERO ? (PERW == 2 ? (raw[n].z >> (8 * d)) & 255u : raw[n].z & 255u) : 120u;  // 128 minus the zero point
+            const Offsets o = {as_half(0xe480e480u - z * 0x10001u), as_half(0xdc00dc00u - z * 0x100010u)};
+            a[n][d] = unpack_half<ZERO>(d ? raw[n].w.y : raw[n].w.x, o, bits);
+            asm volatile("" : "+v"(a[n][d]));
+        }
+    };
+    auto scales = [&](int n) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if constexpr (PER == 4) {
+                sc[n][0][r] = bf16_lo(raw[n].s[r]);
+                sc[n][1][r] = bf16_hi(raw[n].s[r]);
+            } else if constexpr (PER == 2) {
+                sc[n][0][r] = __uint_as_float(__builtin_amdgcn_perm(raw[n].s[r], raw[n].s[r], half ? 0x03020c0cu : 0x01000c0cu));
+            } else {
+                sc[n][0][r] = r % 2 ? bf16_hi(raw[n].s[r / 2]) : bf16_lo(raw[n].s[r / 2]);
+            }
+            asm volatile("" : "+v"(sc[n][0][r]));
+            if constexpr (PERW == 2) asm volatile("" : "+v"(sc[n][1][r]));
+        }
+    };
+    // x: of the MT row tiles, 8 KiB each, a piece of 16 bytes a thread and tile; their scales.  (The compiler's own vectors: HIP's are
+    // copied through scratch memory on their way to LDS.)
+    const int tid = threadIdx.x, js = min(tid, NS - 1);
+    const auto x_rsrc = resource(tm.d + (int64_t)mt0 * kb * 8192), xs_rsrc = resource(tm.scale + (int64_t)mt0 * kb * 16);
+    const int x_lane = tid * 16, xs_lane = (js / 16 * kb * 16 + js % 16) * 4;
+    u32x4 x0, x1, x2, x3;
+    float xsv;
+    auto load_x = [&](int b) __attribute__((always_inline)) {
+        x0 = __builtin_amdgcn_raw_buffer_load_b128(x_rsrc, x_lane, b * 8192, 0);
+        x1 = __builtin_amdgcn_raw_buffer_load_b128(x_rsrc, x_lane, (kb + b) * 8192, 0);
+        if (MT > 2) x2 = __builtin_amdgcn_raw_buffer_load_b128(x_rsrc, x_lane, (2 * kb + b) * 8192, 0);
+        if (MT > 3) x3 = __builtin_amdgcn_raw_buffer_load_b128(x_rsrc, x_lane, (3 * kb + b) * 8192, 0);
+        xsv = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(xs_rsrc, xs_lane, b * 64, 0));
+    };
+    auto store_x = [&](int buf) __attribute__((always_inline)) {
+        s_x[buf][tid] = x0;
+        s_x[buf][512 + tid] = x1;
+        if (MT > 2) s_x[buf][1024 + tid] = x2;
+        if (MT > 3) s_x[buf][1536 + tid] = x3;
+        if (tid < NS) s_scale[buf][tid] = xsv;
+    };
+    static_assert(MT >= 2 && MT <= 4, "two to four row tiles");
+    halfx8 f[2][4];
+    float sx[2];
+    auto read = [&](int buf, int m, int to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[to][i] = *reinterpret_cast<const halfx8*>(&s_x[buf][m * 512 + half * 256 + i * 64 + lane]);
+        sx[to] = s_scale[buf][m * 16 + col];
+    };
     load_x(b0);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) load_w(raw[n], n, b0);
     store_x(0);
+    load_x(min(b0 + 1, b1 - 1));
+    unpack(0);
+    unpack(1);
+    scales(0);
+    scales(1);
+    load_w(raw[0], 0, min(b0 + 1, b1 - 1));
+    load_w(raw[1], 1, min(b0 + 1, b1 - 1));
+    lds_barrier();
+    read(0, 0, 0);
     int buf = 0;
-    for (int b = b0; b < b1; ++b) {
+    for (int b = b0; b < b1; ++b, buf ^= 1) {
+        const int b_1 = min(b + 1, b1 - 1), b_2 = min(b + 2, b1 - 1);  // (behind the slice: the last block once more, not used)
+        floatx4 p[2][2][PERW];
+        float was = 0.f;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            w[n] = wn[n];
-            if (ZERO) z[n] = zn[n];
-            sc[n] = sn[n];
-        }
-        const int next = min(b + 1, b1 - 1);  // (the last block once more, not used)
-        load_w(next);
-        load_x(next);
-        lds_barrier();
-        intx4 a[NT][2];
+        for (int ph = 0; ph <= 2 * MT; ++ph) {
+            const int m = ph / 2, n0 = ph % 2 * 2, to = ph & 1;
+            if (ph < 2 * MT) {
+                if (ph % 2 == 0 && m + 1 < MT) read(buf, m + 1, (m + 1) & 1);
+                if (ph == 2 * MT - 3) {
+                    store_x(buf ^ 1);
+                    load_x(b_2);
+                }
+                if (ph == 2 * MT - 2) lds_barrier();
+                if (ph == 2 * MT - 1) read(buf ^ 1, 0, MT & 1);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) unpack_block<GROUP, ZERO>(w[n], z[n], a[n]);
-        intx4 xf[2][3][2];  // a row tile's operands are read while the one before it is multiplied
-        float sx[2];
-        auto read_x = [&](int m, intx4 (&f)[3][2], float& sxm) {
+                for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                    for (int u = 0; u < PERW; ++u) p[to][n][u] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int t = 0; t < 3; ++t) f[t][h] = *reinterpret_cast<const intx4*>(&s_dig[buf][(m * 6 + h * 3 + t) * 64 + lane]);
-            sxm = s_scale[buf][m * 16 + col];
-        };
-        read_x(0, xf[0], sx[0]);
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            if (m + 1 < MT) read_x(m + 1, xf[(m + 1) & 1], sx[(m + 1) & 1]);
-            float sum[NT][4];
+                    for (int n = 0; n < 2; ++n)
+                        p[to][n][i / 2 * (PERW - 1)] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[n0 + n][i / 2], f[m & 1][i], p[to][n][i / 2 * (PERW - 1)], 0, 0, 0);
+            }
+            if (ph > 0) {  // the last phase's sums
+                const int q = ph - 1, pm = q / 2, pn = q % 2 * 2;
 #pragma unroll
-            for (int u = 0; u < PER; ++u)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    intx4(&f)[3][2] = xf[m & 1];
-                    const intx4 p2 = group_product<GROUP>(a[n], f[0], u), p1 = group_product<GROUP>(a[n], f[1], u), p0 = group_product<GROUP>(a[n], f[2], u);
+                for (int n = 0; n < 2; ++n) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const float v = join_digits(p2[r], p1[r], p0[r]);
-                        sum[n][r] = u == 0 ? v * sc[n].get(r, u) : fmaf(v, sc[n].get(r, u), sum[n][r]);
+                        float t = p[q & 1][n][0][r] * sc[pn + n][0][r];
+                        if constexpr (PERW == 2) t = fmaf(p[q & 1][n][1][r], sc[pn + n][1][r], t);
+                        acc[pn + n][pm][r] = fmaf(t, q % 2 ? was : sx[pm & 1], acc[pn + n][pm][r]);
                     }
+                    asm volatile("" : "+v"(acc[pn + n][pm]));
                 }
+            }
+            if (ph % 2 == 0 && m < MT) was = sx[m & 1];
+            if (ph == 0) {
+                unpack(2);
+                unpack(3);
+                scales(2);
+                scales(3);
+            }
+            if (ph == 2 * MT - 1) {
+                unpack(0);
+                unpack(1);
+            }
+            if (ph < 2 * MT) {
+                // a product, then a few of the vector instructions, and so on
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) acc[n][m][r] = fmaf(sum[n][r], sx[m & 1], acc[n][m][r]);
-                // one row tile at a time: left to itself the compiler keeps every tile's products for the end, and they do not fit the registers
-                asm volatile("" : "+v"(acc[n][m][0]), "+v"(acc[n][m][1]), "+v"(acc[n][m][2]), "+v"(acc[n][m][3]));
+                for (int i = 0; i < 8; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    if (ph == 0 || ph == 2 * MT - 1) __builtin_amdgcn_sched_group_barrier(0x002, 9, 0);
+                    else __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (ph == 0) {
+                load_w(raw[2], 2, b_1);
+                load_w(raw[3], 3, b_1);
             }
         }
-        buf ^= 1;
-        store_x(buf);  // read again only behind the next barrier; last read before this one
+        scales(0);
+        scales(1);
+        __builtin_amdgcn_sched_barrier(0);
+        load_w(raw[0], 0, b_2);
+        load_w(raw[1], 1, b_2);
+        if (MT & 1) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[0][i] = f[1][i];
+            sx[0] = sx[1];
+        }
     }
+    // The halves are joined, and rows written 1 KiB at a time, through LDS: [row][64 pieces of 4 columns], piece c in the place c ^ row % 16
+    // (lanes that hold 16 rows of a piece then meet in no bank).
+    lds_barrier();
+    floatx4* sum = reinterpret_cast<floatx4*>(&s_x[0][0]);
+    auto place = [&](int n, int m) { return (m * 16 + col) * 64 + ((pair * 16 + n * 4 + g4) ^ col); };
+    if (half)
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) sum[place(n, m)] = acc[n][m];
+    lds_barrier();
+    if (!half)
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) sum[place(n, m)] += acc[n][m];
+    lds_barrier();
     float* dst = out + (int64_t)blockIdx.y * M * l.N;
+    const int64_t c = (int64_t)blockIdx.x * 256 + lane * 4;
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int i = 0; i < 2 * MT; ++i) {
+        const int r = i * 8 + wave;
+        const int64_t row = (int64_t)mt0 * 16 + r;
+        if (row >= M || c >= l.N) continue;
+        floatx4 v = sum[r * 64 + (lane ^ (r & 15))];
+        float* q = dst + row * l.N + c;
+        if (c + 4 <= l.N) {
+            if (add) v += *reinterpret_cast<const floatx4_any*>(q);
+            *reinterpret_cast<floatx4_any*>(q) = v;
+        } else {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const int64_t row = (int64_t)(mt0 + m) * 16 + col;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int64_t c = (int64_t)(tile0 + n) * 16 + 4 * g4 + r;
-                if (row < M && c < l.N) dst[row * l.N + c] = add ? dst[row * l.N + c] + acc[n][m][r] : acc[n][m][r];
-            }
+            for (int j = 0; j < 3; ++j)
+                if (c + j < l.N) q[j] = add ? q[j] + v[j] : v[j];
         }
+    }
 }
 
-// How a call of M rows runs: up to 16 by the few-row kernel; more by tiles of up to 64 rows, K sliced until the chip has a workgroup
-// of 256 columns for every CU, each slice at least 4 blocks of 128.
+// How a call of M rows runs: up to 16 by the few-row kernel; more by passes of nearly the same height of up to 64 rows, side by side in
+// one launch (100 rows through 4096 x 4096: 25.5 us, one behind the other 35.6), K sliced until the chip has a workgroup of 256 columns
+// for every CU, each slice at least 4 blocks of 128.
 struct Plan4 {
     int sets = 0, nb = 0, wgs = 0;  // few rows: operands, blocks per wave and chunk, workgroups per slice
-    int row_tiles = 0, slices = 1, slice_blocks = 0;
-    int64_t digit_bytes = 0, scale_bytes = 0, part_bytes = 0;
-    int64_t bytes() const { return digit_bytes + scale_bytes + part_bytes; }
+    int mt = 0, row_tiles = 0;           // more: row tiles of a workgroup, of all
+    int slices = 1, slice_blocks = 0;
+    int64_t term_bytes = 0, scale_bytes = 0, part_bytes = 0;
+    int64_t bytes() const { return term_bytes + scale_bytes + part_bytes; }
 };
 static Plan4 plan_linear4(const Linear4& l, int64_t M) {
     Plan4 p;
@@ -545,12 +720,13 @@ static Plan4 plan_linear4(const Linear4& l, int64_t M) {
         p.wgs = (int)((tiles + rounds - 1) / rounds);
     } else {
         const int64_t groups = ((int64_t)l.N + 255) / 256;
-        p.row_tiles = (int)((M + 15) / 16);
         const int64_t passes = (M + 63) / 64, want = std::max<int64_t>(1, kNumCU / (groups * passes));
+        p.mt = (int)(((M + 15) / 16 + passes - 1) / passes);
+        p.row_tiles = (int)(passes * p.mt);
         const int64_t slices = std::min<int64_t>(want, std::max<int64_t>(1, kb / 4));
         p.slice_blocks = (int)((kb + slices - 1) / slices);
         p.slices = (int)((kb + p.slice_blocks - 1) / p.slice_blocks);
-        p.digit_bytes = p.row_tiles * kb * 6144;
+        p.term_bytes = p.row_tiles * kb * 8192;
         p.scale_bytes = p.row_tiles * kb * 64;
     }
     if (p.slices > 1) p.part_bytes = p.slices * M * l.N * 4;
@@ -559,7 +735,7 @@ static Plan4 plan_linear4(const Linear4& l, int64_t M) {
 
 template <int GROUP, bool ZERO>
 static void launch_linear4(const Linear4& l, const float* x, int M, float* y, int accumulate, const Plan4& p, void* work, hipStream_t st) {
-    float* part = (float*)((char*)work + p.digit_bytes + p.scale_bytes);
+    float* part = (float*)((char*)work + p.term_bytes + p.scale_bytes);
     float* out = p.slices > 1 ? part : y;
     const int add = p.slices > 1 ? 0 : accumulate;
     if (M <= 16) {
@@ -586,18 +762,14 @@ static void launch_linear4(const Linear4& l, const float* x, int M, float* y, in
 #undef CHIRON_FEW
         return;
     }
-    Digits dg;
-    dg.d = (uint8_t*)work;
-    dg.scale = (float*)(dg.d + p.digit_bytes);
-    launch(digits_kernel<ZERO>, dim3((l.Kpad / 8 + 255) / 256, p.row_tiles * 16), dim3(256), st, x, M, l, dg);
-    const dim3 grid((l.N + 255) / 256, p.slices);
-    for (int mt = 0; mt < p.row_tiles;) {  // passes of nearly the same height, two tiles at least
-        const int left = p.row_tiles - mt, passes = (left + 3) / 4, take = (left + passes - 1) / passes;
-        if (take == 4) launch(linear4_kernel<GROUP, ZERO, 4>, grid, dim3(512), st, l, dg, mt, M, p.slice_blocks, out, add);
-        else if (take == 3) launch(linear4_kernel<GROUP, ZERO, 3>, grid, dim3(512), st, l, dg, mt, M, p.slice_blocks, out, add);
-        else launch(linear4_kernel<GROUP, ZERO, 2>, grid, dim3(512), st, l, dg, mt, M, p.slice_blocks, out, add);
-        mt += take;
-    }
+    Terms tm;
+    tm.d = (uint8_t*)work;
+    tm.scale = (float*)(tm.d + p.term_bytes);
+    launch(terms_kernel, dim3((l.Kpad / 128 + 3) / 4, p.row_tiles), dim3(256), st, x, M, l, tm);
+    const dim3 grid((l.N + 255) / 256, p.slices, p.row_tiles / p.mt);
+    if (p.mt == 4) launch(linear4_kernel<GROUP, ZERO, 4>, grid, dim3(512), st, l, tm, M, p.slice_blocks, out, add);
+    else if (p.mt == 3) launch(linear4_kernel<GROUP, ZERO, 3>, grid, dim3(512), st, l, tm, M, p.slice_blocks, out, add);
+    else launch(linear4_kernel<GROUP, ZERO, 2>, grid, dim3(512), st, l, tm, M, p.slice_blocks, out, add);
 }
 
 }  // namespace chiron
@@ -628,7 +800,7 @@ int32_t chiron_linear4_create(const void* w4, const void* scales, const void* ze
     if (K % group != 0) return fail(CHIRON_ERR_SHAPE, "linear4: K=%d must be a multiple of the group %d", K, group);
     if ((uintptr_t)scales & 1) return fail(CHIRON_ERR_INVALID_ARG, "linear4: scales must be 2-byte aligned");
     const int64_t tiles = ((int64_t)N + 15) / 16, kb = ((int64_t)K + 127) / 128;
-    if (tiles * kb * 64 / 256 >= 0x7fffffff || kb * 128 > 0x7fffffff) return fail(CHIRON_ERR_SHAPE, "linear4: %d x %d is too large", N, K);
+    if (tiles * kb * 64 / 256 >= 0x7fffffff || kb >= 65536) return fail(CHIRON_ERR_SHAPE, "linear4: %d x %d is too large", N, K);
     chiron_linear4* l = new (std::nothrow) chiron_linear4();
     if (!l) return fail(CHIRON_ERR_OOM, "host allocation failed");
     Linear4& L = l->L;
@@ -679,7 +851,7 @@ int32_t chiron_op_linear4(const chiron_linear4* l, const float* x, int32_t M, fl
     else CHIRON_L4(32);
 #undef CHIRON_L4
     CHIRON_HIP(hipGetLastError());
-    if (p.slices > 1) return launch_reduce_partials((const float*)((char*)workspace + p.digit_bytes + p.scale_bytes), p.slices, (int64_t)M * L.N, y, accumulate, st);
+    if (p.slices > 1) return launch_reduce_partials((const float*)((char*)workspace + p.term_bytes + p.scale_bytes), p.slices, (int64_t)M * L.N, y, accumulate, st);
     return CHIRON_OK;
 }
 
