@@ -609,6 +609,9 @@ def _logit_rows(t, batch, rows, vocab):
     return t.data_ptr() or None, stride
 
 
+_verify_work = {}  # (requests, drafts, vocabulary) -> 4-byte words of workspace
+
+
 def verify_drafts(logits, tokens, uniforms, noise, draft_logits=None, draft_lens=None, temperature=None):
     """Accept or replace drafted tokens.  logits fp32 [batch, drafts+1, vocab] of the target, tokens int32 [batch, drafts], uniforms fp32
     [batch, drafts] in [0, 1), noise fp32 [batch, vocab] from the unit exponential distribution, draft_logits fp32 [batch, drafts,
@@ -628,13 +631,12 @@ def verify_drafts(logits, tokens, uniforms, noise, draft_logits=None, draft_lens
         b.draft_logits, b.draft_stride = _logit_rows(draft_logits, batch, drafts, vocab)
     b.tokens, b.draft_lens = _address(tokens, torch.int32), _address(draft_lens, torch.int32)
     b.uniforms, b.noise, b.temperature = _address(uniforms, torch.float32), _address(noise, torch.float32), _address(temperature, torch.float32)
-    dev = logits.device
-    work = torch.empty(load().chiron_verify_workspace_bytes(batch, drafts, vocab), dtype=torch.uint8, device=dev)
-    out = torch.empty((batch, rows), dtype=torch.int32, device=dev)
-    accepted = torch.empty(batch, dtype=torch.int32, device=dev)
-    prob = torch.empty((batch, drafts), dtype=torch.float32, device=dev)
-    _check(load().chiron_op_verify_drafts(C.addressof(b), batch, drafts, vocab, _address(out), _address(accepted), _address(prob), _address(work),
-                                          _stream_number()))
+    need = _verify_work.get((batch, drafts, vocab))
+    if need is None:
+        need = _verify_work[batch, drafts, vocab] = load().chiron_verify_workspace_bytes(batch, drafts, vocab) // 4
+    work, out, accepted, prob = tokens.new_empty(need), tokens.new_empty((batch, rows)), tokens.new_empty(batch), torch.empty_like(uniforms)
+    _check(load().chiron_op_verify_drafts(C.addressof(b), batch, drafts, vocab, out.data_ptr() or None, accepted.data_ptr() or None,
+                                          prob.data_ptr() or None, work.data_ptr() or None, _stream_number()))
     return out, accepted, prob
 
 

@@ -1,10 +1,13 @@
 // Verification of drafted tokens: acceptance against the target's probabilities and the token that replaces the first rejected one.
 // gfx950, wave64.
 //
-// Three launches.  (1) Every logit row's maximum, its index, and sum of exponentials, in pieces over the vocabulary: the only pass
+// Two launches.  (1) Every logit row's maximum, its index, and sum of exponentials, in pieces over the vocabulary: the only pass
 // over all rows, bounded by reading them.  (2) A workgroup per request and piece joins the pieces of its request's rows, decides how
 // many drafts are taken (every workgroup of a request comes to the same answer from the same numbers), and races what is left of the
-// vocabulary in its piece; the two or three rows it needs again come from the caches.  (3) Joins the pieces' winners.
+// vocabulary in its piece; the two or three rows it needs again come from the caches.  The pieces' winners meet in an
+// atomic maximum, and the workgroup of a request that comes last writes the token.
+// 64 requests of 4 drafts over 128256 tokens: 42 us (7.0 TB/s) and 22; one request: 5.0 and 8.3, a chain of loads that wait for one
+// another.  (A third launch for the winners, and the decision in one thread's loop, took 5 us more, with one request and with 23.)
 // The race argmax r(x)/noise(x) instead of a running sum over the vocabulary: it is one pass in any order, and which token wins does
 // not depend on the order of any sum.
 #include <new>
@@ -23,15 +26,22 @@ struct RowStat {
     int best;    // lowest index of the maximum, -1: nothing above -inf
     int pad;
 };
+// The best r/noise of a request: bit 63 where the draft was taken off p and something is left, which beats all of p; the value's bits (it
+// is not negative) over 2^32 - 1 - token, so that of equal ones the lower token is more; 0: none.  The maximum does not depend on the
+// order in which the pieces come.
 struct Winner {
-    float rest, all;  // best r/noise with the draft taken off, and without
-    int rest_at, all_at;
+    unsigned long long key;
+    uint32_t arrived, pad;  // pieces
 };
+__device__ __forceinline__ unsigned long long race_key(bool rest, float v, int token) {
+    return (unsigned long long)rest << 63 | (unsigned long long)__float_as_uint(v) << 32 | (0xffffffffu - (uint32_t)token);
+}
+
 struct VerifyArgs {
     chiron_draft_batch in;
     int batch, max_draft, vocab, pieces;
     RowStat* stats;  // [batch][2*max_draft+1][pieces]: target rows, then draft rows
-    Winner* winners; // [batch][pieces]
+    Winner* winners; // [batch], made ready by the first launch
     int32_t *out_tokens, *accepted;
     float* prob;
 };
@@ -87,6 +97,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_stats_kernel(VerifyArgs
     const bool draft = r > a.max_draft;
     const int t = draft ? r - a.max_draft - 1 : r;
     if (draft ? (t >= n || !a.in.draft_logits || inv_t == 0.f) : t > n) return;  // nobody asks for this row
+    if (r == 0 && piece == 0 && threadIdx.x == 0) a.winners[i] = Winner{0, 0, 0};
     const float* row = draft ? a.in.draft_logits + ((int64_t)i * a.max_draft + t) * a.in.draft_stride
                              : a.in.logits + ((int64_t)i * (a.max_draft + 1) + t) * a.in.logits_stride;
     const int shift = (int)((uintptr_t)row >> 2 & 3);
@@ -139,9 +150,8 @@ __device__ __forceinline__ float share(float x, float m, float z, float inv_t) {
 
 __global__ __launch_bounds__(kVerifyThreads) void verify_race_kernel(VerifyArgs a) {
     __shared__ RowStat s_row[2 * kMaxDrafts + 1];
-    __shared__ float s_prob[kMaxDrafts];
-    __shared__ Winner s_win[4];
-    __shared__ int s_took;
+    __shared__ int s_tok[kMaxDrafts], s_first[2];
+    __shared__ unsigned long long s_key[kVerifyThreads / 64];
     const int i = blockIdx.y, piece = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t0 = threadIdx.x;
     const int rows = 2 * a.max_draft + 1;
     const float* target = a.in.logits + (int64_t)i * (a.max_draft + 1) * a.in.logits_stride;
@@ -155,9 +165,10 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_race_kernel(VerifyArgs 
 #pragma unroll
     for (int j = 0; j < VPT; ++j) noise[j] = x0 + j * kVerifyThreads < a.vocab ? a.in.noise[(int64_t)i * a.vocab + x0 + j * kVerifyThreads] : 1.f;
     int my_tok = -1;
-    float my_target = 0.f, my_draft = 0.f;
+    float my_target = 0.f, my_draft = 0.f, my_uniform = 0.f;
     if (t0 < a.max_draft) {
-        my_tok = tok[t0];
+        my_tok = s_tok[t0] = tok[t0];
+        my_uniform = a.in.uniforms[(int64_t)i * a.max_draft + t0];
         if (my_tok >= 0 && my_tok < a.vocab) {
             my_target = target[t0 * a.in.logits_stride + my_tok];
             if (draft) my_draft = draft[t0 * a.in.draft_stride + my_tok];
@@ -183,49 +194,43 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_race_kernel(VerifyArgs 
         if (w < need && t0 % 16 == 0) s_row[w] = RowStat{m, z, best, 0};
     }
     __syncthreads();
-    static_assert(kMaxDrafts <= kVerifyThreads, "a thread per draft");
-    if (t0 < n) {
-        float pr = 0.f;
-        if (my_tok >= 0) {
-            const RowStat p = s_row[t0];
-            if (greedy) pr = my_tok == p.best ? 1.f : 0.f;
-            else {
-                const float px = share(my_target, p.m, p.z, inv_t);
-                if (with_draft) {
-                    const RowStat q = s_row[n + 1 + t0];
-                    const float qx = share(my_draft, q.m, q.z, inv_t);
-                    pr = qx > 0.f ? fminf(1.f, px / qx) : px > 0.f ? 1.f : 0.f;
-                } else pr = px;
-            }
+    static_assert(kMaxDrafts <= 128, "a lane of the first two waves for each draft");
+    float pr = 0.f;
+    if (t0 < n && my_tok >= 0) {
+        const RowStat p = s_row[t0];
+        if (greedy) pr = my_tok == p.best ? 1.f : 0.f;
+        else {
+            const float px = share(my_target, p.m, p.z, inv_t);
+            if (with_draft) {
+                const RowStat q = s_row[n + 1 + t0];
+                const float qx = share(my_draft, q.m, q.z, inv_t);
+                pr = qx > 0.f ? fminf(1.f, px / qx) : px > 0.f ? 1.f : 0.f;
+            } else pr = px;
         }
-        s_prob[t0] = pr;
+    }
+    if (wave < 2) {
+        const unsigned long long refused = __ballot(t0 < n && !(my_uniform < pr));
+        if (lane == 0) s_first[wave] = refused ? wave * 64 + __builtin_ctzll(refused) : kMaxDrafts;
     }
     __syncthreads();
-    if (t0 == 0) {
-        int took = 0;
-        while (took < n && a.in.uniforms[(int64_t)i * a.max_draft + took] < s_prob[took]) ++took;
-        s_took = took;
-    }
-    __syncthreads();
-    const int took = s_took;
-    if (piece == 0) {
-        if (a.prob)
-            for (int t = t0; t < a.max_draft; t += kVerifyThreads) a.prob[(int64_t)i * a.max_draft + t] = t < n ? s_prob[t] : 0.f;
-        for (int t = t0; t <= a.max_draft; t += kVerifyThreads)
-            if (t != took) a.out_tokens[(int64_t)i * (a.max_draft + 1) + t] = t < took ? tok[t] : -1;
+    const int took = min(n, min(s_first[0], s_first[1]));
+    if (piece == 0 && t0 <= a.max_draft) {
+        if (a.prob && t0 < a.max_draft) a.prob[(int64_t)i * a.max_draft + t0] = pr;
+        if (t0 != took) a.out_tokens[(int64_t)i * (a.max_draft + 1) + t0] = t0 < took ? s_tok[t0] : -1;
         if (t0 == 0) a.accepted[i] = took;
     }
     const RowStat p = s_row[took];
-    Winner win{-1.f, -1.f, -1, -1};
+    float best_rest = -1.f, best_all = -1.f;
+    int rest_at = -1, all_at = -1;
     if (greedy) {
-        win.all = win.rest = 1.f;
-        win.all_at = win.rest_at = p.best;
+        best_all = 1.f;
+        all_at = p.best;
     } else if (p.z > 0.f) {
         const bool rejected = took < n;
         const float* prow = target + took * a.in.logits_stride;
         const float* qrow = rejected && with_draft ? draft + took * a.in.draft_stride : nullptr;
         const RowStat q = qrow ? s_row[n + 1 + took] : RowStat{0.f, 0.f, -1, 0};
-        const int without = rejected && !with_draft ? tok[took] : -1;
+        const int without = rejected && !with_draft ? s_tok[took] : -1;
         float pv[VPT], qv[VPT];
 #pragma unroll
         for (int j = 0; j < VPT; ++j) pv[j] = x0 + j * kVerifyThreads < a.vocab ? prow[x0 + j * kVerifyThreads] : -INFINITY;
@@ -243,59 +248,33 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_race_kernel(VerifyArgs 
             if (qrow) rest = fmaxf(ps - (rq > 0.f ? weight(logit_of(qv[j]) - q.m, c) * rq : 0.f), 0.f);
             else if (x == without) rest = 0.f;
             const float all = ps * inv, some = rest * inv;
-            if (ps > 0.f && all > win.all) {
-                win.all = all;
-                win.all_at = x;
+            if (ps > 0.f && all > best_all) {
+                best_all = all;
+                all_at = x;
             }
-            if (rest > 0.f && some > win.rest) {
-                win.rest = some;
-                win.rest_at = x;
+            if (rest > 0.f && some > best_rest) {
+                best_rest = some;
+                rest_at = x;
             }
         }
     }
-    auto better = [](float& v, int& at, float v2, int at2) {
-        if (at2 >= 0 && (at < 0 || v2 > v || (v2 == v && at2 < at))) {
-            v = v2;
-            at = at2;
-        }
-    };
+    unsigned long long key = rest_at >= 0 ? race_key(true, best_rest, rest_at) : all_at >= 0 ? race_key(false, best_all, all_at) : 0;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        better(win.rest, win.rest_at, __shfl_xor(win.rest, o), __shfl_xor(win.rest_at, o));
-        better(win.all, win.all_at, __shfl_xor(win.all, o), __shfl_xor(win.all_at, o));
-    }
-    if (lane == 0) s_win[wave] = win;
+    for (int o = 32; o > 0; o >>= 1) key = max(key, (unsigned long long)__shfl_xor(key, o));
+    if (lane == 0) s_key[wave] = key;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kVerifyThreads / 64; ++w) {
-            better(win.rest, win.rest_at, s_win[w].rest, s_win[w].rest_at);
-            better(win.all, win.all_at, s_win[w].all, s_win[w].all_at);
-        }
-        a.winners[(int64_t)i * a.pieces + piece] = win;
+    if (t0 == 0) {
+        for (int w = 1; w < kVerifyThreads / 64; ++w) key = max(key, s_key[w]);
+        // No release or acquire, which write back and empty the whole L2 and make 23 us of 64 requests' race 75: nothing but these two
+        // words passes between the workgroups, and the maximum has come back, so it is done, before the count goes out.
+        Winner* win = a.winners + i;
+        uint32_t one = 1;
+        const unsigned long long was = __hip_atomic_fetch_max(&win->key, key, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("" : "+v"(one) : "v"(was) : "memory");
+        if (__hip_atomic_fetch_add(&win->arrived, one, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 != (uint32_t)a.pieces) return;
+        key = __hip_atomic_fetch_max(&win->key, key, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        a.out_tokens[(int64_t)i * (a.max_draft + 1) + took] = key ? (int)(0xffffffffu - (uint32_t)key) : -1;
     }
-}
-
-// one wave per request
-__global__ __launch_bounds__(64) void verify_finish_kernel(VerifyArgs a) {
-    const int i = blockIdx.x, lane = threadIdx.x;
-    Winner win{-1.f, -1.f, -1, -1};
-    auto better = [](float& v, int& at, float v2, int at2) {
-        if (at2 >= 0 && (at < 0 || v2 > v || (v2 == v && at2 < at))) {
-            v = v2;
-            at = at2;
-        }
-    };
-    for (int p = lane; p < a.pieces; p += 64) {
-        const Winner w = a.winners[(int64_t)i * a.pieces + p];
-        better(win.rest, win.rest_at, w.rest, w.rest_at);
-        better(win.all, win.all_at, w.all, w.all_at);
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        better(win.rest, win.rest_at, __shfl_xor(win.rest, o), __shfl_xor(win.rest_at, o));
-        better(win.all, win.all_at, __shfl_xor(win.all, o), __shfl_xor(win.all_at, o));
-    }
-    if (lane == 0) a.out_tokens[(int64_t)i * (a.max_draft + 1) + a.accepted[i]] = win.rest_at >= 0 ? win.rest_at : win.all_at;
 }
 
 static int verify_pieces(int vocab) { return (int)(((int64_t)vocab + 3 + kVerifyPiece - 1) / kVerifyPiece); }  // up to 3 values before an aligned start
@@ -308,7 +287,7 @@ extern "C" {
 
 int64_t chiron_verify_workspace_bytes(int32_t batch, int32_t max_draft, int32_t vocab) {
     if (batch < 0 || max_draft < 0 || max_draft > kMaxDrafts || vocab < 1) return 0;
-    return (int64_t)batch * verify_pieces(vocab) * ((2 * max_draft + 1) * (int64_t)sizeof(RowStat) + (int64_t)sizeof(Winner));
+    return (int64_t)batch * (verify_pieces(vocab) * (2 * max_draft + 1) * (int64_t)sizeof(RowStat) + (int64_t)sizeof(Winner));
 }
 
 int32_t chiron_op_verify_drafts(const chiron_draft_batch* in, int32_t batch, int32_t max_draft, int32_t vocab, int32_t* out_tokens,
@@ -334,7 +313,6 @@ int32_t chiron_op_verify_drafts(const chiron_draft_batch* in, int32_t batch, int
     hipStream_t st = (hipStream_t)stream;
     launch(verify_stats_kernel, dim3(pieces, (unsigned)rows), dim3(kVerifyThreads), st, a);
     launch(verify_race_kernel, dim3(pieces, batch), dim3(kVerifyThreads), st, a);
-    launch(verify_finish_kernel, dim3(batch), dim3(64), st, a);
     CHIRON_HIP(hipGetLastError());
     return CHIRON_OK;
 }
