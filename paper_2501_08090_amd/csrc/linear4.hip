@@ -362,8 +362,8 @@ __global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const fl
 // x enters as two fp16 terms of x * 2^up, up to 2^15 of a block of 128; a group costs one multiplication and one fused multiply-add for
 // each result, where three digits cost five instructions.  64 rows through 8192 x 28672 with groups of 64 and zero points: 80 us, 70 of
 // them in the products, against 100 and 87 with digits (17 rows through 28672 x 4096: 31 and 28).  What bounds it is the matrix cores and
-// the vector units, which share issue and power: with no products 56 us are left of the 70, with no loads of weights or x 60.  Products
-// of 60 TFLOP take 24 us at the rate of the matrix cores, the weights 19.
+// the vector units, which share issue and power: with no products 56 us are left of the 70, with no loads of weights or x 60.  The 60
+// GFLOP run at 0.86 PFLOP/s, a large fp16 product of the library reaches 1.1; the weights take 19 us.
 //
 // x for the whole launch: terms [rows/16][K/128][4 steps of 32][2][64 lanes][16 B], scales [rows/16][K/128][16] fp32.  A lane's eight
 // values of a step lie in the order in which masks take weights out of a dword: (4,6) (0,2) (5,7) (1,3).
