@@ -544,14 +544,30 @@ __global__ __launch_bounds__(256) void sparse_merge_kernel(const float* __restri
     const int64_t rh = j / D;  // (row, KV head, head of the group)
     const int e = (int)(j % D), a = (int)(rh % G);
     const int64_t slot0 = rh / G * splits * G + a;
-    float M = -1e30f;
-    for (int s = 0; s < splits; ++s) M = fmaxf(M, part_ml[(slot0 + (int64_t)s * G) * 2]);
-    float num = 0.f, den = 0.f;
-    for (int s = 0; s < splits; ++s) {
-        const int64_t slot = slot0 + (int64_t)s * G;
-        const float f = __builtin_amdgcn_exp2f(part_ml[slot * 2] - M);
-        num += f * part_o[slot * D + e];
-        den += f * part_ml[slot * 2 + 1];
+    float M = -1e30f, num = 0.f, den = 0.f;
+    constexpr int kAtOnce = 8;  // splits whose loads are on their way together
+    for (int s0 = 0; s0 < splits; s0 += kAtOnce) {
+        float2 ml[kAtOnce];
+        float o[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int64_t slot = slot0 + (int64_t)min(s0 + i, splits - 1) * G;
+            ml[i] = *reinterpret_cast<const float2*>(part_ml + slot * 2);
+            o[i] = part_o[slot * D + e];
+        }
+        float top = M;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) top = fmaxf(top, ml[i].x);
+        const float keep = __builtin_amdgcn_exp2f(M - top);
+        M = top;
+        num *= keep;
+        den *= keep;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const float f = s0 + i < splits ? __builtin_amdgcn_exp2f(ml[i].x - M) : 0.f;
+            num += f * o[i];
+            den += f * ml[i].y;
+        }
     }
     out[j] = den > 0.f ? num / den : 0.f;
 }
