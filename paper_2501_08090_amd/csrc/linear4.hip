@@ -215,7 +215,7 @@ __global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const fl
                                                              int accumulate) {
     constexpr int PER = 128 / GROUP, ROWS = SETS == 1 ? 4 : SETS == 2 ? 8 : 16;
     // tiles on their way: as many as the registers hold beside x
-    constexpr int RING = ONE ? 1 : NB == 8 ? 2 : NB == 4 ? (GROUP == 32 || SETS == 2 ? 2 : 3) : NB == 2 ? (SETS == 3 ? (GROUP == 32 ? 1 : 3) : GROUP == 32 ? 3 : 4) : 6;
+    constexpr int RING = ONE ? 1 : NB == 4 ? (GROUP == 32 || SETS == 2 ? 2 : 3) : NB == 2 ? (SETS == 3 ? (GROUP == 32 ? 1 : 3) : GROUP == 32 ? 3 : 4) : 6;
     __shared__ uint4 s_dig[NB * 8 * 2 * SETS * 64];
     __shared__ float s_base[NB * 8][ROWS];
     __shared__ __align__(16) float s_red[2][8][256];
@@ -692,28 +692,21 @@ static Plan4 plan_linear4(const Linear4& l, int64_t M) {
     const int64_t kb = l.Kpad / 128;
     if (M <= 16) {
         p.sets = M <= 4 ? 1 : M <= 8 ? 2 : 3;
-        const int64_t most = p.sets == 3 || (p.sets == 2 && l.group == 32) ? 2 : p.sets == 2 || l.group < 128 ? 4 : 8;  // what LDS and registers hold
+        const int64_t most = p.sets == 3 || (p.sets == 2 && l.group == 32) ? 2 : 4;  // what LDS and registers hold
         const int64_t tiles = ((int64_t)l.N + 15) / 16;
-        int64_t best = 0;
-        for (int64_t s = 1; s <= 16; s *= 2) {
-            if (s > 1 && kb / s < 4) break;
-            // us, from single measurements: x into a CU at 45 B/ns and its conversion, for each workgroup a CU gets; the weights at a
-            // CU's share of 6 TB/s; a second launch for slices and their traffic
-            const int64_t blocks = (kb + s - 1) / s, room = kNumCU / s;
-            const double rounds = (double)((tiles + room - 1) / room);
-            const double turns = blocks > 8 * most && rounds > kFewTiles ? rounds / kFewTiles : 1.0;
-            const double us = turns * (double)(blocks * 128 * M) * (4.0 / 45e3 + 4e-5) + rounds * (double)blocks * 1024 / 23.4e3 +
-                              (s > 1 ? 5.0 + (double)s * (double)(M * l.N) * 8 / 4e6 : 0.0);
-            static_assert(kNumCU % 16 == 0, "a slice's share of the CUs is a whole number");
-            if (best == 0 || us * 1000 < (double)best) {
-                best = (int64_t)(us * 1000);
-                p.slices = (int)s;
-            }
-        }
+        // Slices of at most 32 blocks up to 4 rows, of 16 with more, whose x takes a workgroup longer than a second launch and the slices'
+        // traffic; 32 too with up to 8 rows where that is all of K and there are tiles for every CU; and of 8, where the chip is not full
+        // otherwise.  us with 1 / 2 / 4 / 8 / 16 slices: 1 row through 8192 x 28672 44 / 35 / 29 / 25 / 36, 8 rows through 8192 x 8192
+        // 19 / 16 / 13.6 / 15.6 / 25 and through 28672 x 4096 17.7 / 18.5 / 23 / 38 / 65, 16 rows through 1024 x 4096 12.2 / 9.6 / 7 /
+        // 8.6 / 10.2.
+        const bool whole = M <= 4 || (M <= 8 && kb <= 32 && tiles >= kNumCU);
+        static_assert(kNumCU % 16 == 0, "a slice's share of the CUs is a whole number");
+        while (p.slices < 16 && (kb + p.slices - 1) / p.slices > (whole ? 32 : 16)) p.slices *= 2;
+        if (!whole && p.slices < 16 && tiles * p.slices <= 2 * kNumCU && kb / (2 * p.slices) >= 8) p.slices *= 2;
         p.slice_blocks = (int)((kb + p.slices - 1) / p.slices);
         p.slices = (int)((kb + p.slice_blocks - 1) / p.slice_blocks);
         const int64_t chunks = (p.slice_blocks + 8 * most - 1) / (8 * most), need = (p.slice_blocks + 8 * chunks - 1) / (8 * chunks);
-        p.nb = need <= 1 ? 1 : need <= 2 ? 2 : need <= 4 ? 4 : 8;
+        p.nb = need <= 1 ? 1 : need <= 2 ? 2 : 4;
         const int64_t room = std::max<int64_t>(1, kNumCU / p.slices);
         int64_t rounds = (tiles + room - 1) / room;
         if (p.slice_blocks > 8 * p.nb) rounds = std::min<int64_t>(rounds, kFewTiles);
@@ -749,8 +742,7 @@ static void launch_linear4(const Linear4& l, const float* x, int M, float* y, in
         if (p.sets == 1) {
             if (p.nb == 1) CHIRON_FEW(1, 1);
             else if (p.nb == 2) CHIRON_FEW(1, 2);
-            else if (p.nb == 4 || GROUP < 128) CHIRON_FEW(1, 4);
-            else if constexpr (GROUP == 128) CHIRON_FEW(1, 8);
+            else CHIRON_FEW(1, 4);
         } else if (p.sets == 2) {
             if (p.nb == 1) CHIRON_FEW(2, 1);
             else if (p.nb == 2 || GROUP == 32) CHIRON_FEW(2, 2);

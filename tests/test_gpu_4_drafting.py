@@ -609,6 +609,18 @@ def test_linear4_larger(N, K, group, M, zeros):
     check_linear4(Rows(), w, sk, x, group)
 
 
+@pytest.mark.parametrize("M", (1, 4, 7, 16, 17))
+@pytest.mark.parametrize("group,zeros", ((128, False), (64, True), (32, True)))
+def test_linear4_long_rows(M, group, zeros):
+    K = 70016 - 70016 % group + group  # more than 16 slices hold at once
+    w4, s, z = weights(24, K, group, zeros, 8)
+    w, sk = D.weights4(w4, s, z, group)
+    lin = B.Linear4(w4.cuda(), s.cuda(), None if z is None else z.cuda())
+    x = torch.randn((M, K), generator=torch.Generator().manual_seed(M))
+    check_linear4(lin, w, sk, x, group)
+    check_linear4(lin, w, sk, x, group, torch.randn((M, 24), generator=torch.Generator().manual_seed(1)), True)
+
+
 @pytest.mark.parametrize("M", (3, 7, 12, 20))
 def test_linear4_rows_that_are_not_aligned(M):
     w4, s, z = weights(40, 384, 128, False, 5)
