@@ -5,6 +5,10 @@
 // pieces.  Requests are ragged and the host knows neither their lengths nor where they start, so the grid has a slot for the most
 // pages that `rows` tokens of `batch` requests can touch: n tokens touch at most n/16 + 2 pages, so request i owns the slots from
 // row_starts[i]/16 + 2i on, and a wave finds its request by bisection.
+//
+// Bound by its bytes, of which more are written than read: 5003 bf16 rows of 32 + 2 * 8 heads of 128 30 us (5.4 TB/s), 16384 fp32 rows
+// with the index 142 us (5.2 TB/s; a copy of 4 GiB 4.7).  64 rows 6.4 us: the launch and a chain of loads (where the request's rows
+// start, its length, its pages, its rows).
 #include <new>
 
 #include "draft_ops.h"

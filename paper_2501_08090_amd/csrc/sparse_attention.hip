@@ -13,7 +13,9 @@ typedef int intx4 __attribute__((ext_vector_type(4)));
 // ---- scores -----------------------------------------------------------------------------------------------------
 // score(p) = 2^e(p) * max_h sum_j (q8+[h][j] hi(p)[j] + q8-[h][j] lo(p)[j]): one product of length 2d per page and head, on the 8-bit
 // matrix cores with whole-number accumulation.  A operand: 16 pages x 64 of the record's 2d codes; B: 16 columns, column c = query
-// head c % G of the KV head.  Bounded by the records' bytes, (2d + 1) per page and head.
+// head c % G of the KV head.  Bounded by the records' bytes, (2d + 1) per page and head: 32 rows of some 28000 tokens, 8 KV heads of 128,
+// 29 us with the selection (4.0 TB/s); one row of 8192 tokens 10.7 us, of which the records of a list need 3, the rest is a chain of
+// loads and of joins over the workgroup.
 struct SelectArgs {
     PoolDesc pool;
     IndexDesc index;
@@ -262,7 +264,8 @@ __device__ __forceinline__ bool select_all(const SelectArgs& a, int list, int n,
 }
 
 // One launch, a workgroup per (row, KV head) that scores its pages into LDS and selects: as long as one CU can take in a list's records
-// in about the time of the second launch, or there are lists for half the CUs.
+// in about the time of the second launch, or there are lists for half the CUs.  (Attention included: one row over 4096 tokens of 2 KV
+// heads of 64 14.1 us, in two launches 15.5; over 32768 of 8 of 128 35, in two 24.9.)
 constexpr int kSelectPages = 15360;  // keys that fit 64 KiB of LDS beside the rest
 template <int D, int G>
 __global__ __launch_bounds__(kSelectThreads, 2) void select_pages_kernel(SelectArgs a) {
@@ -319,7 +322,9 @@ __global__ __launch_bounds__(kSelectThreads) void select_scored_kernel(SelectArg
 // with a running maximum and sum.  q and P enter as three bf16 terms (24 bits): with few heads per KV head the terms of one head
 // take different operand columns of one instruction, column = group * G + head, and the sums over the groups are rotations within
 // 16 lanes.  The waves of a workgroup take parts of one list and merge in LDS; a list may be split over `splits` workgroups, whose
-// partial results a second kernel joins.
+// partial results a second kernel joins (selection included, one row over 8192 tokens, 64 pages of 8 lists: 21.1 us, unsplit 23.1; over
+// 32768: 24.9 and 30.3).  Bound by the pages' bytes: 32 rows x 8 lists of 128 pages of 8 KiB 49 us (5.4 TB/s); one row 9 us, a chain of
+// loads: the list, the block table, keys and values.
 constexpr int kSparseWaves = 8;
 template <int D, int G>
 __global__ __launch_bounds__(kSparseWaves * 64, 2) void sparse_attn_kernel(PoolDesc pool, int layer, const float* __restrict__ q,
