@@ -1,8 +1,8 @@
 // Products of few rows with 4-bit weights: y = x W^T, W[n][k] = (w4 - z) * scale, a scale and a zero point for each row and group of
 // 32, 64 or 128 inputs.  gfx950, wave64.
 //
-// x enters, per row and 128 inputs, with 22 bits of its largest value, on two ways:
-//  - up to 16 rows, where bringing x to the matrix cores costs most, as whole multiples of a power of two, |x| <= 2^22, in three signed
+// x enters, per row and 128 inputs, with 22 to 23 bits of its largest value, on two ways:
+//  - up to 16 rows, where bringing x to the matrix cores costs most, as whole multiples of a power of two, |x| < 2^23, in three signed
 //    8-bit digits: a group's digit sums are exact, and are scaled and added over the groups in fp32.  A weight without zero points is
 //    16 * (w4 - 8), which is its four bits, the highest inverted when the matrix is laid out, in the upper half of a byte: three
 //    instructions for eight weights.  With zero points it is w4 - z: eight bytes, seven instructions.
@@ -141,16 +141,19 @@ __device__ __forceinline__ intx4 group_product(const intx4 (&a)[2], const intx4 
 // three digits' sums as one value; the lower two stay below 2^30 (128 products of at most 128 * 128 each)
 __device__ __forceinline__ float join_digits(int p2, int p1, int p0) { return fmaf((float)p2, 65536.f, (float)((p1 << 8) + p0)); }
 
-// A block's power of two from the bits of its largest magnitude: x * 2^up is at most 2^22.  (Below 2^-105 the digits stop at 2^-127.)
-__device__ __forceinline__ int exponent_up(uint32_t top) { return min(127, 22 - __builtin_amdgcn_frexp_expf(__uint_as_float(top))); }
+// A block's power of two from the bits of its largest magnitude: x * 2^up is below 0.9922 * 2^23, where three signed digits end a little
+// higher.  (Below 2^-104 the digits stop at 2^-127.)
+__device__ __forceinline__ int exponent_up(uint32_t top) {
+    return min(127, 23 - __builtin_amdgcn_frexp_expf(__uint_as_float(top)) - ((top & 0x7fffffu) >= 0x7e0000u));
+}
 // what the lowest digit counts; without zero points weights are 16 times themselves.  Infinity or NaN in the block: NaN
 template <bool ZERO>
 __device__ __forceinline__ float block_scale(uint32_t top) {
     return top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : ldexpf(1.f, -exponent_up(top) - (ZERO ? 0 : 4));
 }
-// 8 consecutive values of a row as signed 8-bit digits q = 65536 d2 + 256 d1 + d0, highest first.  Adding 1.5 * 2^23 rounds x * 2^up to
-// a whole number (to nearest, ties to even) and leaves it in the low bits; 0x8080 more carries into the next digit where one is above
-// 127 and leaves d0 and d1 in their bytes with the highest bit inverted.
+// 8 consecutive values of a row as signed 8-bit digits q = 65536 d2 + 256 d1 + d0, highest first, of x * 2^up rounded to a whole number
+// (to nearest, ties to even); 0x8080 more carries into the next digit where one is above 127 and leaves d0 and d1 in their bytes with
+// the highest bit inverted.
 struct Run {
     uint2 digit[3];
 };
@@ -161,7 +164,7 @@ __device__ __forceinline__ Run digits_of(const float (&v)[8], uint32_t top) {
     for (int h = 0; h < 2; ++h) {
         uint32_t q[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = __float_as_uint(fmaf(v[4 * h + i], up, 12582912.f)) - 0x4b400000u + 0x8080u;
+        for (int i = 0; i < 4; ++i) q[i] = (uint32_t)(int)rintf(v[4 * h + i] * up) + 0x8080u;
         const uint32_t a = __builtin_amdgcn_perm(q[1], q[0], 0x05010400u), b = __builtin_amdgcn_perm(q[3], q[2], 0x05010400u);  // d0 d0 d1 d1
         const uint32_t c = __builtin_amdgcn_perm(q[1], q[0], 0x0c0c0602u), d = __builtin_amdgcn_perm(q[3], q[2], 0x0c0c0602u);  // d2 d2
         const uint32_t d0 = __builtin_amdgcn_perm(b, a, 0x05040100u) ^ 0x80808080u, d1 = __builtin_amdgcn_perm(b, a, 0x07060302u) ^ 0x80808080u;
