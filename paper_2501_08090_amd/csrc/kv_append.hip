@@ -4,11 +4,11 @@
 // index needs (old tokens of the page come from the pool) and can write V, which lies transposed inside its tile, in whole 16-byte
 // pieces.  Requests are ragged and the host knows neither their lengths nor where they start, so the grid has a slot for the most
 // pages that `rows` tokens of `batch` requests can touch: n tokens touch at most n/16 + 2 pages, so request i owns the slots from
-// row_starts[i]/16 + 2i on, and a wave finds its request by bisection.
+// row_starts[i]/16 + 2i on, and a wave finds its request by counting those whose slots have begun, 64 at a time.
 //
-// Bound by its bytes, of which more are written than read: 5003 bf16 rows of 32 + 2 * 8 heads of 128 30 us (5.4 TB/s), 16384 fp32 rows
-// with the index 142 us (5.2 TB/s; a copy of 4 GiB 4.7).  64 rows 6.4 us: the launch and a chain of loads (where the request's rows
-// start, its length, its pages, its rows).
+// Bound by its bytes, of which more are written than read: 5003 bf16 rows of 32 + 2 * 8 heads of 128, which the caches do not hold, 33 us
+// (5.0 TB/s), 16384 fp32 rows with the index 130 us (5.8 TB/s; a copy of 4 GiB 4.7).  64 rows 5.1 us: the launch and a chain of loads
+// (where the request's rows start, its length, its pages, its rows).
 #include <new>
 
 #include "draft_ops.h"
@@ -30,7 +30,34 @@ IndexDesc index_layout(const PoolDesc& p) {
     return x;
 }
 
-// 8 values from dim e on of a row of fp32 or bf16; VEC: 16-byte aligned
+// 4 values from dim e on of a row of fp32 or bf16; VEC: 16-byte aligned; STREAM: nobody reads them again
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+template <bool F32, bool VEC, bool STREAM>
+__device__ __forceinline__ void load4(const void* row, int e, float (&x)[4]) {
+    if (F32) {
+        const float* p = reinterpret_cast<const float*>(row) + e;
+        if (VEC) {
+            const floatx4* pv = reinterpret_cast<const floatx4*>(p);
+            const floatx4 a = STREAM ? __builtin_nontemporal_load(pv) : *pv;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = a[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = p[i];
+        }
+    } else {
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(row) + e;
+        if (VEC) {
+            const u32x2* pv = reinterpret_cast<const u32x2*>(p);
+            const u32x2 a = STREAM ? __builtin_nontemporal_load(pv) : *pv;
+            x[0] = bf16_lo(a[0]); x[1] = bf16_hi(a[0]); x[2] = bf16_lo(a[1]); x[3] = bf16_hi(a[1]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = __uint_as_float((uint32_t)p[i] << 16);
+        }
+    }
+}
+// 8
 template <bool F32, bool VEC>
 __device__ __forceinline__ void load8(const void* row, int e, float (&x)[8]) {
     if (F32) {
@@ -120,7 +147,38 @@ struct AppendArgs {
     float* q_out;
     const int32_t *bt, *row_starts, *seq_lens;
     int layer, n_q, max_blocks, batch, rows, page_wgs;
+    bool stream;  // the queries with the streaming hint
 };
+
+// 4 dims of the lower half of a head and their partners, so that a wave's loads and stores are whole lines
+template <int D, bool F32, bool VEC, bool STREAM>
+__device__ __forceinline__ void rotate_queries(const AppendArgs& a) {
+    const int64_t j = (int64_t)(blockIdx.x - a.page_wgs) * 256 + threadIdx.x;  // (row, head, piece)
+    const int per_row = a.n_q * (D / 8);
+    const int64_t r = j / per_row;
+    if (r >= a.rows) return;
+    const int w = (int)(j - r * per_row), head = w / (D / 8), e = w % (D / 8) * 4;
+    const void* src = (const char*)a.q + r * a.q_stride;
+    float x[4], y[4];
+    load4<F32, VEC, STREAM>(src, head * D + e, x);
+    load4<F32, VEC, STREAM>(src, head * D + e + D / 2, y);
+    const floatx4 c = *reinterpret_cast<const floatx4*>(a.cos_t + r * (D / 2) + e), s = *reinterpret_cast<const floatx4*>(a.sin_t + r * (D / 2) + e);
+    floatx4 u, v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const Turned w = turn(x[i], y[i], c[i], s[i]);
+        u[i] = w.a;
+        v[i] = w.b;
+    }
+    floatx4* dst = reinterpret_cast<floatx4*>(a.q_out + (r * a.n_q + head) * D + e);
+    if (STREAM) {
+        __builtin_nontemporal_store(u, dst);
+        __builtin_nontemporal_store(v, dst + D / 8);
+    } else {
+        dst[0] = u;
+        dst[D / 8] = v;
+    }
+}
 
 // workgroups 0 .. page_wgs-1: four (page slot, KV head) each; the others: queries
 template <int D, bool F32, bool VEC>
@@ -128,45 +186,23 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendArgs a) {
     constexpr int P = D / 32, H = D / 64;  // pieces of 8 dims per lane; a piece's rotary partner is H pieces further
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if ((int)blockIdx.x >= a.page_wgs) {
-        const int64_t j = (int64_t)(blockIdx.x - a.page_wgs) * 256 + threadIdx.x;  // (row, head, piece of the lower half)
-        const int per_row = a.n_q * (D / 16);
-        const int64_t r = j / per_row;
-        if (r >= a.rows) return;
-        const int w = (int)(j - r * per_row), head = w / (D / 16), e = w % (D / 16) * 8;
-        const void* src = (const char*)a.q + r * a.q_stride;
-        float x[8], y[8], c[8], s[8];
-        load8<F32, VEC>(src, head * D + e, x);
-        load8<F32, VEC>(src, head * D + e + D / 2, y);
-        load8<true, true>(a.cos_t + r * (D / 2), e, c);
-        load8<true, true>(a.sin_t + r * (D / 2), e, s);
-        float* dst = a.q_out + (r * a.n_q + head) * D + e;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float4 u, v;
-            float* up = &u.x;
-            float* vp = &v.x;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const Turned w = turn(x[4 * h + i], y[4 * h + i], c[4 * h + i], s[4 * h + i]);
-                up[i] = w.a;
-                vp[i] = w.b;
-            }
-            *reinterpret_cast<float4*>(dst + 4 * h) = u;
-            *reinterpret_cast<float4*>(dst + D / 2 + 4 * h) = v;
-        }
+        if (a.stream) rotate_queries<D, F32, VEC, true>(a);
+        else rotate_queries<D, F32, VEC, false>(a);
         return;
     }
     const int n_kv = a.pool.n_kv;
     const int64_t task = (int64_t)blockIdx.x * 4 + wave;
     const int slot = (int)(task / n_kv), kvh = (int)(task % n_kv);
     // request i owns the slots from row_starts[i]/16 + 2i on: the last i whose first slot is not behind this one
-    int lo = 0, hi = a.batch - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (a.row_starts[mid] / kBlockSize + 2 * mid <= slot) lo = mid;
-        else hi = mid - 1;
+    int req = -1;
+    for (int i0 = 0; i0 < a.batch; i0 += 64) {
+        const int i = min(i0 + lane, a.batch - 1);
+        const uint64_t begun = __ballot(i0 + lane < a.batch && a.row_starts[i] / kBlockSize + 2 * i <= slot);
+        req += __popcll(begun);
+        if (begun != ~(uint64_t)0) break;
     }
-    const int req = lo, r0 = a.row_starts[req], r1 = a.row_starts[req + 1], old = a.seq_lens[req];
+    if (req < 0) return;
+    const int r0 = a.row_starts[req], r1 = a.row_starts[req + 1], old = a.seq_lens[req];
     if (r0 < 0 || r1 > a.rows || r1 <= r0 || old < 0) return;
     const int page = old / kBlockSize + slot - (r0 / kBlockSize + 2 * req);
     const int64_t end = (int64_t)old + (r1 - r0), first = (int64_t)page * kBlockSize;
@@ -177,26 +213,44 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendArgs a) {
     const int64_t row0 = r0 + first - old;  // the row of the page's token 0 (may lie before r0)
     uint16_t* tile = a.pool.base + tile_base(a.pool, a.layer, block, kvh);
 
+    // Everything new that the page needs is on its way before the first of it is used: rows outside the request are replaced by its first
+    // or last, so that no load hangs on a branch.
+    // V: lane = (dim l of 16, four tokens 4u ..); a piece holds those tokens of the dims 32b + l and 32b + 16 + l
+    const int l = lane & 15, u = lane >> 4;
+    float vx[D / 32][2][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const void* src = (const char*)a.v + min(max(row0 + 4 * u + i, (int64_t)r0), (int64_t)r1 - 1) * a.v_stride;
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) {
+            vx[b][0][i] = load1<F32>(src, kvh * D + 32 * b + l);
+            vx[b][1][i] = load1<F32>(src, kvh * D + 32 * b + 16 + l);
+        }
+    }
     // K: lane = (token, group); piece c of 8 dims at (c*16 + token)*8
     const int t = lane & 15, g = lane >> 4;
     const bool is_new = t >= t0 && t < t1;
+    const int64_t r = min(max(row0 + t, (int64_t)r0), (int64_t)r1 - 1);
+    float kx[H][8], ky[H][8], kc[H][8], ks[H][8];
+#pragma unroll
+    for (int p = 0; p < H; ++p) {
+        const int e = (g + 4 * p) * 8;
+        const void* src = (const char*)a.k + r * a.k_stride;
+        load8<F32, VEC>(src, kvh * D + e, kx[p]);
+        load8<F32, VEC>(src, kvh * D + e + D / 2, ky[p]);
+        load8<true, true>(a.cos_t + r * (D / 2), e, kc[p]);
+        load8<true, true>(a.sin_t + r * (D / 2), e, ks[p]);
+    }
     float k[P][8];
     if (is_new) {
-        const int64_t r = row0 + t;
-        const void* src = (const char*)a.k + r * a.k_stride;
 #pragma unroll
         for (int p = 0; p < H; ++p) {
-            const int e = (g + 4 * p) * 8;
-            float x[8], y[8], c[8], s[8];
-            load8<F32, VEC>(src, kvh * D + e, x);
-            load8<F32, VEC>(src, kvh * D + e + D / 2, y);
-            load8<true, true>(a.cos_t + r * (D / 2), e, c);
-            load8<true, true>(a.sin_t + r * (D / 2), e, s);
             uint4 ux, uy;
             uint32_t *px = &ux.x, *py = &uy.x;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const Turned w0 = turn(x[2 * i], y[2 * i], c[2 * i], s[2 * i]), w1 = turn(x[2 * i + 1], y[2 * i + 1], c[2 * i + 1], s[2 * i + 1]);
+                const Turned w0 = turn(kx[p][2 * i], ky[p][2 * i], kc[p][2 * i], ks[p][2 * i]);
+                const Turned w1 = turn(kx[p][2 * i + 1], ky[p][2 * i + 1], kc[p][2 * i + 1], ks[p][2 * i + 1]);
                 px[i] = pack_bf16_rne(w0.a, w1.a);
                 py[i] = pack_bf16_rne(w0.b, w1.b);
                 k[p][2 * i] = bf16_lo(px[i]);
@@ -217,20 +271,10 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendArgs a) {
     }
     if (a.index.base) write_record<P>(a.index, a.layer, block, kvh, k, t < t1);
 
-    // V: lane = (dim l of 16, four tokens 4u ..); a piece holds those tokens of the dims 32b + l and 32b + 16 + l
-    const int l = lane & 15, u = lane >> 4;
     uint16_t* vtile = tile + 16 * D;
 #pragma unroll
     for (int b = 0; b < D / 32; ++b) {
-        float x[2][4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int tk = 4 * u + i;
-            const bool on = tk >= t0 && tk < t1;
-            const void* src = (const char*)a.v + (row0 + tk) * a.v_stride;
-            x[0][i] = on ? load1<F32>(src, kvh * D + 32 * b + l) : 0.f;
-            x[1][i] = on ? load1<F32>(src, kvh * D + 32 * b + 16 + l) : 0.f;
-        }
+        const float (&x)[2][4] = vx[b];
         const uint4 w = make_uint4(pack_bf16_rne(x[0][0], x[0][1]), pack_bf16_rne(x[0][2], x[0][3]), pack_bf16_rne(x[1][0], x[1][1]),
                                    pack_bf16_rne(x[1][2], x[1][3]));
         uint16_t* dst = vtile + ((b * 4 + u) * 16 + l) * 8;
@@ -360,10 +404,13 @@ int32_t chiron_append_kv_rope(chiron_kvpool* p, chiron_kvindex* index, int32_t l
     a.bt = block_table; a.row_starts = row_starts; a.seq_lens = seq_lens;
     a.layer = layer; a.n_q = in->n_q_heads; a.max_blocks = max_blocks_per_seq; a.batch = batch; a.rows = rows;
     const int64_t tasks = ((int64_t)rows / kBlockSize + 2 * (int64_t)batch) * p->d.n_kv;
-    const int64_t q_wgs = in->q ? ((int64_t)rows * in->n_q_heads * (d / 16) + 255) / 256 : 0;
+    const int64_t q_wgs = in->q ? ((int64_t)rows * in->n_q_heads * (d / 8) + 255) / 256 : 0;
     const int64_t page_wgs = (tasks + 3) / 4;
     if (page_wgs + q_wgs > 0x7fffffff) return fail(CHIRON_ERR_SHAPE, "append: %d rows of %d heads are too many for one call", rows, in->n_q_heads);
     a.page_wgs = (int)page_wgs;
+    // Queries that the L2s do not hold together anyway go past them (5003 bf16 rows of 32 heads of 128 37.5 us, 42.8 without; 16384 fp32
+    // rows with the index 128 and 140); fewer stay there for who reads them next.
+    a.stream = (int64_t)rows * in->n_q_heads * d * 4 > (32 << 20);
     hipStream_t st = (hipStream_t)stream;
     const dim3 grid((unsigned)(page_wgs + q_wgs));
     const bool f32 = in->dtype == CHIRON_F32;
