@@ -364,7 +364,7 @@ __global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const fl
 // ---- more rows -------------------------------------------------------------------------------------------------
 // x enters as two fp16 terms of x * 2^up, up to 2^15 of a block of 128; a group costs one multiplication and one fused multiply-add for
 // each result, where three digits cost five instructions.  64 rows through 8192 x 28672 with groups of 64 and zero points: 80 us, 70 of
-// them in the products, against 100 and 87 with digits (17 rows through 28672 x 4096: 31 and 28).  What bounds it is the matrix cores and
+// them in this kernel, against 100 and 87 with digits (17 rows through 28672 x 4096: 31 and 28).  What bounds it is the matrix cores and
 // the vector units, which share issue and power: with no products 56 us are left of the 70, with no loads of weights or x 60.  The 60
 // GFLOP run at 0.86 PFLOP/s, a large fp16 product of the library reaches 1.1; the weights take 19 us.
 //

@@ -14,8 +14,8 @@ typedef int intx4 __attribute__((ext_vector_type(4)));
 // score(p) = 2^e(p) * max_h sum_j (q8+[h][j] hi(p)[j] + q8-[h][j] lo(p)[j]): one product of length 2d per page and head, on the 8-bit
 // matrix cores with whole-number accumulation.  A operand: 16 pages x 64 of the record's 2d codes; B: 16 columns, column c = query
 // head c % G of the KV head.  Bounded by the records' bytes, (2d + 1) per page and head: 32 rows of some 28000 tokens, 8 KV heads of 128,
-// 29 us with the selection (4.0 TB/s); one row of 8192 tokens 10.7 us, of which the records of a list need 3, the rest is a chain of
-// loads and of joins over the workgroup.
+// 34 us with the selection (3.4 TB/s, 29 us where the last-level cache still holds them); one row of 8192 tokens 11 us, of which the
+// scores take 3.7, the selection 2.5, the rest is the launch and a chain of loads.
 struct SelectArgs {
     PoolDesc pool;
     IndexDesc index;

@@ -6,7 +6,7 @@
 // many drafts are taken (every workgroup of a request comes to the same answer from the same numbers), and races what is left of the
 // vocabulary in its piece; the two or three rows it needs again come from the caches.  The pieces' winners meet in an
 // atomic maximum, and the workgroup of a request that comes last writes the token.
-// 64 requests of 4 drafts over 128256 tokens: 42 us (7.0 TB/s) and 22; one request: 5.0 and 8.3, a chain of loads that wait for one
+// 64 requests of 4 drafts over 128256 tokens: 46 us (6.4 TB/s) and 23; one request: 5.4 and 8.7, a chain of loads that wait for one
 // another.  (A third launch for the winners, and the decision in one thread's loop, took 5 us more, with one request and with 23.)
 // The race argmax r(x)/noise(x) instead of a running sum over the vocabulary: it is one pass in any order, and which token wins does
 // not depend on the order of any sum.
