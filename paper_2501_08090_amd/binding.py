@@ -254,7 +254,7 @@ class KVPool:
             heads = q.shape[1]
             qp, qs = _rows_of(q, rows, heads, d, dtype)
             if q_out is None:
-                q_out = torch.empty((rows, heads, d), dtype=torch.float32, device=q.device)
+                q_out = q.new_empty((rows, heads, d)) if dtype is torch.float32 else torch.empty((rows, heads, d), dtype=torch.float32, device=q.device)
             elif q_out.shape != q.shape:
                 raise ValueError("q_out must have q's shape %s, got %s" % (tuple(q.shape), tuple(q_out.shape)))
             out = _address(q_out, torch.float32)
@@ -573,8 +573,7 @@ def op_select_pages(model, pool, kv_index, layer, q, block_table, ctx_lens, top,
     """The pages that each row of q (fp32, rotated) attends, chosen by the page index.  Row r is a token of request row_seq[r] (of
     request r without it) that sees ctx_lens[r] positions.  -> pages int32 [rows, n_kv_heads, top] ascending, then -1; counts int32 [rows]"""
     rows, top = _check_rows(model, q, block_table, ctx_lens, row_seq), index(top)
-    pages = torch.empty((rows, model.cfg.n_kv_heads, max(top, 0)), dtype=torch.int32, device=q.device)
-    counts = torch.empty(rows, dtype=torch.int32, device=q.device)
+    pages, counts = ctx_lens.new_empty((rows, model.cfg.n_kv_heads, max(top, 0))), ctx_lens.new_empty(rows)
     _check(load().chiron_op_select_pages(model._h, pool._h, kv_index._h, index(layer), _address(q, torch.float32), _address(block_table, torch.int32),
                                          _address(row_seq, torch.int32), _address(ctx_lens, torch.int32), rows, top, index(n_first),
                                          index(n_last), _address(pages), _address(counts), _stream_number()))
@@ -662,7 +661,7 @@ class Linear4:
         if y is None:
             if accumulate:
                 raise ValueError("accumulate needs y")
-            y = torch.empty((M, self.N), dtype=torch.float32, device=x.device)
+            y = x.new_empty((M, self.N))
         elif y.numel() != M * self.N:
             raise ValueError("y must be [%d, %d], got %s" % (M, self.N, tuple(y.shape)))
         need = self._work.get(M)
