@@ -94,6 +94,17 @@ def check_append(n_q, n_kv, d, old, new, dtype, seed, layer=0, **kw):
 
 
 @pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("shift", (0, 1))
+def test_append_more_queries_than_the_caches_hold(dtype, shift):
+    check_append(16, 1, 128, old=[0, 7], new=[2200, 2000], dtype=dtype, seed=21, shift=shift)
+
+
+@pytest.mark.parametrize("requests", (63, 64, 65, 150))
+def test_append_many_requests(requests):
+    check_append(4, 2, 64, old=[i * 11 % 40 for i in range(requests)], new=[i * 7 % 5 for i in range(requests)], dtype=torch.bfloat16, seed=22)
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
 @pytest.mark.parametrize("heads", ((4, 2, 64), (8, 8, 128), (16, 1, 128), (12, 12, 64)))
 def test_append_rope_ragged(heads, dtype):
     check_append(*heads, old=[0, 15, 16, 5, 40, 31], new=[1, 1, 1, 0, 37, 18], dtype=dtype, seed=3)
