@@ -14,6 +14,7 @@
 // for W and x alike, so that a group of 32 is what the halves of the operand registers hold.  Scales and zero points lie as
 // [tile][block][row][group of the block], so that what a lane needs of a block is one load.
 #include <algorithm>
+#include <cmath>
 #include <new>
 
 #include "draft_ops.h"
@@ -682,7 +683,7 @@ __global__ __launch_bounds__(512, 2) void linear4_kernel(Linear4 l, Terms tm, in
 
 // How a call of M rows runs: up to 16 by the few-row kernel; more by passes of nearly the same height of up to 64 rows, side by side in
 // one launch (100 rows through 4096 x 4096: 25.5 us, one behind the other 35.6), K sliced until the chip has a workgroup of 256 columns
-// for every CU, each slice at least 4 blocks of 128.
+// for every CU or further slices cost more than they save.
 struct Plan4 {
     int sets = 0, nb = 0, wgs = 0;  // few rows: operands, blocks per wave and chunk, workgroups per slice
     int mt = 0, row_tiles = 0;           // more: row tiles of a workgroup, of all
@@ -719,7 +720,11 @@ static Plan4 plan_linear4(const Linear4& l, int64_t M) {
         const int64_t passes = (M + 63) / 64, want = std::max<int64_t>(1, kNumCU / (groups * passes));
         p.mt = (int)(((M + 15) / 16 + passes - 1) / passes);
         p.row_tiles = (int)(passes * p.mt);
-        const int64_t slices = std::min<int64_t>(want, std::max<int64_t>(1, kb / 4));
+        // a block takes a workgroup 1.3 us, a slice's sums to memory and back M N 8 bytes at 4 TB/s: the least of kb 1.3 / s + s M N 2e-6.
+        // us with 2 / 4 / 8 / 16 slices, 64 rows: 600 x 1024 17.4 / 14.2 / 13.2 / 13.2, 2048 x 2048 25 / 18.5 / 16.7 / 17.7, 4096 x 4096 39 / 27 /
+        // 23 / 25, 14336 x 4096 40 / 30 / 37 / 52.
+        const int64_t least = (int64_t)std::sqrt(6.5e5 * (double)kb / ((double)M * (double)l.N));
+        const int64_t slices = std::max<int64_t>(1, std::min(std::min(want, least), kb));
         p.slice_blocks = (int)((kb + slices - 1) / slices);
         p.slices = (int)((kb + p.slice_blocks - 1) / p.slice_blocks);
         p.term_bytes = p.row_tiles * kb * 8192;
