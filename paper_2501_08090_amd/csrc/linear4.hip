@@ -2,11 +2,11 @@
 // 32, 64 or 128 inputs.  gfx950, wave64.
 //
 // x enters, per row and 128 inputs, with 22 to 23 bits of its largest value, on two ways:
-//  - up to 16 rows, where bringing x to the matrix cores costs most, as whole multiples of a power of two, |x| < 2^23, in three signed
-//    8-bit digits: a group's digit sums are exact, and are scaled and added over the groups in fp32.  A weight without zero points is
+//  - few rows (passes of up to 16), where bringing x to the matrix cores costs most, as whole multiples of a power of two, |x| < 2^23,
+//    in three signed 8-bit digits: a group's digit sums are exact, and are scaled and added over the groups in fp32.  A weight without zero points is
 //    16 * (w4 - 8), which is its four bits, the highest inverted when the matrix is laid out, in the upper half of a byte: three
 //    instructions for eight weights.  With zero points it is w4 - z: eight bytes, seven instructions.
-//  - more rows as two fp16 terms, whose products with w4 - z, exact in fp16, meet in one fp32 sum.
+//  - many rows as two fp16 terms, whose products with w4 - z, exact in fp16, meet in one fp32 sum.
 // (Scales multiply sums, not weights: w4 - z times a bf16 scale has 12 bits, one more than fp16.)
 //
 // Layout: tiles of 16 rows of W and 128 of K, 1 KiB each, a tile's blocks one behind the other: lane l holds row l % 16 and 32 values
@@ -200,7 +200,7 @@ __device__ __forceinline__ uint32_t block_top(const float (&v)[8]) {
     return top;
 }
 
-// ---- up to 16 rows ---------------------------------------------------------------------------------------------
+// ---- few rows --------------------------------------------------------------------------------------------------
 // A workgroup converts its slice of x to digits once, in LDS, and then walks tiles of 16 columns; its 8 waves own NB blocks of K each,
 // whose x stays in registers, and add their sums through LDS.  With up to 4 rows the three digits of a row take different columns of
 // one operand (column = 4 * digit + row), with up to 8 two operands (8 * digit + row), else three.  A slice of more than 8 NB blocks
@@ -215,7 +215,7 @@ constexpr int kFewTiles = 12;
 __device__ __forceinline__ int few_slot(int k64, int g, int c) { return g * 16 + (c ^ (g * 4 + (k64 & 3))); }
 // ONE: no workgroup has more than one tile, so that there is nothing to read ahead.
 template <int GROUP, bool ZERO, int SETS, int NB, bool ONE>
-__global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const float* __restrict__ x, int M, int slice_blocks, float* __restrict__ y,
+__global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const float* __restrict__ x, int rows, int pass_rows, int slice_blocks, float* __restrict__ y,
                                                              int accumulate) {
     constexpr int PER = 128 / GROUP, ROWS = SETS == 1 ? 4 : SETS == 2 ? 8 : 16;
     // tiles on their way: as many as the registers hold beside x
@@ -229,7 +229,9 @@ __global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const fl
     const int kb = l.Kpad / 128, tiles = (l.N + 15) / 16;
     const int out_row = threadIdx.x & 15, out_m = threadIdx.x >> 4;  // what a thread writes of a tile
     const int k0 = blockIdx.y * slice_blocks, k1 = min(kb, k0 + slice_blocks);
-    y += (int64_t)blockIdx.y * M * l.N;
+    const int m0 = blockIdx.z * pass_rows, M = min(pass_rows, rows - m0);  // this pass's rows
+    x += (int64_t)m0 * l.K;
+    y += ((int64_t)blockIdx.y * rows + m0) * l.N;
     // what digit a column holds in each set: weight 2^(16 - 8 digit), none behind the third
     float f[SETS];
 #pragma unroll
@@ -362,7 +364,7 @@ __global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const fl
     }
 }
 
-// ---- more rows -------------------------------------------------------------------------------------------------
+// ---- many rows -------------------------------------------------------------------------------------------------
 // x enters as two fp16 terms of x * 2^up, up to 2^15 of a block of 128; a group costs one multiplication and one fused multiply-add for
 // each result, where three digits cost five instructions.  64 rows through 8192 x 28672 with groups of 64 and zero points: 80 us, 70 of
 // them in this kernel, against 100 and 87 with digits (17 rows through 28672 x 4096: 31 and 28).  What bounds it is the matrix cores and
@@ -681,11 +683,11 @@ __global__ __launch_bounds__(512, 2) void linear4_kernel(Linear4 l, Terms tm, in
     }
 }
 
-// How a call of M rows runs: up to 16 by the few-row kernel; more by passes of nearly the same height of up to 64 rows, side by side in
-// one launch (100 rows through 4096 x 4096: 25.5 us, one behind the other 35.6), K sliced until the chip has a workgroup of 256 columns
+// How a call of M rows runs: by passes of the few-row kernel, or by tiles of nearly the same height of up to 64 rows, side by side in one
+// launch (100 rows through 4096 x 4096: 25.5 us, one behind the other 35.6), K sliced until the chip has a workgroup of 256 columns
 // for every CU or further slices cost more than they save.
 struct Plan4 {
-    int sets = 0, nb = 0, wgs = 0;  // few rows: operands, blocks per wave and chunk, workgroups per slice
+    int passes = 0, pass_rows = 0, sets = 0, nb = 0, wgs = 0;  // few rows: operands, blocks per wave and chunk, workgroups per slice and pass
     int mt = 0, row_tiles = 0;           // more: row tiles of a workgroup, of all
     int slices = 1, slice_blocks = 0;
     int64_t term_bytes = 0, scale_bytes = 0, part_bytes = 0;
@@ -694,35 +696,42 @@ struct Plan4 {
 static Plan4 plan_linear4(const Linear4& l, int64_t M) {
     Plan4 p;
     const int64_t kb = l.Kpad / 128;
-    if (M <= 16) {
-        p.sets = M <= 4 ? 1 : M <= 8 ? 2 : 3;
+    // More than 16 rows by passes of up to 16 too, as long as all passes' weights stay within 2^27 (2^26 * 1.25 with smaller groups): one
+    // launch, or two, for the tiles' three, but every pass unpacks the weights again.  us passes / tiles, groups of 128: 64 rows through
+    // 600 x 1024 5.2 / 13.2, 4096 x 4096 16.4 / 23, 8192 x 4096 (2^27) 22.9 / 26, 14336 x 4096 32 / 30; 32 rows through 4096 x 14336
+    // (1.75 * 2^26) 23.4 / 21.7, 14336 x 4096 21.3 / 22.1; groups of 64: 64 rows through 4096 x 4096 (2^26) 19.3 / 23.8, 48 through 8192
+    // x 4096 (1.5 * 2^26) 24.9 / 23.2.
+    const int64_t passes = (M + 15) / 16, limit = (l.group == 128 ? 8 : 5) * ((int64_t)1 << 24);
+    if (passes == 1 || passes * l.N * kb * 128 <= limit) {
+        p.passes = (int)passes;
+        p.pass_rows = (int)((M + p.passes - 1) / p.passes);
+        p.sets = p.pass_rows <= 4 ? 1 : p.pass_rows <= 8 ? 2 : 3;
         const int64_t most = p.sets == 3 || (p.sets == 2 && l.group == 32) ? 2 : 4;  // what LDS and registers hold
-        const int64_t tiles = ((int64_t)l.N + 15) / 16;
+        const int64_t tiles = ((int64_t)l.N + 15) / 16, all = tiles * p.passes;
         // Slices of at most 32 blocks up to 4 rows, of 16 with more, whose x takes a workgroup longer than a second launch and the slices'
         // traffic; 32 too with up to 8 rows where that is all of K and there are tiles for every CU; and of 8, where the chip is not full
         // otherwise.  us with 1 / 2 / 4 / 8 / 16 slices: 1 row through 8192 x 28672 44 / 35 / 29 / 25 / 36, 8 rows through 8192 x 8192
         // 19 / 16 / 13.6 / 15.6 / 25 and through 28672 x 4096 17.7 / 18.5 / 23 / 38 / 65, 16 rows through 1024 x 4096 12.2 / 9.6 / 7 /
         // 8.6 / 10.2.
-        const bool whole = M <= 4 || (M <= 8 && kb <= 32 && tiles >= kNumCU);
+        const bool whole = p.sets == 1 || (p.sets == 2 && kb <= 32 && all >= kNumCU);
         static_assert(kNumCU % 16 == 0, "a slice's share of the CUs is a whole number");
         while (p.slices < 16 && (kb + p.slices - 1) / p.slices > (whole ? 32 : 16)) p.slices *= 2;
-        if (!whole && p.slices < 16 && tiles * p.slices <= 2 * kNumCU && kb / (2 * p.slices) >= 8) p.slices *= 2;
+        if (!whole && p.slices < 16 && all * p.slices <= 2 * kNumCU && kb / (2 * p.slices) >= 8) p.slices *= 2;
         p.slice_blocks = (int)((kb + p.slices - 1) / p.slices);
         p.slices = (int)((kb + p.slice_blocks - 1) / p.slice_blocks);
         const int64_t chunks = (p.slice_blocks + 8 * most - 1) / (8 * most), need = (p.slice_blocks + 8 * chunks - 1) / (8 * chunks);
         p.nb = need <= 1 ? 1 : need <= 2 ? 2 : 4;
-        const int64_t room = std::max<int64_t>(1, kNumCU / p.slices);
+        const int64_t room = std::max<int64_t>(1, kNumCU / (p.slices * p.passes));
         int64_t rounds = (tiles + room - 1) / room;
         if (p.slice_blocks > 8 * p.nb) rounds = std::min<int64_t>(rounds, kFewTiles);
         p.wgs = (int)((tiles + rounds - 1) / rounds);
     } else {
         const int64_t groups = ((int64_t)l.N + 255) / 256;
-        const int64_t passes = (M + 63) / 64, want = std::max<int64_t>(1, kNumCU / (groups * passes));
-        p.mt = (int)(((M + 15) / 16 + passes - 1) / passes);
-        p.row_tiles = (int)(passes * p.mt);
+        const int64_t high = (M + 63) / 64, want = std::max<int64_t>(1, kNumCU / (groups * high));
+        p.mt = (int)((passes + high - 1) / high);
+        p.row_tiles = (int)(high * p.mt);
         // a block takes a workgroup 1.3 us, a slice's sums to memory and back M N 8 bytes at 4 TB/s: the least of kb 1.3 / s + s M N 2e-6.
-        // us with 2 / 4 / 8 / 16 slices, 64 rows: 600 x 1024 17.4 / 14.2 / 13.2 / 13.2, 2048 x 2048 25 / 18.5 / 16.7 / 17.7, 4096 x 4096 39 / 27 /
-        // 23 / 25, 14336 x 4096 40 / 30 / 37 / 52.
+        // us with 2 / 4 / 8 / 16 slices, 64 rows: 8192 x 8192 65 / 41 / 31.7 / 41, 14336 x 4096 40 / 30 / 37 / 52, 4096 x 14336 104 / 59 / 37.5 / 30.
         const int64_t least = (int64_t)std::sqrt(6.5e5 * (double)kb / ((double)M * (double)l.N));
         const int64_t slices = std::max<int64_t>(1, std::min(std::min(want, least), kb));
         p.slice_blocks = (int)((kb + slices - 1) / slices);
@@ -739,13 +748,13 @@ static void launch_linear4(const Linear4& l, const float* x, int M, float* y, in
     float* part = (float*)((char*)work + p.term_bytes + p.scale_bytes);
     float* out = p.slices > 1 ? part : y;
     const int add = p.slices > 1 ? 0 : accumulate;
-    if (M <= 16) {
-        const dim3 grid(p.wgs, p.slices);
+    if (p.passes) {
+        const dim3 grid(p.wgs, p.slices, p.passes);
         const bool one = p.wgs == (l.N + 15) / 16;
 #define CHIRON_FEW(SETS_, NB_)                                                                                                                        \
     do {                                                                                                                                              \
-        if (one) launch(linear4_few_kernel<GROUP, ZERO, SETS_, NB_, true>, grid, dim3(512), st, l, x, M, p.slice_blocks, out, add);              \
-        else launch(linear4_few_kernel<GROUP, ZERO, SETS_, NB_, false>, grid, dim3(512), st, l, x, M, p.slice_blocks, out, add);                 \
+        if (one) launch(linear4_few_kernel<GROUP, ZERO, SETS_, NB_, true>, grid, dim3(512), st, l, x, M, p.pass_rows, p.slice_blocks, out, add);              \
+        else launch(linear4_few_kernel<GROUP, ZERO, SETS_, NB_, false>, grid, dim3(512), st, l, x, M, p.pass_rows, p.slice_blocks, out, add);                 \
     } while (0)
         if (p.sets == 1) {
             if (p.nb == 1) CHIRON_FEW(1, 1);

@@ -632,6 +632,57 @@ def test_linear4_long_rows(M, group, zeros):
     check_linear4(lin, w, sk, x, group, torch.randn((M, 24), generator=torch.Generator().manual_seed(1)), True)
 
 
+def some_columns(lin, pick):
+    """lin as far as check_linear4 goes, of the columns `pick`"""
+    class Some:
+        N = len(pick)
+
+        def __call__(self, x, y, accumulate):
+            whole = None
+            if y is not None:
+                whole = torch.zeros((x.shape[0], lin.N), device="cuda")
+                whole[:, pick] = y
+            return lin(x, whole, accumulate)[:, pick]
+    return Some()
+
+
+# rows and sizes that the tiled kernel takes: every height of its tiles, one pass and more
+@pytest.mark.parametrize("N,K,group,M", ((8001, 8448, 128, 17), (8001, 8448, 128, 32), (5333, 8448, 128, 48), (4001, 8448, 128, 64), (2700, 8448, 128, 100),
+                                         (1900, 8448, 128, 130), (5003, 8480, 32, 17), (3400, 8480, 32, 33), (2507, 8480, 32, 64), (5003, 8512, 64, 20),
+                                         (3401, 8512, 64, 40), (2507, 8512, 64, 64), (1700, 8512, 64, 100)))
+@pytest.mark.parametrize("zeros", (False, True))
+def test_linear4_many_rows(N, K, group, M, zeros):
+    w4, s, z = weights(N, K, group, zeros, 12)
+    lin = B.Linear4(w4.cuda(), s.cuda(), None if z is None else z.cuda())
+    pick = np.r_[0:20, 240:272, N // 2:N // 2 + 20, N - 40:N]
+    w, sk = D.weights4(w4[pick], s[pick], None if z is None else z[pick], group)
+    x = torch.randn((M, K), generator=torch.Generator().manual_seed(M))
+    x[:, 17] *= 100.0
+    check_linear4(some_columns(lin, pick), w, sk, x, group)
+    check_linear4(some_columns(lin, pick), w, sk, x, group, torch.randn((M, len(pick)), generator=torch.Generator().manual_seed(1)), True)
+    flat = torch.zeros(M * K + 1, device="cuda")
+    flat[1:] = x.view(-1).cuda()
+    assert torch.equal(lin(flat[1:].view(M, K)), lin(x.cuda()))
+
+
+def test_linear4_many_rows_of_every_kind():
+    w4, s, z = weights(2507, 8512, 64, True, 9)
+    pick = np.r_[0:64]
+    w, sk = D.weights4(w4[pick], s[pick], z[pick], 64)
+    lin = B.Linear4(w4.cuda(), s.cuda(), z.cuda())
+    some = some_columns(lin, pick)
+    x = torch.randn((64, 8512), generator=torch.Generator().manual_seed(4))
+    x[0] = 0
+    x[0, 100] = 1e-30
+    x[1, 64:128] = 0
+    x[1, 300] = 1e20
+    check_linear4(some, w, sk, x, 64)
+    x[0, 5], x[1, 8500] = float("nan"), float("-inf")
+    check_linear4(some, w, sk, x, 64)
+    x = torch.full((64, 8512), 1e-41)
+    assert lin(x.cuda()).abs().max().item() < 1e-36
+
+
 @pytest.mark.parametrize("M", (3, 7, 12, 20))
 def test_linear4_rows_that_are_not_aligned(M):
     w4, s, z = weights(40, 384, 128, False, 5)
