@@ -195,9 +195,10 @@ __device__ __forceinline__ uint32_t block_top(const float (&v)[8]) {
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-    return top;
+    top = max(top, (uint32_t)row_move<kRor8>((int)top));
+    top = max(top, (uint32_t)row_move<kRor4>((int)top));
+    top = max(top, (uint32_t)row_move<kRor2>((int)top));
+    return max(top, (uint32_t)row_move<kRor1>((int)top));
 }
 
 // ---- few rows --------------------------------------------------------------------------------------------------
@@ -206,7 +207,7 @@ __device__ __forceinline__ uint32_t block_top(const float (&v)[8]) {
 // one operand (column = 4 * digit + row), with up to 8 two operands (8 * digit + row), else three.  A slice of more than 8 NB blocks
 // goes in chunks, whose sums wait in LDS (for kFewTiles tiles at most): adding them up in y would put a load behind the weights on their
 // way, and what it waits for would be all of them.  The loops hold no branch that depends on a wave: blocks behind the slice's end
-// read the last one again and count with 0.  8 rows through 28672 x 4096: 17.7 us, 3.4 TB/s; one through 4096 x 4096: 5.
+// read the last one again and count with 0.  8 rows through 28672 x 4096: 17 us, 3.6 TB/s; one through 4096 x 4096: 5.
 // Bound by what stands before and beside the stream of weights: the launch, bringing x in (its conversion is a chain of loads, a maximum
 // over 16 lanes and LDS) and, with more rows, the scaling of the digits' sums.
 // Digits lie in LDS as the operands want them, 16 bytes a lane, column c of lane group g and step k in the place c ^ (4 g + k % 4) of its
