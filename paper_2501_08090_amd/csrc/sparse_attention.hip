@@ -155,10 +155,14 @@ __device__ __forceinline__ void select_top(const SelectArgs& a, int n, const Key
             hi = max(hi, k);
         }
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
+        for (int o = 32; o >= 16; o >>= 1) {
             lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
             hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
         }
+        lo = min(lo, (uint32_t)row_move<kRor8>((int)lo)), hi = max(hi, (uint32_t)row_move<kRor8>((int)hi));
+        lo = min(lo, (uint32_t)row_move<kRor4>((int)lo)), hi = max(hi, (uint32_t)row_move<kRor4>((int)hi));
+        lo = min(lo, (uint32_t)row_move<kRor2>((int)lo)), hi = max(hi, (uint32_t)row_move<kRor2>((int)hi));
+        lo = min(lo, (uint32_t)row_move<kRor1>((int)lo)), hi = max(hi, (uint32_t)row_move<kRor1>((int)hi));
         if (lane == 0) {
             sh.lo[wave] = lo;
             sh.hi[wave] = hi;

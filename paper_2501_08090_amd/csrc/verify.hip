@@ -37,6 +37,10 @@ __device__ __forceinline__ unsigned long long race_key(bool rest, float v, int t
     return (unsigned long long)rest << 63 | (unsigned long long)__float_as_uint(v) << 32 | (0xffffffffu - (uint32_t)token);
 }
 
+template <int Ctrl>
+__device__ __forceinline__ unsigned long long moved(unsigned long long key) {
+    return (unsigned long long)(uint32_t)row_move<Ctrl>((int)(key >> 32)) << 32 | (uint32_t)row_move<Ctrl>((int)key);
+}
 struct VerifyArgs {
     chiron_draft_batch in;
     int batch, max_draft, vocab, pieces;
@@ -74,15 +78,24 @@ __device__ __forceinline__ void join(float& m, float& z, int& best, float m2, fl
         if (m2 == m) best = min(best, best2);
     }
 }
-// joins over LANES neighbouring lanes
+// joins over 16 neighbouring lanes, or all 64: every step with a lane that has joined others
+template <int Ctrl>
+__device__ __forceinline__ void join_moved(float& m, float& z, int& best, float c) {
+    const float m2 = row_move<Ctrl>(m), z2 = row_move<Ctrl>(z);
+    join(m, z, best, m2, z2, row_move<Ctrl>(best), c);
+}
 template <int LANES>
 __device__ __forceinline__ void join_lanes(float& m, float& z, int& best, float c) {
 #pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) {
+    for (int o = LANES / 2; o >= 16; o >>= 1) {
         const float m2 = __shfl_xor(m, o), z2 = __shfl_xor(z, o);
         const int b2 = __shfl_xor(best, o);
         join(m, z, best, m2, z2, b2, c);
     }
+    join_moved<kRor8>(m, z, best, c);
+    join_moved<kRor4>(m, z, best, c);
+    join_moved<kRor2>(m, z, best, c);
+    join_moved<kRor1>(m, z, best, c);
 }
 
 // Rows of any length begin at any multiple of 4 bytes: a piece is 1024 vectors of 16 bytes counted from the 16-byte boundary at or
@@ -259,8 +272,12 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_race_kernel(VerifyArgs 
         }
     }
     unsigned long long key = rest_at >= 0 ? race_key(true, best_rest, rest_at) : all_at >= 0 ? race_key(false, best_all, all_at) : 0;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) key = max(key, (unsigned long long)__shfl_xor(key, o));
+    key = max(key, (unsigned long long)__shfl_xor(key, 32));
+    key = max(key, (unsigned long long)__shfl_xor(key, 16));
+    key = max(key, moved<kRor8>(key));
+    key = max(key, moved<kRor4>(key));
+    key = max(key, moved<kRor2>(key));
+    key = max(key, moved<kRor1>(key));
     if (lane == 0) s_key[wave] = key;
     __syncthreads();
     if (t0 == 0) {
