@@ -137,7 +137,7 @@ int32_t chiron_gather_kv(const chiron_kvpool *p, int32_t layer, const int32_t *b
  *   block_table  dev int32 [batch, max_blocks_per_seq]; a written page must belong to one request only
  *   index        optional: the records of every written page are brought up to date from all its tokens (old and new)
  * A request may bring no row.  Tokens whose page is not one of the pool, or behind the table's last column, are not
- * written.  rows == 0 is a no-op.  No other slot of a page is touched. */
+ * written, nor are some of those of row starts that do not ascend.  rows == 0 is a no-op.  No other slot of a page is touched. */
 enum { CHIRON_F32 = 2 };
 typedef struct chiron_kvindex chiron_kvindex;
 typedef struct {

@@ -204,9 +204,10 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendArgs a) {
     if (req < 0) return;
     const int r0 = a.row_starts[req], r1 = a.row_starts[req + 1], old = a.seq_lens[req];
     if (r0 < 0 || r1 > a.rows || r1 <= r0 || old < 0) return;
-    const int page = old / kBlockSize + slot - (r0 / kBlockSize + 2 * req);
+    const int ahead = slot - (r0 / kBlockSize + 2 * req);  // below 0 only where the row starts do not ascend
+    const int page = old / kBlockSize + ahead;
     const int64_t end = (int64_t)old + (r1 - r0), first = (int64_t)page * kBlockSize;
-    if (first >= end || page >= a.max_blocks) return;
+    if (ahead < 0 || first >= end || page >= a.max_blocks) return;
     const int block = a.bt[(size_t)req * a.max_blocks + page];
     if (block < 0 || block >= a.pool.num_blocks) return;
     const int t0 = (int)max((int64_t)0, old - first), t1 = (int)min((int64_t)kBlockSize, end - first);  // new tokens of the page
