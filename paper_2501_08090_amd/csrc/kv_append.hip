@@ -385,7 +385,8 @@ int32_t chiron_append_kv_rope(chiron_kvpool* p, chiron_kvindex* index, int32_t l
     if (!in->q != !in->q_out) return fail(CHIRON_ERR_INVALID_ARG, "append: q and q_out come together");
     const int d = p->d.d;
     if (in->q && (in->n_q_heads < 1 || in->n_q_heads > 0x7fffffff / d)) return fail(CHIRON_ERR_INVALID_ARG, "append: n_q_heads %d", in->n_q_heads);
-    if (rows == 0 || batch == 0) return CHIRON_OK;
+    if (rows == 0) return CHIRON_OK;
+    if (batch == 0) return fail(CHIRON_ERR_INVALID_ARG, "append: %d rows of no request", rows);
     if (!in->k || !in->v || !in->cos || !in->sin || !block_table || !row_starts || !seq_lens)
         return fail(CHIRON_ERR_INVALID_ARG, "append: a pointer argument is null");
     if (max_blocks_per_seq < 1) return fail(CHIRON_ERR_INVALID_ARG, "max_blocks_per_seq must be positive");

@@ -31,3 +31,13 @@ def test_append_row_starts_out_of_order_stay_inside_the_table():
     for b in range(cols, 64):  # pages of other requests than the first, which alone has rows in order
         assert np.array_equal(ak[b], before[0][b]) and np.array_equal(av[b], before[1][b]), b
         assert (codes[b] == 0x55).all() and (exps[b] == 0x55).all(), b
+
+
+def test_append_rows_of_no_request_are_refused():
+    c = D.Cache(2, 1, 64, 4)
+    k, cs = torch.ones((3, 1, 64), device="cuda"), torch.zeros((3, 32), device="cuda")
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    with pytest.raises(B.ChironError) as e:
+        c.pool.append_rope(0, k, k, cs, cs, torch.zeros((1, 4), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), none, q=k)
+    assert e.value.code == -1
+    c.pool.append_rope(0, k[:0], k[:0], cs[:0], cs[:0], torch.zeros((1, 4), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), none)
