@@ -117,7 +117,8 @@ int32_t chiron_op_sparse_attention(chiron_model *m, const chiron_kvpool *p, int3
  *     out_tokens[i] = x_0 .. x_{a-1}, new token, -1, ...
  * With uniforms uniform in [0,1) and noise from the unit exponential distribution the tokens are distributed as the target's
  * own samples.  draft_logits null: drafts that were not sampled (q is 1 at x_t).  temperature 0 (or no number above it): the greedy choice:
- * prob is 1 where x_t has the highest logit (of equal ones the lowest token), else 0, and the new token has the highest.
+ * prob is 1 where x_t has the highest logit (of equal ones the lowest token), else 0, and the new token has the highest.  temperature
+ * +inf: the same share for every token whose logit is above -inf.
  * NaN logits count as -inf, +inf as the largest finite value; in a row without any logit above -inf every p is 0 and the new token -1.
  * A drafted token outside 0 .. vocab-1 has prob 0.
  *   logits        dev fp32 [batch][max_draft+1][vocab], row (i,t) at logits + (i*(max_draft+1)+t)*logits_stride

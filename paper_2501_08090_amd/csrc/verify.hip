@@ -54,10 +54,13 @@ struct VerifyArgs {
 __device__ __forceinline__ float weight(float d, float c) { return __builtin_amdgcn_exp2f(d * c); }
 __device__ __forceinline__ float log2e_over(float inv_t) { return fminf(inv_t * 1.44269504088896341f, kTopF32); }
 __device__ __forceinline__ float logit_of(float x) { return x != x ? -INFINITY : fminf(x, kTopF32); }
+// 1 / T of a request; 0: greedy.  A temperature above 0 never comes out as that: 1 / inf is taken as the least number above 0, which
+// leaves logits that are no infinity alike and those of -inf at -inf.
+constexpr float kLeastF32 = 1.401298464324817e-45f;
 __device__ __forceinline__ float inv_temperature(const VerifyArgs& a, int i) {
     if (!a.in.temperature) return 1.f;
     const float t = a.in.temperature[i];
-    return t > 0.f ? fminf(1.f / t, kTopF32) : 0.f;  // 0: greedy
+    return t > 0.f ? fmaxf(fminf(1.f / t, kTopF32), kLeastF32) : 0.f;
 }
 __device__ __forceinline__ int drafts_of(const VerifyArgs& a, int i) {
     return a.in.draft_lens ? min(max(a.in.draft_lens[i], 0), a.max_draft) : a.max_draft;

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import drafting as D
+import test_gpu_4_drafting as T
 from paper_2501_08090_amd import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -41,3 +42,24 @@ def test_append_rows_of_no_request_are_refused():
         c.pool.append_rope(0, k, k, cs, cs, torch.zeros((1, 4), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), none, q=k)
     assert e.value.code == -1
     c.pool.append_rope(0, k[:0], k[:0], cs[:0], cs[:0], torch.zeros((1, 4), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), none)
+
+
+@pytest.mark.parametrize("with_draft", (True, False))
+def test_verify_temperature_without_end(with_draft):
+    """softmax(logits / T) at T = +inf: the same for every token whose logit is above -inf, and so at 3e38, where the quotients are below
+    2^-100.  The definition for these is that of logits which are all 0 or -inf."""
+    logits, draft, tokens, u, noise = T.drafts(8, 3, 3001, 61)
+    logits[1, :, ::2] = float("-inf")
+    draft[2, :, ::3] = float("-inf")
+    draft[3, 0, tokens[3, 0].long()] = float("-inf")
+    temp = torch.tensor([float("inf")] * 5 + [3e38, 1.0, 0.0])
+    print("verify", tuple(logits.shape), temp.tolist(), flush=True)
+    out, took, prob = (t.cpu().numpy() for t in B.verify_drafts(logits.cuda(), tokens.cuda(), u.cuda(), noise.cuda(), draft.cuda() if with_draft else None,
+                                                                None, temp.cuda()))
+    flat = lambda z, t: torch.where(z.isneginf(), z, torch.zeros(())).numpy() if t > 1e38 else z.numpy()  # noqa: E731
+    for i in range(8):
+        t = float(temp[i])
+        want, a, pr, near = D.verify(flat(logits[i], t), tokens[i].numpy(), u[i].numpy(), noise[i].numpy(), flat(draft[i], t) if with_draft else None, 3,
+                                     1.0 if t > 1e38 else t)
+        assert (abs(prob[i] - pr) <= 2.0 ** -16 * pr).all(), (i, prob[i], pr)
+        assert near or (took[i] == a and out[i].tolist() == want), (i, out[i], want)
