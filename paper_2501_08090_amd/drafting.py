@@ -11,6 +11,7 @@ whatever the draft.
 runs it on the two-layer toy decoder with random weights.
 """
 import argparse
+import math
 
 import numpy as np
 import torch
@@ -87,10 +88,17 @@ class Drafter:
 
 
 def sample(logits, temperature, noise):
-    """a token per row: argmax of softmax(logits / T) / noise, or of the logits where T is 0"""
-    t = torch.where(temperature > 0, temperature, torch.ones_like(temperature))[:, None]
-    race = torch.softmax(logits / t, -1) / noise
-    return torch.where((temperature > 0)[:, None], race, logits).argmax(-1).to(torch.int32)
+    """A token per row: argmax of softmax(logits / T) / noise over the tokens of a probability above 0, or of the logits where T is 0 (or
+    no number above it).  The probabilities are those that verify_drafts takes a draft to be sampled from: NaN logits count as -inf,
+    +inf as the largest finite value, 1 / T stays within fp32's range, and T = +inf leaves logits above -inf alike."""
+    f = torch.finfo(torch.float32)
+    z = torch.where(logits.isnan(), torch.full_like(logits, -math.inf), logits).clamp(max=f.max)
+    top = z.amax(-1, keepdim=True)
+    t = torch.where(temperature > 0, temperature, torch.ones_like(temperature))
+    inv = (1.0 / t).clamp(f.tiny * f.eps, f.max)[:, None]
+    w = torch.exp((z - torch.where(top.isinf(), torch.zeros_like(top), top)) * inv)
+    race = torch.where(w > 0, w / w.sum(-1, keepdim=True) / noise, torch.full_like(w, -1.0))
+    return torch.where((temperature > 0)[:, None], race, z).argmax(-1).to(torch.int32)
 
 
 def draft_and_verify(drafter, block_table, seq_lens, tokens, drafts, temperature, generator):
