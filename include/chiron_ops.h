@@ -148,9 +148,9 @@ int32_t chiron_linear4_create(const void *w4, const void *scales, const void *ze
                               void *stream, chiron_linear4 **out);
 int32_t chiron_linear4_destroy(chiron_linear4 *l);
 
-/* y[M,N] = x[M,K] * W^T, or y += (accumulate != 0).  x, y dev fp32 row-major, not overlapping.  Per row and 128 inputs, x
- * enters with an error of at most 2^-23 of its largest value, or 2^-128: few rows as whole multiples of a power of
- * two in three 8-bit digits, many rows as two fp16 terms.  Sums over the groups are fp32.  A NaN or an infinity in a
+/* y[M,N] = x[M,K] * W^T, or y += (accumulate != 0).  x, y dev fp32 row-major, not overlapping.  An element of x enters with an
+ * error of at most 2^-22 of itself and 2^-30.9 of the largest of its row's 128 inputs (or 2^-128): few rows as whole multiples of a
+ * power of two in four 8-bit digits, many rows as two fp16 terms.  Sums over the groups are fp32.  A NaN or an infinity in a
  * row of x makes that row of y NaN.  M <= 65535. */
 int32_t chiron_op_linear4(const chiron_linear4 *l, const float *x, int32_t M, float *y, int32_t accumulate, void *workspace,
                           void *stream);

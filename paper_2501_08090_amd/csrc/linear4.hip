@@ -1,12 +1,15 @@
 // Products of few rows with 4-bit weights: y = x W^T, W[n][k] = (w4 - z) * scale, a scale and a zero point for each row and group of
 // 32, 64 or 128 inputs.  gfx950, wave64.
 //
-// x enters, per row and 128 inputs, with 22 to 23 bits of its largest value, on two ways:
-//  - few rows (passes of up to 16), where bringing x to the matrix cores costs most, as whole multiples of a power of two, |x| < 2^23,
-//    in three signed 8-bit digits: a group's digit sums are exact, and are scaled and added over the groups in fp32.  A weight without zero points is
+// x enters on two ways, of which neither loses what is small beside something large:
+//  - few rows (passes of up to 16), where bringing x to the matrix cores costs most, per row and 128 inputs as whole multiples of a power of
+//    two, |x| < 2^31, in four signed 8-bit digits: 31 bits of the largest value, so that an input of fp32's own 24 bits loses none of them
+//    until it is 2^-7 of that, and one of 2^-10 of it keeps 21.  (Three digits left 13 of those, and did not use the last quarter of the matrix
+//    operands' columns.)  A group's digit sums are exact, and are scaled and added over the groups in fp32.  A weight without zero points is
 //    16 * (w4 - 8), which is its four bits, the highest inverted when the matrix is laid out, in the upper half of a byte: three
 //    instructions for eight weights.  With zero points it is w4 - z: eight bytes, seven instructions.
-//  - many rows as two fp16 terms, whose products with w4 - z, exact in fp16, meet in one fp32 sum.
+//  - many rows as two fp16 terms (off by 2^-22 of an input and 2^-39 of the largest of its 128), whose products with w4 - z, exact in fp16,
+//    meet in one fp32 sum.
 // (Scales multiply sums, not weights: w4 - z times a bf16 scale has 12 bits, one more than fp16.)
 //
 // Layout: tiles of 16 rows of W and 128 of K, 1 KiB each, a tile's blocks one behind the other: lane l holds row l % 16 and 32 values
@@ -139,24 +142,24 @@ __device__ __forceinline__ intx4 group_product(const intx4 (&a)[2], const intx4 
     }
     return p;
 }
-// three digits' sums as one value; the lower two stay below 2^30 (128 products of at most 128 * 128 each)
-__device__ __forceinline__ float join_digits(int p2, int p1, int p0) { return fmaf((float)p2, 65536.f, (float)((p1 << 8) + p0)); }
+// four digits' sums as one value; two of them stay below 2^30 (128 products of at most 128 * 128 each)
+__device__ __forceinline__ float join_digits(int p3, int p2, int p1, int p0) { return fmaf((float)((p3 << 8) + p2), 65536.f, (float)((p1 << 8) + p0)); }
 
-// A block's power of two from the bits of its largest magnitude: x * 2^up is below 0.9922 * 2^23, where three signed digits end a little
-// higher.  (Below 2^-104 the digits stop at 2^-127.)
+// A block's power of two from the bits of its largest magnitude: x * 2^up is below 0.9922 * 2^31, where four signed digits end a little
+// higher.  (Below 2^-96 the digits stop at 2^-127.)
 __device__ __forceinline__ int exponent_up(uint32_t top) {
-    return min(127, 23 - __builtin_amdgcn_frexp_expf(__uint_as_float(top)) - ((top & 0x7fffffu) >= 0x7e0000u));
+    return min(127, 31 - __builtin_amdgcn_frexp_expf(__uint_as_float(top)) - ((top & 0x7fffffu) >= 0x7e0000u));
 }
 // what the lowest digit counts; without zero points weights are 16 times themselves.  Infinity or NaN in the block: NaN
 template <bool ZERO>
 __device__ __forceinline__ float block_scale(uint32_t top) {
     return top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : ldexpf(1.f, -exponent_up(top) - (ZERO ? 0 : 4));
 }
-// 8 consecutive values of a row as signed 8-bit digits q = 65536 d2 + 256 d1 + d0, highest first, of x * 2^up rounded to a whole number
-// (to nearest, ties to even); 0x8080 more carries into the next digit where one is above 127 and leaves d0 and d1 in their bytes with
-// the highest bit inverted.
+// 8 consecutive values of a row as signed 8-bit digits q = 2^24 d3 + 2^16 d2 + 2^8 d1 + d0, highest first, of x * 2^up rounded to a whole
+// number (to nearest, ties to even); 0x808080 more carries into the next digit where one is above 127 and leaves the lower three in their
+// bytes with the highest bit inverted.
 struct Run {
-    uint2 digit[3];
+    uint2 digit[4];
 };
 __device__ __forceinline__ Run digits_of(const float (&v)[8], uint32_t top) {
     const float up = top >= 0x7f800000u ? 0.f : ldexpf(1.f, exponent_up(top));
@@ -165,16 +168,13 @@ __device__ __forceinline__ Run digits_of(const float (&v)[8], uint32_t top) {
     for (int h = 0; h < 2; ++h) {
         uint32_t q[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = (uint32_t)(int)rintf(v[4 * h + i] * up) + 0x8080u;
+        for (int i = 0; i < 4; ++i) q[i] = (uint32_t)(int)rintf(v[4 * h + i] * up) + 0x808080u;
         const uint32_t a = __builtin_amdgcn_perm(q[1], q[0], 0x05010400u), b = __builtin_amdgcn_perm(q[3], q[2], 0x05010400u);  // d0 d0 d1 d1
-        const uint32_t c = __builtin_amdgcn_perm(q[1], q[0], 0x0c0c0602u), d = __builtin_amdgcn_perm(q[3], q[2], 0x0c0c0602u);  // d2 d2
-        const uint32_t d0 = __builtin_amdgcn_perm(b, a, 0x05040100u) ^ 0x80808080u, d1 = __builtin_amdgcn_perm(b, a, 0x07060302u) ^ 0x80808080u;
-        const uint32_t d2 = __builtin_amdgcn_perm(d, c, 0x05040100u);
-        if (h == 0) {
-            r.digit[0].x = d2; r.digit[1].x = d1; r.digit[2].x = d0;
-        } else {
-            r.digit[0].y = d2; r.digit[1].y = d1; r.digit[2].y = d0;
-        }
+        const uint32_t c = __builtin_amdgcn_perm(q[1], q[0], 0x07030602u), d = __builtin_amdgcn_perm(q[3], q[2], 0x07030602u);  // d2 d2 d3 d3
+        const uint32_t digit[4] = {__builtin_amdgcn_perm(d, c, 0x07060302u), __builtin_amdgcn_perm(d, c, 0x05040100u) ^ 0x80808080u,
+                                   __builtin_amdgcn_perm(b, a, 0x07060302u) ^ 0x80808080u, __builtin_amdgcn_perm(b, a, 0x05040100u) ^ 0x80808080u};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) (h == 0 ? r.digit[t].x : r.digit[t].y) = digit[t];
     }
     return r;
 }
@@ -203,8 +203,8 @@ __device__ __forceinline__ uint32_t block_top(const float (&v)[8]) {
 
 // ---- few rows --------------------------------------------------------------------------------------------------
 // A workgroup converts its slice of x to digits once, in LDS, and then walks tiles of 16 columns; its 8 waves own NB blocks of K each,
-// whose x stays in registers, and add their sums through LDS.  With up to 4 rows the three digits of a row take different columns of
-// one operand (column = 4 * digit + row), with up to 8 two operands (8 * digit + row), else three.  A slice of more than 8 NB blocks
+// whose x stays in registers, and add their sums through LDS.  With up to 4 rows the four digits of a row take different columns of
+// one operand (column = 4 * digit + row), with up to 8 those of two operands (8 * (digit % 2) + row), else four.  A slice of more than 8 NB blocks
 // goes in chunks, whose sums wait in LDS (for kFewTiles tiles at most): adding them up in y would put a load behind the weights on their
 // way, and what it waits for would be all of them.  The loops hold no branch that depends on a wave: blocks behind the slice's end
 // read the last one again and count with 0.  8 rows through 28672 x 4096: 17 us, 3.6 TB/s; one through 4096 x 4096: 5.
@@ -218,9 +218,9 @@ __device__ __forceinline__ int few_slot(int k64, int g, int c) { return g * 16 +
 template <int GROUP, bool ZERO, int SETS, int NB, bool ONE>
 __global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const float* __restrict__ x, int rows, int pass_rows, int slice_blocks, float* __restrict__ y,
                                                              int accumulate) {
-    constexpr int PER = 128 / GROUP, ROWS = SETS == 1 ? 4 : SETS == 2 ? 8 : 16;
+    constexpr int PER = 128 / GROUP, ROWS = 4 * SETS;
     // tiles on their way: as many as the registers hold beside x
-    constexpr int RING = ONE ? 1 : NB == 4 ? (GROUP == 32 || SETS == 2 ? 2 : 3) : NB == 2 ? (SETS == 3 ? (GROUP == 32 ? 1 : 3) : GROUP == 32 ? 3 : 4) : 6;
+    constexpr int RING = ONE ? 1 : NB == 4 ? (GROUP == 32 || SETS == 2 ? 2 : 3) : NB == 2 ? (SETS == 4 ? (GROUP == 32 ? 1 : 3) : GROUP == 32 ? 3 : 4) : 6;
     __shared__ uint4 s_dig[NB * 8 * 2 * SETS * 64];
     __shared__ float s_base[NB * 8][ROWS];
     __shared__ __align__(16) float s_red[2][8][256];
@@ -233,12 +233,12 @@ __global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const fl
     const int m0 = blockIdx.z * pass_rows, M = min(pass_rows, rows - m0);  // this pass's rows
     x += (int64_t)m0 * l.K;
     y += ((int64_t)blockIdx.y * rows + m0) * l.N;
-    // what digit a column holds in each set: weight 2^(16 - 8 digit), none behind the third
+    // what digit a column holds in each set: weight 2^(24 - 8 digit)
     float f[SETS];
 #pragma unroll
     for (int s = 0; s < SETS; ++s) {
         const int d = s * (16 / ROWS) + col / ROWS;
-        f[s] = d == 0 ? 65536.f : d == 1 ? 256.f : d == 2 ? 1.f : 0.f;
+        f[s] = d == 0 ? 16777216.f : d == 1 ? 65536.f : d == 2 ? 256.f : 1.f;
     }
     const int step = gridDim.x, home = blockIdx.x;
     int buf = 0;
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const fl
                 const uint32_t top = block_top(v[i]);
                 const Run d = digits_of(v[i], top);
 #pragma unroll
-                for (int t = 0; t < 3; ++t) {
+                for (int t = 0; t < 4; ++t) {
                     const int set = t / (16 / ROWS), c = t % (16 / ROWS) * ROWS + m;
                     reinterpret_cast<uint2*>(&s_dig[(k64 * SETS + set) * 64 + few_slot(k64, g, c)])[half] = d.digit[t];
                 }
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const fl
             }
         }
         lds_barrier();
-        intx4 xf[NB][SETS][2];  // (columns of no row or digit hold anything: whole numbers that nobody reads)
+        intx4 xf[NB][SETS][2];  // (columns of no row hold anything: whole numbers that nobody reads)
         float base[NB];
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const fl
                         float v;
                         if constexpr (SETS == 1) v = (float)p[0][r];
                         else if constexpr (SETS == 2) v = fmaf((float)p[0][r], f[0], (float)p[1][r] * f[1]);
-                        else v = join_digits(p[0][r], p[1][r], p[2][r]);
+                        else v = join_digits(p[0][r], p[1][r], p[2][r], p[3][r]);
                         sum[r] = u == 0 ? v * sc[j][i].get(r, u) : fmaf(v, sc[j][i].get(r, u), sum[r]);
                     }
                 }
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const fl
                 for (int w = 0; w < 8; ++w) {
                     v += s_red[buf][w][out_m * 16 + out_row];
                     if (SETS <= 2) v += s_red[buf][w][(out_m + ROWS) * 16 + out_row];
-                    if (SETS <= 1) v += s_red[buf][w][(out_m + 2 * ROWS) * 16 + out_row];
+                    if (SETS <= 1) v += s_red[buf][w][(out_m + 2 * ROWS) * 16 + out_row] + s_red[buf][w][(out_m + 3 * ROWS) * 16 + out_row];
                 }
                 if (k1 - k0 > NB * 8) {  // several chunks: kFewTiles tiles a workgroup at most
                     float& sum = s_acc[(t - home) / step][threadIdx.x];
@@ -697,23 +697,24 @@ struct Plan4 {
 static Plan4 plan_linear4(const Linear4& l, int64_t M) {
     Plan4 p;
     const int64_t kb = l.Kpad / 128;
-    // More than 16 rows by passes of up to 16 too, as long as all passes' weights stay within 2^27 (2^26 * 1.25 with smaller groups): one
-    // launch, or two, for the tiles' three, but every pass unpacks the weights again.  us passes / tiles, groups of 128: 64 rows through
-    // 600 x 1024 5.2 / 13.2, 4096 x 4096 16.4 / 23, 8192 x 4096 (2^27) 22.9 / 26, 14336 x 4096 32 / 30; 32 rows through 4096 x 14336
-    // (1.75 * 2^26) 23.4 / 21.7, 14336 x 4096 21.3 / 22.1; groups of 64: 64 rows through 4096 x 4096 (2^26) 19.3 / 23.8, 48 through 8192
-    // x 4096 (1.5 * 2^26) 24.9 / 23.2.
-    const int64_t passes = (M + 15) / 16, limit = (l.group == 128 ? 8 : 5) * ((int64_t)1 << 24);
+    // More than 16 rows by passes of up to 16 too, as long as all passes' weights stay within 2^27, 1.25 * 2^26 or 0.75 * 2^26 (groups of 128, 64
+    // or 32): one launch, or two, for the tiles' three, but every pass unpacks the weights again, and the smaller the groups, the more of
+    // the time goes by results and groups.  us passes / tiles, groups of 128: 64 rows through 4096 x 4096 15.7 / 23.3, 8192 x 4096 (2^27) 22.9 /
+    // 26.8, 14336 x 4096 32.7 / 29.6; 32 rows through 4096 x 14336 (1.75 * 2^26) 23.1 / 21.7, 14336 x 4096 21.3 / 21.1; groups of 64 with zero
+    // points: 64 rows through 4096 x 4096 (2^26) 19.0 / 24.0, 48 through 5120 x 5120 (1.17 * 2^26) 28.3 / 22.7 and 8192 x 4096 (1.5 * 2^26) 25.3 / 23.8;
+    // groups of 32: 64 rows through 2048 x 4096 (2^25) 17.0 / 21.9 and 4096 x 4096 (2^26) 22.9 / 25.0, 32 through 8192 x 4096 (2^26) 23.2 / 20.6.
+    const int64_t passes = (M + 15) / 16, limit = (l.group == 128 ? 8 : l.group == 64 ? 5 : 3) * ((int64_t)1 << 24);
     if (passes == 1 || passes * l.N * kb * 128 <= limit) {
         p.passes = (int)passes;
         p.pass_rows = (int)((M + p.passes - 1) / p.passes);
-        p.sets = p.pass_rows <= 4 ? 1 : p.pass_rows <= 8 ? 2 : 3;
-        const int64_t most = p.sets == 3 || (p.sets == 2 && l.group == 32) ? 2 : 4;  // what LDS and registers hold
+        p.sets = p.pass_rows <= 4 ? 1 : p.pass_rows <= 8 ? 2 : 4;
+        const int64_t most = p.sets == 4 || (p.sets == 2 && l.group == 32) ? 2 : 4;  // what LDS and registers hold
         const int64_t tiles = ((int64_t)l.N + 15) / 16, all = tiles * p.passes;
         // Slices of at most 32 blocks up to 4 rows, of 16 with more, whose x takes a workgroup longer than a second launch and the slices'
         // traffic; 32 too with up to 8 rows where that is all of K and there are tiles for every CU; and of 8, where the chip is not full
-        // otherwise.  us with 1 / 2 / 4 / 8 / 16 slices: 1 row through 8192 x 28672 44 / 35 / 29 / 25 / 36, 8 rows through 8192 x 8192
-        // 19 / 16 / 13.6 / 15.6 / 25 and through 28672 x 4096 17.7 / 18.5 / 23 / 38 / 65, 16 rows through 1024 x 4096 12.2 / 9.6 / 7 /
-        // 8.6 / 10.2.
+        // otherwise.  us with 1 / 2 / 4 / 8 / 16 slices: 1 row through 8192 x 28672 41 / 35 / 29 / 25 / 29, 8 rows through 8192 x 8192
+        // 19 / 16 / 13.5 / 15.6 / 25 and through 28672 x 4096 16.8 / 17.5 / 23 / 38 / 67, 16 rows through 1024 x 4096 11.7 / 9.3 / 6.9 /
+        // 8.5 / 10.1.
         const bool whole = p.sets == 1 || (p.sets == 2 && kb <= 32 && all >= kNumCU);
         static_assert(kNumCU % 16 == 0, "a slice's share of the CUs is a whole number");
         while (p.slices < 16 && (kb + p.slices - 1) / p.slices > (whole ? 32 : 16)) p.slices *= 2;
@@ -766,8 +767,8 @@ static void launch_linear4(const Linear4& l, const float* x, int M, float* y, in
             else if (p.nb == 2 || GROUP == 32) CHIRON_FEW(2, 2);
             else if constexpr (GROUP != 32) CHIRON_FEW(2, 4);
         } else {
-            if (p.nb == 1) CHIRON_FEW(3, 1);
-            else CHIRON_FEW(3, 2);
+            if (p.nb == 1) CHIRON_FEW(4, 1);
+            else CHIRON_FEW(4, 2);
         }
 #undef CHIRON_FEW
         return;

@@ -63,3 +63,64 @@ def test_verify_temperature_without_end(with_draft):
                                      1.0 if t > 1e38 else t)
         assert (abs(prob[i] - pr) <= 2.0 ** -16 * pr).all(), (i, prob[i], pr)
         assert near or (took[i] == a and out[i].tolist() == want), (i, out[i], want)
+
+
+def beside_large_ones(M, N, K, group, zeros, large, small, seed):
+    """weights and x: one input of every 128 is `large` and meets weights of 0, the others are `small`"""
+    w4, s, z = T.weights(N, K, group, zeros, seed)
+    at = torch.arange(5, K, 128)
+    zp = z[:, at // group] if zeros else torch.full((N, len(at)), 8, dtype=torch.uint8)
+    w4[:, at // 2] = (w4[:, at // 2] & 15) | zp << 4
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((M, K), generator=g) * small
+    x[:, at] = large * (1 + torch.rand((M, len(at)), generator=g)) * torch.where(torch.rand((M, len(at)), generator=g) < 0.5, -1, 1)
+    return w4, s, z, x
+
+
+@pytest.mark.parametrize("M,N,K", ((1, 200, 1024), (4, 200, 1024), (8, 200, 1024), (16, 200, 1024), (33, 200, 1024), (64, 4001, 8576)))
+@pytest.mark.parametrize("group,zeros", ((128, False), (64, True), (32, False)))
+@pytest.mark.parametrize("large,small", ((1e3, 1.0), (1e3, 2.0 ** -16), (1e5, 1.0)))
+def test_linear4_small_inputs_beside_large_ones(M, N, K, group, zeros, large, small):
+    """tolerance: x off by 2^-22 of itself and 2^-30.9 of the largest of its 128, for each product, and fp32 sums over the groups, of
+    which an input's four digits can be twice its size"""
+    w4, s, z, x = beside_large_ones(M, N, K, group, zeros, large, small, 71)
+    lin = B.Linear4(w4.cuda(), s.cuda(), None if z is None else z.cuda())
+    print("linear4", N, K, "group", group, "rows", M, "beside", large, small, flush=True)
+    pick = np.r_[0:40, N - 40:N]
+    w, _ = D.weights4(w4[pick], s[pick], None if z is None else z[pick], group)
+    got = lin(x.cuda())[:, pick].double().cpu().numpy()
+    xd = x.double().numpy()
+    top = np.abs(xd).reshape(M, K // 128, 128).max(2).repeat(128, 1)
+    off = 2.0 ** -22 * abs(xd) + 2.0 ** -30.9 * top
+    parts = abs(xd) @ abs(w).T
+    tol = off @ abs(w).T + 2 * (K // group + 6) * 2.0 ** -24 * parts
+    err = abs(got - xd @ w.T)
+    assert (err <= tol).all(), (err / tol).max()
+    # and with all of the error in one direction: no input may be lost beside the large one
+    if small == 1.0:
+        x[:, torch.arange(K) % 128 != 5] = 0.75 * 2.0 ** -14
+        ones = torch.full_like(w4, 0x99)
+        ones[:, torch.arange(5, K, 128) // 2] = 0x89
+        lin = B.Linear4(ones.cuda(), torch.ones_like(s).cuda())
+        want = 0.75 * 2.0 ** -14 * (K - K // 128)
+        tol = 2.0 ** -30.9 * 2 * large * K + 2.0 ** -21 * want
+        assert abs(lin(x.cuda()).double().cpu().numpy() - want).max() <= tol
+
+
+@pytest.mark.parametrize("M", (1, 3, 7, 16))
+@pytest.mark.parametrize("zeros", (False, True))
+@pytest.mark.parametrize("large", (1.98437, 1.98438, -1.98437, -1.98438, 1.0, 1.9999999))
+def test_linear4_hands_x_through(M, zeros, large):
+    """a matrix that hands x through: off by 2^-30.9 of the largest of the 128, and two roundings of digits up to twice x"""
+    w4 = torch.full((128, 64), 0x88, dtype=torch.uint8)
+    for n in range(128):
+        w4[n, n // 2] = 0x98 if n % 2 else 0x89
+    s = torch.ones((128, 1), dtype=torch.bfloat16)
+    lin = B.Linear4(w4.cuda(), s.cuda(), torch.full((128, 1), 8, dtype=torch.uint8, device="cuda") if zeros else None)
+    g = torch.Generator().manual_seed(M)
+    x = (torch.rand((M, 128), generator=g) * 2 - 1) * 2.0 ** torch.randint(-12, 0, (M, 128), generator=g)
+    x[:, 77] = large
+    x[:, 78] = -large
+    got = lin(x.cuda()).double().cpu()
+    err = (got - x.double()).abs()
+    assert (err <= 2.0 ** -30.9 * abs(large) + 2.0 ** -22 * x.double().abs()).all(), err.max()
