@@ -139,7 +139,8 @@ int32_t chiron_op_verify_drafts(const chiron_draft_batch *in /* host */, int32_t
 
 /* ---- products with 4-bit weights ------------------------------------------------------------------------------
  *
- * W[n][k] = (w4[n][k] - z[n][k/group]) * scale[n][k/group], w4 in 0 .. 15, z in 0 .. 15 (null: 8 everywhere).
+ * W[n][k] = (w4[n][k] - z[n][k/group]) * scale[n][k/group], w4 in 0 .. 15, z in 0 .. 64 (null: 8 everywhere; one above 64 is an
+ * invalid argument, and with zero points the call waits for the stream to find out).
  *   w4      dev uint8 [N, K/2]: k even in the low four bits, k odd in the high four
  *   scales  dev bf16 [N, K/group];  zeros dev uint8 [N, K/group] or null
  * group 32, 64 or 128, K a multiple of group below 2^23, any N >= 1.  The library keeps its own repacked copy. */

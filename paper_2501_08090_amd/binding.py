@@ -641,7 +641,7 @@ def verify_drafts(logits, tokens, uniforms, noise, draft_logits=None, draft_lens
 
 class Linear4:
     """A matrix of 4-bit weights: W[n][k] = (w4[n][k] - zero[n][k // group]) * scale[n][k // group].  w4 uint8 [N, K/2] (even k in the
-    low bits), scales bf16 [N, K/group], zeros uint8 [N, K/group] or None (8); group 32, 64 or 128."""
+    low bits), scales bf16 [N, K/group], zeros uint8 [N, K/group], 0 .. 64, or None (8); group 32, 64 or 128."""
 
     def __init__(self, w4, scales, zeros=None):
         self.N, self.K = w4.shape[0], 2 * w4.shape[1]

@@ -64,7 +64,10 @@ __global__ __launch_bounds__(256) void pack4_kernel(const uint8_t* __restrict__ 
     *reinterpret_cast<uint4*>(l.w + j * 16) = make_uint4(out[0], out[1], out[2], out[3]);
 }
 
-__global__ __launch_bounds__(256) void pack4_scales_kernel(const uint16_t* __restrict__ scales, const uint8_t* __restrict__ zeros, Linear4 l) {
+// Zero points up to 64: w4 - z is exact in all that the kernels make of it (64 + z is a whole number of fp16's steps up to there).
+// too_large: set where one is larger.
+constexpr int kMaxZero = 64;
+__global__ __launch_bounds__(256) void pack4_scales_kernel(const uint16_t* __restrict__ scales, const uint8_t* __restrict__ zeros, Linear4 l, uint32_t* too_large) {
     const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;  // (tile, block, row, group of the block)
     const int per = 128 / l.group, kb = l.Kpad / 128, live = l.K / l.group;
     const int64_t tb = j / (16 * per), tile = tb / kb;
@@ -74,7 +77,11 @@ __global__ __launch_bounds__(256) void pack4_scales_kernel(const uint16_t* __res
     const int g = (int)(tb % kb) * per + w % per;
     const bool there = n < l.N && g < live;
     l.scale[j] = there ? scales[n * live + g] : 0;
-    if (l.zero) l.zero[j] = there ? (uint8_t)(128 - (zeros[n * live + g] & 15)) : 128;
+    if (l.zero) {
+        const int z = there ? zeros[n * live + g] : 0;
+        l.zero[j] = (uint8_t)(128 - min(z, kMaxZero));
+        if (z > kMaxZero) *too_large = 1;
+    }
 }
 
 // ---- pieces that the kernels share -----------------------------------------------------------------------------
@@ -819,13 +826,19 @@ int32_t chiron_linear4_create(const void* w4, const void* scales, const void* ze
     const int64_t ns = tiles * 16 * (L.Kpad / group);
     int32_t rc = dev_alloc((void**)&L.w, (size_t)(tiles * kb * 1024));
     if (!rc) rc = dev_alloc((void**)&L.scale, (size_t)ns * 2);
-    if (!rc && zeros) rc = dev_alloc((void**)&L.zero, (size_t)ns);
+    if (!rc && zeros) rc = dev_alloc((void**)&L.zero, (size_t)ns + 4);  // behind them a word: one is too large
     if (!rc) {
         hipStream_t st = (hipStream_t)stream;
+        uint32_t* flag = zeros ? (uint32_t*)(L.zero + ns) : nullptr;
+        uint32_t too_large = 0;
+        hipError_t e = zeros ? hipMemsetAsync(flag, 0, 4, st) : hipSuccess;
         launch(pack4_kernel, dim3((unsigned)((tiles * kb * 64 + 255) / 256)), dim3(256), st, (const uint8_t*)w4, L);
-        launch(pack4_scales_kernel, dim3((unsigned)((ns + 255) / 256)), dim3(256), st, (const uint16_t*)scales, (const uint8_t*)zeros, L);
-        const hipError_t e = hipGetLastError();
+        launch(pack4_scales_kernel, dim3((unsigned)((ns + 255) / 256)), dim3(256), st, (const uint16_t*)scales, (const uint8_t*)zeros, L, flag);
+        if (e == hipSuccess) e = hipGetLastError();
+        if (e == hipSuccess && zeros) e = hipMemcpyAsync(&too_large, flag, 4, hipMemcpyDeviceToHost, st);
+        if (e == hipSuccess && zeros) e = hipStreamSynchronize(st);
         if (e != hipSuccess) rc = fail(CHIRON_ERR_HIP, "linear4: %s", hipGetErrorString(e));
+        else if (too_large) rc = fail(CHIRON_ERR_INVALID_ARG, "linear4: a zero point is above %d", kMaxZero);
     }
     if (rc) {
         chiron_linear4_destroy(l);

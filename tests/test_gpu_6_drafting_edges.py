@@ -124,3 +124,27 @@ def test_linear4_hands_x_through(M, zeros, large):
     got = lin(x.cuda()).double().cpu()
     err = (got - x.double()).abs()
     assert (err <= 2.0 ** -30.9 * abs(large) + 2.0 ** -22 * x.double().abs()).all(), err.max()
+
+
+@pytest.mark.parametrize("M,N,K,group", ((1, 40, 256, 128), (6, 40, 256, 64), (16, 40, 256, 32), (40, 75, 640, 32), (64, 4001, 8448, 128), (64, 2507, 8480, 32)))
+def test_linear4_zero_points_up_to_64(M, N, K, group):
+    """formats that store the zero point less one reach 16"""
+    w4, s, z = T.weights(N, K, group, True, 81)
+    z[:, ::2] = 16
+    z[::3, 1::2] = torch.randint(0, 65, z[::3, 1::2].shape, generator=torch.Generator().manual_seed(1), dtype=torch.uint8)
+    z[0] = 64
+    pick = np.r_[0:20, N - 20:N]
+    w, sk = D.weights4(w4[pick], s[pick], z[pick], group)
+    lin = B.Linear4(w4.cuda(), s.cuda(), z.cuda())
+    T.check_linear4(T.some_columns(lin, pick), w, sk, torch.randn((M, K), generator=torch.Generator().manual_seed(2)), group)
+
+
+@pytest.mark.parametrize("where", ((0, 0), (39, 1), (17, 0)))
+def test_linear4_refuses_larger_zero_points(where):
+    w4, s, z = T.weights(40, 256, 128, True, 82)
+    z[where] = 65
+    with pytest.raises(B.ChironError) as e:
+        B.Linear4(w4.cuda(), s.cuda(), z.cuda())
+    assert e.value.code == -1 and "zero point" in str(e.value)
+    z[where] = 64
+    B.Linear4(w4.cuda(), s.cuda(), z.cuda())
