@@ -104,7 +104,9 @@ int32_t chiron_op_select_pages(chiron_model *m, const chiron_kvpool *p, const ch
 int32_t chiron_op_sparse_attention(chiron_model *m, const chiron_kvpool *p, int32_t layer, const float *q,
                                    const int32_t *block_table, const int32_t *row_seq, const int32_t *ctx_lens, int32_t rows,
                                    const int32_t *pages, const int32_t *counts, int32_t top, float *out, void *stream);
-/* Both use the model's attention workspace (rows <= max_batch; calls on one model must not overlap). */
+/* Both use the model's attention workspace (rows <= max_batch; calls on one model must not overlap).  Tables of more than
+ * (8192 + 2 max_batch) * G * head_dim columns, 8 million tokens at the least, have no room in it for one row's scores: the selection
+ * refuses them. */
 
 /* ---- verification of drafted tokens ---------------------------------------------------------------------------
  *

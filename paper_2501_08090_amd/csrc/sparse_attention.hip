@@ -23,7 +23,7 @@ struct SelectArgs {
     const int32_t *bt, *row_seq, *ctx_lens;
     float* scores;  // [rows][n_kv][max_blocks]
     int32_t *pages, *counts;
-    int layer, max_blocks, rows, top, n_first, n_last;
+    int layer, max_blocks, top, n_first, n_last;
 };
 
 constexpr float kTop = 3.4028234663852886e38f;
@@ -625,7 +625,7 @@ int32_t chiron_op_select_pages(chiron_model* m, const chiron_kvpool* p, const ch
     if (lists > 0x7fffffff) return fail(CHIRON_ERR_BATCH_TOO_LARGE, "select: %lld lists are too many", (long long)lists);
     SelectArgs a;
     a.pool = p->d; a.index = x->d; a.q = q; a.bt = block_table; a.row_seq = row_seq; a.ctx_lens = ctx_lens; a.scores = m->aws.part_o;
-    a.pages = pages; a.counts = counts; a.layer = layer; a.max_blocks = mb; a.rows = rows; a.top = top; a.n_first = n_first; a.n_last = n_last;
+    a.pages = pages; a.counts = counts; a.layer = layer; a.max_blocks = mb; a.top = top; a.n_first = n_first; a.n_last = n_last;
     hipStream_t st = (hipStream_t)stream;
     const int d = p->d.d;
     // us of a CU for a whole list's records at 45 B/ns, against some 5 us for the second launch
@@ -637,18 +637,27 @@ int32_t chiron_op_select_pages(chiron_model* m, const chiron_kvpool* p, const ch
         else CHIRON_BY_HEADS(CHIRON_SELECT, 64)
 #undef CHIRON_SELECT
     } else {
-        // the scores lie in the attention workspace
-        if (lists * mb > (int64_t)m->aws.cap_items * m->cfg.n_q_heads * d)
-            return fail(CHIRON_ERR_BATCH_TOO_LARGE, "select: scores of %d rows x %d heads x %d pages exceed the model's workspace", rows, n_kv, mb);
-        const int chunks = (int)std::min<int64_t>((mb + 255) / 256, std::max<int64_t>(1, 4 * kNumCU / lists));
-        const dim3 grid((unsigned)lists, chunks);
-        if (mb > top) {
+        // The scores lie in the attention workspace: as many rows at once as it holds, one range behind the other on the stream.
+        const int64_t at_once = (int64_t)m->aws.cap_items * m->cfg.n_q_heads * d / ((int64_t)n_kv * mb);
+        if (at_once < 1) return fail(CHIRON_ERR_SHAPE, "select: scores of %d heads x %d pages exceed the model's workspace", n_kv, mb);
+        for (int64_t r0 = 0; r0 < rows; r0 += at_once) {
+            const int64_t n = std::min<int64_t>(at_once, rows - r0), part = n * n_kv;
+            a.q = q + r0 * m->cfg.n_q_heads * d;
+            a.ctx_lens = ctx_lens + r0;
+            a.row_seq = row_seq ? row_seq + r0 : nullptr;
+            a.bt = row_seq ? block_table : block_table + r0 * mb;
+            a.pages = pages + r0 * n_kv * top;
+            a.counts = counts ? counts + r0 : nullptr;
+            const int chunks = (int)std::min<int64_t>((mb + 255) / 256, std::max<int64_t>(1, 4 * kNumCU / part));
+            const dim3 grid((unsigned)part, chunks);
+            if (mb > top) {
 #define CHIRON_SCORES(D_, G_) launch(page_scores_kernel<D_, G_>, grid, dim3(256), st, a)
-            if (d == 128) CHIRON_BY_HEADS(CHIRON_SCORES, 128)
-            else CHIRON_BY_HEADS(CHIRON_SCORES, 64)
+                if (d == 128) CHIRON_BY_HEADS(CHIRON_SCORES, 128)
+                else CHIRON_BY_HEADS(CHIRON_SCORES, 64)
 #undef CHIRON_SCORES
+            }
+            launch(select_scored_kernel, dim3((unsigned)part), dim3(kSelectThreads), st, a);
         }
-        launch(select_scored_kernel, dim3((unsigned)lists), dim3(kSelectThreads), st, a);
     }
     CHIRON_HIP(hipGetLastError());
     return CHIRON_OK;

@@ -148,3 +148,18 @@ def test_linear4_refuses_larger_zero_points(where):
     assert e.value.code == -1 and "zero point" in str(e.value)
     z[where] = 64
     B.Linear4(w4.cuda(), s.cuda(), z.cuda())
+
+
+@pytest.mark.parametrize("heads,rows,cols", (((1, 1, 64), 64, 16384), ((2, 2, 64), 40, 30000), ((4, 1, 128), 63, 120001)))
+@pytest.mark.parametrize("pass_seq", (True, False))
+def test_select_pages_of_tables_wider_than_the_workspace(heads, rows, cols, pass_seq):
+    """rows x KV heads x columns beyond what the model's workspace holds of scores at once"""
+    lens = [(r * 97) % 700 if r % 9 else 0 for r in range(rows)]
+    lens[rows // 2], lens[-1] = 9000, 5001
+    c, bt = T.filled(*heads, lens, 91, cols=cols)
+    assert rows * heads[1] * cols > (8192 + 2 * 64) * heads[0] * heads[2]
+    q = torch.randn((rows, heads[0] * heads[2]), generator=torch.Generator().manual_seed(1)).cuda()
+    seq = list(range(rows))
+    if pass_seq:
+        seq = [(r * 7 + 3) % rows for r in seq]
+    T.check_select(c, bt, q, [lens[s] for s in seq], seq, 33, 1, 1, pass_seq=pass_seq)
