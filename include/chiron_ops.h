@@ -128,7 +128,7 @@ int32_t chiron_op_sparse_attention(chiron_model *m, const chiron_kvpool *p, int3
  *   tokens        dev int32 [batch, max_draft];  uniforms dev fp32 [batch, max_draft];  noise dev fp32 [batch][vocab] (contiguous)
  *   out_tokens    dev int32 [batch, max_draft+1];  accepted dev int32 [batch];  prob dev fp32 [batch, max_draft] (optional)
  *   workspace     dev, chiron_verify_workspace_bytes() bytes, 16-byte aligned, caller-owned, in use until the stream has passed
- * 0 <= max_draft <= 127. */
+ * 0 <= max_draft <= 127; batch * (2 max_draft + 1) <= 65535, with draft_logits or without (more requests: several calls). */
 int64_t chiron_verify_workspace_bytes(int32_t batch, int32_t max_draft, int32_t vocab);
 typedef struct {
     const float *logits, *draft_logits;

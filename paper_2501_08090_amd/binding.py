@@ -614,7 +614,8 @@ _verify_work = {}  # (requests, drafts, vocabulary) -> 4-byte words of workspace
 def verify_drafts(logits, tokens, uniforms, noise, draft_logits=None, draft_lens=None, temperature=None):
     """Accept or replace drafted tokens.  logits fp32 [batch, drafts+1, vocab] of the target, tokens int32 [batch, drafts], uniforms fp32
     [batch, drafts] in [0, 1), noise fp32 [batch, vocab] from the unit exponential distribution, draft_logits fp32 [batch, drafts,
-    vocab] or None (drafts that were not sampled), draft_lens int32 [batch], temperature fp32 [batch] (0: greedy).
+    vocab] or None (drafts that were not sampled), draft_lens int32 [batch], temperature fp32 [batch] (0: greedy).  At most 127 drafts,
+    and batch * (2 drafts + 1) at most 65535.
     -> tokens int32 [batch, drafts+1] (the accepted ones, the new one, then -1), accepted int32 [batch], prob fp32 [batch, drafts]"""
     batch, rows, vocab = logits.shape
     drafts = rows - 1

@@ -163,3 +163,15 @@ def test_select_pages_of_tables_wider_than_the_workspace(heads, rows, cols, pass
     if pass_seq:
         seq = [(r * 7 + 3) % rows for r in seq]
     T.check_select(c, bt, q, [lens[s] for s in seq], seq, 33, 1, 1, pass_seq=pass_seq)
+
+
+@pytest.mark.parametrize("batch,n,with_draft", ((257, 127, True), (257, 127, False), (65535, 0, True)))
+def test_verify_largest_calls(batch, n, with_draft):
+    """65535 rows of statistics, 2 n + 1 a request, are the most that one call takes"""
+    logits, draft, tokens, u, noise = T.drafts(batch, n, 5, 95)
+    assert batch * (2 * n + 1) == 65535
+    T.check_verify(logits, tokens, u, noise, draft if with_draft else None, strict=False)
+    more = [torch.cat((t, t[:1])).cuda() for t in (logits, tokens, u, noise)]
+    with pytest.raises(B.ChironError) as e:
+        B.verify_drafts(*more)
+    assert e.value.code == -3
