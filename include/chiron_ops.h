@@ -100,7 +100,10 @@ int32_t chiron_op_select_pages(chiron_model *m, const chiron_kvpool *p, const ch
 /* out[r][a] = softmax_t(q[r][a] . K_t / sqrt(d)) . V_t over the tokens t < ctx_lens[r] of the pages listed for (r, a / G)
  * in pages[r][a / G][0 .. counts[r]-1] (counts null: all `top` entries).  Lists may be any, in any order, without an
  * entry twice; entries that name no page of the row (negative, or behind ctx_lens[r]) count for nothing; a row that sees
- * no token gets zeros.  out dev fp32 [rows, n_q_heads*head_dim]. */
+ * no token gets zeros.  out dev fp32 [rows, n_q_heads*head_dim].
+ * Slots behind ctx_lens[r] may hold anything.  NaN and infinities that a row does attend, and in q, leave undefined what they
+ * meet and nothing else: one in a key the row's outputs of its KV head, one in a value its own dim of these (which is then no
+ * finite number), one in q its own head's.  (q and the weights go through the products in three terms, of which some are 0.) */
 int32_t chiron_op_sparse_attention(chiron_model *m, const chiron_kvpool *p, int32_t layer, const float *q,
                                    const int32_t *block_table, const int32_t *row_seq, const int32_t *ctx_lens, int32_t rows,
                                    const int32_t *pages, const int32_t *counts, int32_t top, float *out, void *stream);

@@ -175,3 +175,36 @@ def test_verify_largest_calls(batch, n, with_draft):
     with pytest.raises(B.ChironError) as e:
         B.verify_drafts(*more)
     assert e.value.code == -3
+
+
+@pytest.mark.parametrize("heads", ((2, 2, 64), (8, 2, 128), (32, 2, 64)))
+def test_sparse_attention_infinities_in_attended_places(heads):
+    """a key or query that is none leaves its own head's outputs undefined, a value its own dim's, and nothing else"""
+    n_q, n_kv, d = heads
+    G = n_q // n_kv
+    lens = [150, 90, 100]
+    for what in ("key", "value", "query"):
+        for val in (float("inf"), float("-inf"), float("nan")):
+            c, bt = T.filled(*heads, lens, 97, spread=False)
+            q = torch.randn((3, n_q * d), generator=torch.Generator().manual_seed(2)).cuda()
+            ctx = D.dev(np.array(lens, np.int32))
+            pages = D.dev(np.tile(np.arange(10, dtype=np.int32), (3, n_kv, 1)))
+            want = B.op_sparse_attention(c.model, c.pool, 0, q, D.dev(bt), ctx, pages).view(3, n_q, d).clone()
+            k, v = c.pool.layer_views(0)  # [page, token, head, d/8, 8] and [page, 4, 4 (token), head, d/32, 2, 16]
+            if what == "key":
+                k[int(bt[1, 2]), 3, 1, 2, 5] = val
+            elif what == "value":
+                v[int(bt[1, 2]), 1, 2, 1, 1, 1, 7] = val
+            else:
+                q[1, G * d + 9] = val
+            print(what, val, flush=True)
+            got = B.op_sparse_attention(c.model, c.pool, 0, q, D.dev(bt), ctx, pages).view(3, n_q, d)
+            same = torch.ones((3, n_q, d), dtype=torch.bool, device="cuda")
+            if what == "key":
+                same[1, G:] = False
+            elif what == "value":
+                same[1, G:, 32 + 16 + 7] = False
+                assert not got[1, G:, 32 + 16 + 7].isfinite().any()
+            else:
+                same[1, G] = False
+            assert torch.equal(got[same], want[same])
