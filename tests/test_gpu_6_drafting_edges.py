@@ -208,3 +208,60 @@ def test_sparse_attention_infinities_in_attended_places(heads):
             else:
                 same[1, G] = False
             assert torch.equal(got[same], want[same])
+
+
+def lists_near(q, c, bt, ctx, seq, top):
+    """page lists of odd lengths for every row and KV head: a stride through the row's pages, shuffled"""
+    rng = np.random.default_rng(5)
+    lists = np.full((len(ctx), c.n_kv, top), -1, np.int32)
+    counts = np.zeros(len(ctx), np.int32)
+    for r, n in enumerate(ctx):
+        pages = -(-n // 16)
+        counts[r] = min(pages, top - r % 7)
+        for h in range(c.n_kv):
+            lists[r, h, :counts[r]] = rng.permutation(pages)[:counts[r]]
+    return lists, counts
+
+
+@pytest.mark.parametrize("heads", ((2, 2, 64), (8, 2, 128)))
+def test_select_pages_long_lists_in_one_launch(heads):
+    """128 lists and more, of several rounds of 512 pages each: every wave scores more than once 64 pages"""
+    lens = [9601, 27199, 8192, 12000, 16001, 10001]
+    c, bt = T.filled(*heads, lens, 101)
+    rows = 64
+    seq = [r % 6 for r in range(rows)]
+    ctx = [lens[s] - 37 * (r // 6) for r, s in enumerate(seq)]
+    ctx[7], ctx[8] = 513 * 16, 1024 * 16 + 1
+    seq[7], seq[8] = 1, 1
+    q = torch.randn((rows, heads[0] * heads[2]), generator=torch.Generator().manual_seed(3)).cuda()
+    assert rows * heads[1] >= 128
+    for top in (45, 700):
+        T.check_select(c, bt, q, ctx, seq, top, 1, 1)
+
+
+@pytest.mark.parametrize("top", (600, 701, 1100))
+def test_sparse_attention_lists_that_a_wave_fetches_in_pieces(top):
+    """129 lists and more, so that no list is split, with more than 64 entries a wave"""
+    lens = [17000, 11111]
+    c, bt = T.filled(3, 3, 64, lens, 102, spread=False)
+    rows = 48
+    seq = [r % 2 for r in range(rows)]
+    ctx = [lens[s] - 5 * r for r, s in enumerate(seq)]
+    q = torch.randn((rows, 192), generator=torch.Generator().manual_seed(4)).cuda()
+    lists, counts = lists_near(q, c, bt, ctx, seq, top)
+    assert rows * 3 > 128
+    T.check_attend(c, bt, q, ctx, seq, D.dev(lists), D.dev(counts))
+
+
+@pytest.mark.parametrize("M", (5, 8))
+@pytest.mark.parametrize("zeros", (False, True))
+@pytest.mark.parametrize("N,K", ((8003, 2080), (12001, 4096), (28671, 3104)))
+def test_linear4_several_chunks_and_tiles(M, zeros, N, K):
+    """groups of 32 and 5 to 8 rows: a workgroup goes through more than one chunk of K for more than one tile"""
+    w4, s, z = T.weights(N, K, 32, zeros, 103)
+    lin = B.Linear4(w4.cuda(), s.cuda(), None if z is None else z.cuda())
+    pick = np.r_[0:20, 16 * 256:16 * 256 + 32, N // 2:N // 2 + 20, N - 40:N]
+    w, sk = D.weights4(w4[pick], s[pick], None if z is None else z[pick], 32)
+    x = torch.randn((M, K), generator=torch.Generator().manual_seed(M))
+    T.check_linear4(T.some_columns(lin, pick), w, sk, x, 32)
+    T.check_linear4(T.some_columns(lin, pick), w, sk, x, 32, torch.randn((M, len(pick)), generator=torch.Generator().manual_seed(1)), True)
