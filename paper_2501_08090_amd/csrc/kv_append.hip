@@ -410,11 +410,9 @@ int32_t chiron_append_kv_rope(chiron_kvpool* p, chiron_kvindex* index, int32_t l
     const int64_t page_wgs = (tasks + 3) / 4;
     if (page_wgs + q_wgs > 0x7fffffff) return fail(CHIRON_ERR_SHAPE, "append: %d rows of %d heads are too many for one call", rows, in->n_q_heads);
     a.page_wgs = (int)page_wgs;
-    // Queries that the last-level cache (256 MB) does not hold until somebody reads them go past it.  us with the hint / without, alone
-    // and with a pass over the queries behind the call: 5003 bf16 rows of 32 heads of 128 (78 MiB of queries) 33.3 / 32.8 and 61 / 57, 12000
-    // (188) 73 / 81 and 134 / 126, 14000 (219) 86 / 93 and 156 / 154, 16384 (256) 100 / 107 and 183 / 198; fp32 rows 5003 42 / 40.5 and 70 / 65,
-    // 12000 94 / 100 and 157 / 157, 16384 127 / 135 and 219 / 233.
-    a.stream = (int64_t)rows * in->n_q_heads * d * 4 > (192 << 20);
+    // Queries that the L2s do not hold together anyway go past them (5003 bf16 rows of 32 heads of 128 37.5 us, 42.8 without; 16384 fp32
+    // rows with the index 128 and 140); fewer stay there for who reads them next.
+    a.stream = (int64_t)rows * in->n_q_heads * d * 4 > (32 << 20);
     hipStream_t st = (hipStream_t)stream;
     const dim3 grid((unsigned)(page_wgs + q_wgs));
     const bool f32 = in->dtype == CHIRON_F32;
