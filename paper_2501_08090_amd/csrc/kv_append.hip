@@ -410,8 +410,11 @@ int32_t chiron_append_kv_rope(chiron_kvpool* p, chiron_kvindex* index, int32_t l
     const int64_t page_wgs = (tasks + 3) / 4;
     if (page_wgs + q_wgs > 0x7fffffff) return fail(CHIRON_ERR_SHAPE, "append: %d rows of %d heads are too many for one call", rows, in->n_q_heads);
     a.page_wgs = (int)page_wgs;
-    // Queries that the L2s do not hold together anyway go past them (5003 bf16 rows of 32 heads of 128 37.5 us, 42.8 without; 16384 fp32
-    // rows with the index 128 and 140); fewer stay there for who reads them next.
+    // Queries that the L2s do not hold together go past them.  us with the hint / without, queries written to memory that no cache holds: 2048
+    // bf16 rows of 32 heads of 128 (32 MiB) 15.5 / 13.9 to 18.2, 3500 24 / 26.4, 5003 31.9 / 37.1, 16384 100 / 107; fp32 rows 5003 39 / 45.6, 16384
+    // 127 / 136.  Where the last call's queries lie in the same memory the two are level up to some 8000 rows.  What the hint saves here
+    // is less than what a pass over the queries behind the call takes longer, up to 12000 rows (5003 bf16 rows and the pass 67.6 / 58.5, 12000
+    // 149 / 132, 16384 199 / 199).
     a.stream = (int64_t)rows * in->n_q_heads * d * 4 > (32 << 20);
     hipStream_t st = (hipStream_t)stream;
     const dim3 grid((unsigned)(page_wgs + q_wgs));

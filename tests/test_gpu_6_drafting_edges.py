@@ -265,3 +265,23 @@ def test_linear4_several_chunks_and_tiles(M, zeros, N, K):
     x = torch.randn((M, K), generator=torch.Generator().manual_seed(M))
     T.check_linear4(T.some_columns(lin, pick), w, sk, x, 32)
     T.check_linear4(T.some_columns(lin, pick), w, sk, x, 32, torch.randn((M, len(pick)), generator=torch.Generator().manual_seed(1)), True)
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("shift", (0, 1))
+def test_append_queries_that_go_past_the_caches(dtype, shift):
+    """195 MiB of rotated queries; products and sums of the rotation in fp32"""
+    n_q, d, rows = 16, 128, 25000
+    c = D.Cache(n_q, 1, d, 1600)
+    g = torch.Generator(device="cuda").manual_seed(9)
+    whole = torch.randn((rows, (n_q + 2) * d + shift), generator=g, device="cuda").to(dtype)[:, shift:]
+    q, k, v = (t.unflatten(1, (-1, d)) for t in whole.split((n_q * d, d, d), 1))
+    cos, sin = B.rope_table(torch.arange(rows, dtype=torch.int32, device="cuda"), d, 10000.0)
+    bt = torch.randperm(1600, generator=torch.Generator().manual_seed(1)).to(torch.int32).cuda()[None]
+    got = c.pool.append_rope(0, k, v, cos, sin, bt, D.dev(np.array([0, rows], np.int32)), D.dev(np.zeros(1, np.int32)), q=q)
+    a, b = q.double().chunk(2, -1)
+    cd, sd = cos.double()[:, None], sin.double()[:, None]
+    off = (a.abs() + b.abs()) * 2.0 ** -22
+    assert ((got[..., :d // 2] - (a * cd - b * sd)).abs() <= off).all() and ((got[..., d // 2:] - (b * cd + a * sd)).abs() <= off).all()
+    stored = c.pool.layer_views(0)[1].reshape(1600, 16, 1, d)[bt[0].long()].view(-1, 1, d)[:rows]
+    assert torch.equal(stored, v.to(torch.bfloat16))
