@@ -7,8 +7,9 @@
 // row_starts[i]/16 + 2i on, and a wave finds its request by counting those whose slots have begun, 64 at a time.
 //
 // Bound by its bytes, of which more are written than read: 5003 bf16 rows of 32 + 2 * 8 heads of 128, which the caches do not hold, 33 us
-// (5.0 TB/s), 16384 fp32 rows with the index 130 us (5.8 TB/s; a copy of 4 GiB 4.7).  64 rows 5.1 us: the launch and a chain of loads
-// (where the request's rows start, its length, its pages, its rows).
+// (5.0 TB/s), 16384 fp32 rows with the index 130 us (5.8 TB/s; a copy of 4 GiB 4.7).  64 rows 5.4 us: the launch and a chain of loads
+// (where the request's rows start, its length, its pages, its rows); with the index 9.8, the old tokens' keys being one load more
+// behind these.
 #include <new>
 
 #include "draft_ops.h"

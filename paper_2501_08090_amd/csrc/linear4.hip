@@ -214,7 +214,7 @@ __device__ __forceinline__ uint32_t block_top(const float (&v)[8]) {
 // one operand (column = 4 * digit + row), with up to 8 those of two operands (8 * (digit % 2) + row), else four.  A slice of more than 8 NB blocks
 // goes in chunks, whose sums wait in LDS (for kFewTiles tiles at most): adding them up in y would put a load behind the weights on their
 // way, and what it waits for would be all of them.  The loops hold no branch that depends on a wave: blocks behind the slice's end
-// read the last one again and count with 0.  8 rows through 28672 x 4096: 17 us, 3.6 TB/s; one through 4096 x 4096: 5.
+// read the last one again and count with 0.  8 rows through 28672 x 4096: 17 us, 3.6 TB/s; one through 4096 x 4096: 5.1.
 // Bound by what stands before and beside the stream of weights: the launch, bringing x in (its conversion is a chain of loads, a maximum
 // over 16 lanes and LDS) and, with more rows, the scaling of the digits' sums.
 // Digits lie in LDS as the operands want them, 16 bytes a lane, column c of lane group g and step k in the place c ^ (4 g + k % 4) of its
@@ -374,10 +374,10 @@ __global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const fl
 
 // ---- many rows -------------------------------------------------------------------------------------------------
 // x enters as two fp16 terms of x * 2^up, up to 2^15 of a block of 128; a group costs one multiplication and one fused multiply-add for
-// each result, where three digits cost five instructions.  64 rows through 8192 x 28672 with groups of 64 and zero points: 80 us, 70 of
-// them in this kernel, against 100 and 87 with digits (17 rows through 28672 x 4096: 31 and 28).  What bounds it is the matrix cores and
-// the vector units, which share issue and power: with no products 56 us are left of the 70, with no loads of weights or x 60.  The 60
-// GFLOP run at 0.86 PFLOP/s, a large fp16 product of the library reaches 1.1; the weights take 19 us.
+// each result, where four digits cost six instructions.  64 rows through 8192 x 28672 with groups of 64 and zero points: 80 us, 70 of
+// them in this kernel, against 100 and 87 with three digits (17 rows through 28672 x 4096: 29, by passes with four digits 30).  What bounds
+// it is the matrix cores and the vector units, which share issue and power: with no products 56 us are left of the 70, with no loads of
+// weights or x 60.  The 60 GFLOP run at 0.86 PFLOP/s, a large fp16 product of the library reaches 1.1; the weights take 19 us.
 //
 // x for the whole launch: terms [rows/16][K/128][4 steps of 32][2][64 lanes][16 B], scales [rows/16][K/128][16] fp32.  A lane's eight
 // values of a step lie in the order in which masks take weights out of a dword: (4,6) (0,2) (5,7) (1,3).

@@ -628,7 +628,10 @@ int32_t chiron_op_select_pages(chiron_model* m, const chiron_kvpool* p, const ch
     a.pages = pages; a.counts = counts; a.layer = layer; a.max_blocks = mb; a.top = top; a.n_first = n_first; a.n_last = n_last;
     hipStream_t st = (hipStream_t)stream;
     const int d = p->d.d;
-    // us of a CU for a whole list's records at 45 B/ns, against some 5 us for the second launch
+    // us of a CU for a whole list's records at 45 B/ns, against some 5 us for the second launch.  The host knows the table's width, not what
+    // the rows see of it, and short lists cost less in the wrong form than long ones: us in one launch / two, 8 KV heads of 128, tables of
+    // 8192 columns: one row of 100 pages 7.0 / 8.8, 510 10.7 / 10.8, 2000 23.6 / 13.8; 4 rows 7.3 / 11.4, 10.7 / 12.8, 23.8 / 16.7; 15 rows 7.3 /
+    // 11.5, 10.9 / 13.6, 26.4 / 24.9.
     const bool one = mb <= kSelectPages && (lists * 2 >= kNumCU || (double)mb * 2 * d / 45e3 <= 5.0);
     if (one) {
         const size_t lds = ((size_t)mb + 63) / 64 * 64 * 4;

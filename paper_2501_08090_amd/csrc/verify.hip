@@ -6,7 +6,7 @@
 // many drafts are taken (every workgroup of a request comes to the same answer from the same numbers), and races what is left of the
 // vocabulary in its piece; the two or three rows it needs again come from the caches.  The pieces' winners meet in an
 // atomic maximum, and the workgroup of a request that comes last writes the token.
-// 64 requests of 4 drafts over 128256 tokens: 46 us (6.4 TB/s) and 23; one request: 5.4 and 8.7, a chain of loads that wait for one
+// 64 requests of 4 drafts over 128256 tokens: 46 us (6.4 TB/s) and 23; one request: 5.6 and 8.6, a chain of loads that wait for one
 // another.  (A third launch for the winners, and the decision in one thread's loop, took 5 us more, with one request and with 23.)
 // The race argmax r(x)/noise(x) instead of a running sum over the vocabulary: it is one pass in any order, and which token wins does
 // not depend on the order of any sum.
@@ -50,7 +50,8 @@ struct VerifyArgs {
     float* prob;
 };
 
-// exp(d / T) with c = log2(e) / T, for sums: |d / T| 2^-24 off, where that is much the term is small
+// exp(d / T) with c = log2(e) / T by one product and the machine's exponential: off by up to |d / T| 2^-22 + 2^-23 of itself, as c has three
+// roundings and the product one.  In a sum that is much only where the term is small.
 __device__ __forceinline__ float weight(float d, float c) { return __builtin_amdgcn_exp2f(d * c); }
 __device__ __forceinline__ float log2e_over(float inv_t) { return fminf(inv_t * 1.44269504088896341f, kTopF32); }
 __device__ __forceinline__ float logit_of(float x) { return x != x ? -INFINITY : fminf(x, kTopF32); }
@@ -253,7 +254,8 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_race_kernel(VerifyArgs 
         if (qrow)
 #pragma unroll
             for (int j = 0; j < VPT; ++j) qv[j] = x0 + j * kVerifyThreads < a.vocab ? qrow[x0 + j * kVerifyThreads] : -INFINITY;
-        // exponentials and quotients of the machine's own precision: 2 to 3 units in the last place, as far as who wins a race goes
+        // Exponentials and reciprocals of the machine's own precision: r / noise is off by up to |d / T| 2^-22 + 2^-21 of itself, 2^-16 for a
+        // token with e^-50 of the largest share.  Only a race as close as that can go to the other token.
         const float rp = 1.f / p.z, rq = q.z > 0.f ? 1.f / q.z : 0.f;
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
