@@ -104,7 +104,7 @@ def sample(logits, temperature, noise):
 def draft_and_verify(drafter, block_table, seq_lens, tokens, drafts, temperature, generator):
     """One round: `drafts` tokens drafted behind tokens [batch], verified by one step of the model, accepted or replaced.
     -> new tokens int32 [batch, drafts+1] (accepted + 1 of them, then -1), accepted int32 [batch], and the next round's
-    seq_lens and tokens.  The pages of the positions seq_lens .. seq_lens+drafts must be in the block table."""
+    seq_lens and tokens (token 0 for a request whose logits left nothing to choose, where the new token is -1).  The pages of the positions seq_lens .. seq_lens+drafts must be in the block table."""
     model, pool = drafter.model, drafter.pool
     batch, vocab, dev = tokens.numel(), model.cfg.vocab, tokens.device
     fed, draft_logits = [tokens], []
@@ -120,7 +120,7 @@ def draft_and_verify(drafter, block_table, seq_lens, tokens, drafts, temperature
                                        draft_logits=torch.stack(draft_logits, 1) if drafts else None, temperature=temperature)
     seq_next = seq_lens + accepted + 1
     drafter.index.update(block_table, seq_lens, seq_next, drafts + 1)  # the model's keys have taken the place of the draft's
-    return out, accepted, seq_next, out.gather(1, accepted.long()[:, None]).view(-1)
+    return out, accepted, seq_next, out.gather(1, accepted.long()[:, None]).view(-1).clamp(min=0)  # a step takes no token that is none
 
 
 def main(argv=None):

@@ -7,7 +7,10 @@ import torch
 
 import drafting as D
 import test_gpu_4_drafting as T
+import test_gpu_5_draft_and_verify as V
 from paper_2501_08090_amd import binding as B
+from paper_2501_08090_amd import drafting as DV
+from paper_2501_08090_amd import inputs as I
 
 pytestmark = pytest.mark.gpu
 
@@ -285,3 +288,18 @@ def test_append_queries_that_go_past_the_caches(dtype, shift):
     assert ((got[..., :d // 2] - (a * cd - b * sd)).abs() <= off).all() and ((got[..., d // 2:] - (b * cd + a * sd)).abs() <= off).all()
     stored = c.pool.layer_views(0)[1].reshape(1600, 16, 1, d)[bt[0].long()].view(-1, 1, d)[:rows]
     assert torch.equal(stored, v.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("temperature", (0.0, 0.8))
+def test_rounds_of_a_model_without_logits_go_on(temperature):
+    """logits that are all NaN: the new token is -1, what the next round is fed is a token all the same"""
+    m = dict(I.TINY)
+    w = I.make_weights(m, seed=7, device="cuda", std=0.02)
+    w["final_norm"] = torch.full_like(w["final_norm"], float("nan"))
+    d, bt, sl = V.setup(m, np.array([20, 5], np.int32), 40, w, 64, 4, 24, seed=7)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    tokens = torch.tensor([1, 2], dtype=torch.int32, device="cuda")
+    for r in range(2):
+        out, accepted, sl, tokens = DV.draft_and_verify(d, bt, sl, tokens, 2, torch.full((2,), temperature, device="cuda"), g)
+        assert (out == -1).all() and (accepted == 0).all() and (tokens == 0).all() and sl.tolist() == [21 + r, 6 + r]
