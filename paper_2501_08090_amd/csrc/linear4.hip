@@ -327,6 +327,9 @@ __global__ __launch_bounds__(512, 2) void linear4_few_kernel(Linear4 l, const fl
                         else v = join_digits(p[0][r], p[1][r], p[2][r], p[3][r]);
                         sum[r] = u == 0 ? v * sc[j][i].get(r, u) : fmaf(v, sc[j][i].get(r, u), sum[r]);
                     }
+                    // one group's sums are done before the next's products begin: the compiler otherwise holds all 32 products, and scratch
+                    // memory for what they displace costs 4 us a launch
+                    if constexpr (SETS == 4 && GROUP == 32) asm volatile("" : "+v"(sum[0]), "+v"(sum[1]), "+v"(sum[2]), "+v"(sum[3]));
                 }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) acc[r] = fmaf(sum[r], base[i], acc[r]);
@@ -704,13 +707,14 @@ struct Plan4 {
 static Plan4 plan_linear4(const Linear4& l, int64_t M) {
     Plan4 p;
     const int64_t kb = l.Kpad / 128;
-    // More than 16 rows by passes of up to 16 too, as long as all passes' weights stay within 2^27, 1.25 * 2^26 or 0.75 * 2^26 (groups of 128, 64
-    // or 32): one launch, or two, for the tiles' three, but every pass unpacks the weights again, and the smaller the groups, the more of
+    // More than 16 rows by passes of up to 16 too, as long as all passes' weights stay within 2^27, 1.25 * 2^26 or 2^26 (groups of 128, 64 or
+    // 32): one launch, or two, for the tiles' three, but every pass unpacks the weights again, and the smaller the groups, the more of
     // the time goes by results and groups.  us passes / tiles, groups of 128: 64 rows through 4096 x 4096 15.7 / 23.3, 8192 x 4096 (2^27) 22.9 /
     // 26.8, 14336 x 4096 32.7 / 29.6; 32 rows through 4096 x 14336 (1.75 * 2^26) 23.1 / 21.7, 14336 x 4096 21.3 / 21.1; groups of 64 with zero
     // points: 64 rows through 4096 x 4096 (2^26) 19.0 / 24.0, 48 through 5120 x 5120 (1.17 * 2^26) 28.3 / 22.7 and 8192 x 4096 (1.5 * 2^26) 25.3 / 23.8;
-    // groups of 32: 64 rows through 2048 x 4096 (2^25) 17.0 / 21.9 and 4096 x 4096 (2^26) 22.9 / 25.0, 32 through 8192 x 4096 (2^26) 23.2 / 20.6.
-    const int64_t passes = (M + 15) / 16, limit = (l.group == 128 ? 8 : l.group == 64 ? 5 : 3) * ((int64_t)1 << 24);
+    // groups of 32: 64 rows through 2048 x 4096 (2^25) 14.9 / 21.9 and 4096 x 4096 (2^26) 21.2 / 25.1, 32 through 8192 x 4096 (2^26) 21.3 / 20.6, 48
+    // through 5120 x 5120 (1.17 * 2^26) 33.3 / 23.7.
+    const int64_t passes = (M + 15) / 16, limit = (l.group == 128 ? 8 : l.group == 64 ? 5 : 4) * ((int64_t)1 << 24);
     if (passes == 1 || passes * l.N * kb * 128 <= limit) {
         p.passes = (int)passes;
         p.pass_rows = (int)((M + p.passes - 1) / p.passes);
