@@ -176,6 +176,82 @@ int32_t chiron_kv_index_update(chiron_kvindex *x, const chiron_kvpool *p, int32_
                                const int32_t *block_table, int32_t max_blocks_per_seq, const int32_t *from,
                                const int32_t *to, int32_t batch, int32_t max_new, void *stream);
 
+/* ---- page lists: block tables and slot maps laid out on the device -----------------------------------------------
+ *
+ * A page list holds the pages that nobody uses: pages[0 .. count-1].  Everything is whole-number arithmetic in a fixed order:
+ * the same inputs give the same tables, whatever ran before on the device.
+ *   pages  dev int32 [capacity], capacity <= 2^30;  count  dev int32 [1], 0 .. capacity (other values count as the nearer of the two)
+ * Calls that share a list or a table must not overlap. */
+typedef struct {
+    int32_t *pages, *count;
+    int32_t capacity;
+} chiron_page_list;
+
+/* What chiron_kv_grant_pages lays out for the rows of a step (one row: one new token); all but row_starts may be null. */
+typedef struct {
+    int32_t *row_starts; /* dev [batch+1]: request i brings the rows row_starts[i] .. row_starts[i+1]-1           */
+    int32_t *row_seq;    /* dev [max_rows]: request of the row, -1 behind the last row                            */
+    int32_t *pos;        /* dev [max_rows]: position of the row's token, 0 behind the last row                    */
+    int64_t *slots;      /* dev [max_rows]: slot(row_seq, pos), -1 behind the last row and where there is no page */
+    int32_t *granted;    /* dev [batch]: new_lens[i], or 0 for a request that has to wait                         */
+} chiron_row_maps;
+
+/* Request i holds seq_lens[i] tokens and asks for new_lens[i] more.  The columns seq_lens[i]/16 .. (seq_lens[i]+new_lens[i]-1)/16 of its
+ * block table that hold no page (-1) need one each: need_i.  Request i is granted if
+ *     it fits the table: seq_lens[i], new_lens[i] >= 0 and seq_lens[i] + new_lens[i] <= 16 * max_blocks_per_seq,
+ *     the rows of the requests 0 .. i that fit it are at most max_rows together, and
+ *     need_i = 0, or need_0 + .. + need_i (of the requests that fit) is at most the list's count.
+ * The granted ones' empty columns get the last pages of the list, the first of these to the lowest request and column; the count goes
+ * down by as many.  Another request changes nothing and brings no row (a request with new_lens 0 is granted nothing and keeps nothing
+ * waiting).  A call repeated on its own result grants the same rows and takes no page.
+ *   block_table  dev int32 [batch, max_blocks_per_seq], in and out;  seq_lens, new_lens  dev int32 [batch]
+ *   workspace    dev, chiron_kv_pages_workspace_bytes(batch) bytes, 16-byte aligned, caller-owned, in use until the stream has passed
+ * max_blocks_per_seq <= 2^26. */
+int64_t chiron_kv_pages_workspace_bytes(int32_t batch);
+int32_t chiron_kv_grant_pages(const chiron_page_list *list /* host */, int32_t *block_table, int32_t max_blocks_per_seq,
+                              const int32_t *seq_lens, const int32_t *new_lens, int32_t batch, int32_t max_rows,
+                              const chiron_row_maps *out /* host */, void *workspace, void *stream);
+
+/* Gives back the pages that lie wholly within the positions from[i] .. to[i]-1 of each request: the columns ceil(from[i]/16) ..
+ * to[i]/16 - 1 (to null: all from ceil(from[i]/16) on).  A page found there (an entry >= 0) goes to the end of the list, the lowest
+ * request and column first, and its entry becomes -1; pages for which the list has no room stay.  A page that other requests use as well
+ * (a shared prefix) is the caller's to leave out.  from 0: an ended request; from = the tokens accepted: rejected drafts; from = the sinks,
+ * to = seq_len - window + 1: what a window has passed.
+ *   from, to  dev int32 [batch] (negative: 0) */
+int32_t chiron_kv_release_pages(const chiron_page_list *list /* host */, int32_t *block_table, int32_t max_blocks_per_seq,
+                                const int32_t *from, const int32_t *to, int32_t batch, void *workspace, void *stream);
+
+/* ---- cache in 8 bits --------------------------------------------------------------------------------------------
+ *
+ * A pool whose values are 8-bit codes with one power of two for each page and KV head, keys and values apart:
+ *     value = code * 2^e,   code an int8 in -127 .. 127 (CHIRON_INT8) or an e4m3 number up to 448 (CHIRON_E4M3)
+ *     e = the smallest whole number, at least -100, with  max |x| <= 127 * 2^e  (448 * 2^e)  over the page's tokens
+ *     code = x / 2^e rounded to the nearest, ties to even
+ * so that every value is a bf16 number.  NaN counts as 0, what is beyond +-2^100 as that.  Where new tokens come to a page that holds old
+ * ones, e is the larger of the page's and the new tokens' own, and the old codes are rounded again if it grew (at most half a step of
+ * the new e more).  It never shrinks while a page has tokens.
+ * The pool is a descriptor over CALLER-owned device memory, `bytes` >= chiron_kv8_pool_bytes(m, num_blocks), 256-byte aligned; it is
+ * not cleared.  Half a bf16 pool's size, and 2 bytes for each layer, page and KV head.  Layout:
+ *     per layer  codes [num_blocks][n_kv_heads][K tile, V tile of 16*head_dim], then int8 e [num_blocks][n_kv_heads][K, V], the layer's
+ *     total padded to 256 bytes;  K tile [d/16][16 tokens][16 dims],  V tile [d/64][4 tokens/4][16 dims][4 dims/16][4 tokens]. */
+enum { CHIRON_INT8 = 3, CHIRON_E4M3 = 4 };
+typedef struct chiron_kvpool8 chiron_kvpool8;
+int64_t chiron_kv8_pool_bytes(const chiron_model *m, int32_t num_blocks); /* 0: bad arguments */
+int32_t chiron_kv8_pool_create(const chiron_model *m, void *dev_mem, uint64_t bytes, int32_t num_blocks, int32_t format,
+                               chiron_kvpool8 **out);
+int32_t chiron_kv8_pool_destroy(chiron_kvpool8 *p); /* does not free dev_mem */
+
+/* chiron_append_kv_rope into such a pool: same rows, same rotation, same arguments but the page index. */
+int32_t chiron_kv8_append_rope(chiron_kvpool8 *p, int32_t layer, const chiron_new_rows *in, const int32_t *block_table,
+                               int32_t max_blocks_per_seq, const int32_t *row_starts, const int32_t *seq_lens, int32_t batch,
+                               int32_t rows, void *stream);
+
+/* Logical read-back, the counterpart of chiron_append_kv: token j is at position pos[j] of row seq_idx[j] of the block table.
+ * k_out, v_out dev bf16 [n, n_kv_heads, head_dim], exact; zeros where there is no page (a position that is negative or behind the
+ * table's last column, an entry that is no page of the pool). seq_idx must name rows of the table. */
+int32_t chiron_kv8_gather(const chiron_kvpool8 *p, int32_t layer, const int32_t *block_table, int32_t max_blocks_per_seq,
+                          const int32_t *seq_idx, const int32_t *pos, int64_t n, void *k_out, void *v_out, void *stream);
+
 /* Eviction support (Design: a mixed instance evicts a batch request when an interactive one arrives, and
  * saves its KV cache by migrating it to CPU memory so that it can restart fast).
  * chiron_kv_swap_out copies the first n_pages pages of one request (every layer, K and V) into `image`;

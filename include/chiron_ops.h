@@ -111,6 +111,40 @@ int32_t chiron_op_sparse_attention(chiron_model *m, const chiron_kvpool *p, int3
  * (8192 + 2 max_batch) * G * head_dim columns, 8 million tokens at the least, have no room in it for one row's scores: the selection
  * refuses them. */
 
+/* ---- attention of new rows: windows, first tokens that stay, caches in 8 bits -------------------------------------
+ *
+ * Request i brings the rows row_starts[i] .. row_starts[i+1]-1 of q, single tokens or whole prompts, whose keys and values are in
+ * the cache already (chiron_append_kv_rope, chiron_kv8_append_rope with the same row_starts and seq_lens): its row t is the token at
+ * position p = seq_lens[i] + t.  For query head a, with KV head a / G,
+ *     out[r][a] = softmax_u(q[r][a] . K_u / sqrt(d)) . V_u  over the positions  u <= p  with  u > p - window  or  u < n_sinks
+ * (window 0: over all u <= p).  Pages that no row of a request sees are not touched: their entries may be -1.  Positions whose entry
+ * is no page of the pool, or behind the table's last column, count as not there; a row that sees none gets zeros.  What other slots hold
+ * (behind a request's last token, out of every window) may be anything.  NaN and infinities in a key that a row sees leave its outputs
+ * of that KV head undefined, in a value the same dim of these, in q its own head's, and reach no other row.
+ *   in           host, read during the call
+ *     dtype      CHIRON_F32: q and out fp32, products in three bf16 terms (fp32's accuracy); CHIRON_BF16: q and out bf16, one
+ *                term, weights rounded to bf16 (errors of the order of out's own rounding), scores, sums and the softmax in fp32
+ *     q, out     dev [rows][n_q_heads][head_dim], 16-byte aligned; q rows q_stride elements apart (16-byte multiples), heads and dims
+ *                contiguous; out contiguous, not overlapping q
+ *     n_q_heads  a multiple of the pool's KV heads, at most 16 times as many
+ *     max_new    >= the rows of any request (those behind a request's first max_new are left as they were)
+ *   row_starts dev int32 [batch+1], ascending from 0 to at most rows (rows behind the last request are left as they were, as are some
+ *                of row starts that do not ascend);  seq_lens dev int32 [batch], tokens cached before these (negative: 0)
+ *   block_table  dev int32 [batch, max_blocks_per_seq], max_blocks_per_seq <= 2^26
+ *   workspace    dev, chiron_row_attention_workspace_bytes() bytes, 16-byte aligned, caller-owned, in use until the stream has passed */
+typedef struct {
+    const void *q;
+    void *out;
+    int64_t q_stride;
+    int32_t dtype, n_q_heads;
+    const int32_t *block_table, *row_starts, *seq_lens;
+    int32_t max_blocks_per_seq, batch, rows, max_new, window, n_sinks;
+} chiron_attn_rows;
+int64_t chiron_row_attention_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t batch, int32_t rows,
+                                             int32_t max_new); /* 0: nothing to do, or bad arguments */
+int32_t chiron_op_row_attention(const chiron_kvpool *p, int32_t layer, const chiron_attn_rows *in, void *workspace, void *stream);
+int32_t chiron_op_row_attention8(const chiron_kvpool8 *p, int32_t layer, const chiron_attn_rows *in, void *workspace, void *stream);
+
 /* ---- verification of drafted tokens ---------------------------------------------------------------------------
  *
  * Request i drafted n_i = draft_lens[i] (0 .. max_draft; null: max_draft) tokens x_t = tokens[i][t]; logits[i][t] are the

@@ -7,6 +7,7 @@ fallback: if the library has not been built, loading raises.
 """
 import ctypes as C
 import os
+from collections import namedtuple
 from operator import index
 
 import torch
@@ -16,6 +17,8 @@ LIB_PATH = os.environ.get("CHIRON_LIB", os.path.join(_HERE, "libchiron.so"))
 
 CHIRON_BF16 = 1
 CHIRON_F32 = 2
+CHIRON_INT8 = 3
+CHIRON_E4M3 = 4
 ERRORS = {0: "OK", -1: "INVALID_ARG", -2: "SHAPE", -3: "BATCH_TOO_LARGE", -4: "BLOCK_TABLE", -5: "OOM", -6: "HIP", -7: "TOKEN"}
 
 # every symbol the headers declare (tests check that the library exports all of them)
@@ -32,6 +35,9 @@ SYMBOLS = [
     "chiron_op_rope_table", "chiron_op_select_pages", "chiron_op_sparse_attention", "chiron_verify_workspace_bytes",
     "chiron_op_verify_drafts", "chiron_linear4_create", "chiron_linear4_destroy", "chiron_op_linear4",
     "chiron_linear4_workspace_bytes",
+    "chiron_kv_pages_workspace_bytes", "chiron_kv_grant_pages", "chiron_kv_release_pages", "chiron_kv8_pool_bytes", "chiron_kv8_pool_create",
+    "chiron_kv8_pool_destroy", "chiron_kv8_append_rope", "chiron_kv8_gather", "chiron_row_attention_workspace_bytes",
+    "chiron_op_row_attention", "chiron_op_row_attention8",
 ]
 
 
@@ -61,6 +67,20 @@ class DraftBatch(C.Structure):
         (n, C.c_void_p) for n in ("tokens", "draft_lens", "uniforms", "noise", "temperature")]
 
 
+class PageListArgs(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("count", C.c_void_p), ("capacity", C.c_int32)]
+
+
+class RowMapArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("row_starts", "row_seq", "pos", "slots", "granted")]
+
+
+class AttnRows(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("q_stride", C.c_int64), ("dtype", C.c_int32), ("n_q_heads", C.c_int32)] + [
+        (n, C.c_void_p) for n in ("block_table", "row_starts", "seq_lens")] + [
+        (n, C.c_int32) for n in ("max_blocks_per_seq", "batch", "rows", "max_new", "window", "n_sinks")]
+
+
 class ProfilePoint(C.Structure):
     _fields_ = [("batch", C.c_int32), ("lat_ms_median", C.c_double), ("lat_ms_p99", C.c_double),
                 ("lat_ms_mean", C.c_double), ("tokens_per_s", C.c_double)]
@@ -76,7 +96,10 @@ _HOT = {"chiron_decode_step": "pppppipp", "chiron_decode_step_multi": "pppppiipp
         "chiron_op_gate_up_swiglu": "ppipp", "chiron_op_swiglu_ffn": "pppipip", "chiron_op_paged_attention": "ppipppipp",
         "chiron_append_kv_rope": "ppippippiip", "chiron_kv_index_update": "ppiipippiip", "chiron_op_select_pages": "pppippppiiiippp",
         "chiron_op_sparse_attention": "ppippppippipp", "chiron_verify_workspace_bytes": "iii", "chiron_op_verify_drafts": "piiippppp",
-        "chiron_op_linear4": "ppipipp", "chiron_linear4_workspace_bytes": "pi"}
+        "chiron_op_linear4": "ppipipp", "chiron_linear4_workspace_bytes": "pi",
+        "chiron_kv_pages_workspace_bytes": "i", "chiron_kv_grant_pages": "ppippiippp", "chiron_kv_release_pages": "ppippipp",
+        "chiron_kv8_append_rope": "pippippiip", "chiron_kv8_gather": "pipipplppp", "chiron_row_attention_workspace_bytes": "iiiiii",
+        "chiron_op_row_attention": "pippp", "chiron_op_row_attention8": "pippp"}
 _TYPES = {"p": C.c_void_p, "i": C.c_int32, "l": C.c_int64}
 
 
@@ -93,6 +116,9 @@ def load():
         lib.chiron_kv_index_bytes.restype = C.c_int64
         lib.chiron_verify_workspace_bytes.restype = C.c_int64
         lib.chiron_linear4_workspace_bytes.restype = C.c_int64
+        lib.chiron_kv_pages_workspace_bytes.restype = C.c_int64
+        lib.chiron_kv8_pool_bytes.restype = C.c_int64
+        lib.chiron_row_attention_workspace_bytes.restype = C.c_int64
         for name, types in _HOT.items():
             getattr(lib, name).argtypes = [_TYPES[t] for t in types]
         _lib = lib
@@ -157,6 +183,32 @@ def _rows_of(t, rows, heads, d, dtype):
     if s2 != 1 or (s1 != d and heads > 1) or s0 < heads * d:
         raise TypeError("heads and dims of a row must be contiguous")
     return t.data_ptr(), s0
+
+
+def _new_rows(cfg, k, v, cos, sin, block_table, row_starts, seq_lens, q, q_out):
+    """the arguments that an append of new rows takes between the layer and the stream, and the rotated q"""
+    rows, batch, d, dtype = k.shape[0], seq_lens.numel(), cfg.head_dim, k.dtype
+    if dtype not in _ROW_TYPES:
+        raise TypeError("expected torch.float32 or torch.bfloat16, got %s" % dtype)
+    width = block_table.shape[1] if block_table.dim() == 2 else -1
+    if width < 0 or block_table.shape[0] < batch or row_starts.numel() != batch + 1:
+        raise ValueError("%d requests need %d row starts and as many rows of the block table, got %d and %s" % (
+            batch, batch + 1, row_starts.numel(), tuple(block_table.shape)))
+    if cos.numel() != rows * (d // 2) or sin.numel() != cos.numel():
+        raise ValueError("cos and sin must be [%d, %d], got %s and %s" % (rows, d // 2, tuple(cos.shape), tuple(sin.shape)))
+    kp, ks = _rows_of(k, rows, cfg.n_kv_heads, d, dtype)
+    vp, vs = _rows_of(v, rows, cfg.n_kv_heads, d, dtype)
+    qp = qs = heads = out = 0
+    if q is not None:
+        heads = q.shape[1]
+        qp, qs = _rows_of(q, rows, heads, d, dtype)
+        if q_out is None:
+            q_out = q.new_empty((rows, heads, d)) if dtype is torch.float32 else torch.empty((rows, heads, d), dtype=torch.float32, device=q.device)
+        elif q_out.shape != q.shape:
+            raise ValueError("q_out must have q's shape %s, got %s" % (tuple(q.shape), tuple(q_out.shape)))
+        out = _address(q_out, torch.float32)
+    r = NewRows(qp, kp, vp, qs, ks, vs, _ROW_TYPES[dtype], heads, _address(cos, torch.float32), _address(sin, torch.float32), out)
+    return (r, _address(block_table, torch.int32), width, _address(row_starts, torch.int32), _address(seq_lens, torch.int32), batch, rows), q_out
 
 
 def make_config(m, max_batch, max_blocks_per_seq):
@@ -237,31 +289,8 @@ class KVPool:
         k, v [rows, n_kv_heads, head_dim], q [rows, n_q_heads, head_dim]: fp32 or bf16 alike, rows of any stride (slices of a fused
         projection's rows, for one); cos, sin fp32 [rows, head_dim/2] (rope_table); request i brings the rows row_starts[i] ..
         row_starts[i+1]-1 at the positions from seq_lens[i] on.  index: a KVIndex to bring up to date.  Returns the rotated q, fp32."""
-        cfg = self.model.cfg
-        rows, batch, d, dtype = k.shape[0], seq_lens.numel(), cfg.head_dim, k.dtype
-        if dtype not in _ROW_TYPES:
-            raise TypeError("expected torch.float32 or torch.bfloat16, got %s" % dtype)
-        width = block_table.shape[1] if block_table.dim() == 2 else -1
-        if width < 0 or block_table.shape[0] < batch or row_starts.numel() != batch + 1:
-            raise ValueError("%d requests need %d row starts and as many rows of the block table, got %d and %s" % (
-                batch, batch + 1, row_starts.numel(), tuple(block_table.shape)))
-        if cos.numel() != rows * (d // 2) or sin.numel() != cos.numel():
-            raise ValueError("cos and sin must be [%d, %d], got %s and %s" % (rows, d // 2, tuple(cos.shape), tuple(sin.shape)))
-        kp, ks = _rows_of(k, rows, cfg.n_kv_heads, d, dtype)
-        vp, vs = _rows_of(v, rows, cfg.n_kv_heads, d, dtype)
-        qp = qs = heads = out = 0
-        if q is not None:
-            heads = q.shape[1]
-            qp, qs = _rows_of(q, rows, heads, d, dtype)
-            if q_out is None:
-                q_out = q.new_empty((rows, heads, d)) if dtype is torch.float32 else torch.empty((rows, heads, d), dtype=torch.float32, device=q.device)
-            elif q_out.shape != q.shape:
-                raise ValueError("q_out must have q's shape %s, got %s" % (tuple(q.shape), tuple(q_out.shape)))
-            out = _address(q_out, torch.float32)
-        r = NewRows(qp, kp, vp, qs, ks, vs, _ROW_TYPES[dtype], heads, _address(cos, torch.float32), _address(sin, torch.float32), out)
-        _check(load().chiron_append_kv_rope(self._h, index._h if index is not None else None, _whole(layer), C.addressof(r),
-                                            _address(block_table, torch.int32), width, _address(row_starts, torch.int32),
-                                            _address(seq_lens, torch.int32), batch, rows, _stream_number()))
+        args, q_out = _new_rows(self.model.cfg, k, v, cos, sin, block_table, row_starts, seq_lens, q, q_out)
+        _check(load().chiron_append_kv_rope(self._h, index._h if index is not None else None, _whole(layer), C.addressof(args[0]), *args[1:], _stream_number()))
         return q_out
 
     def layer_views(self, layer):
@@ -347,6 +376,119 @@ class KVIndex:
             self.close()
         except Exception:
             pass
+
+
+class KVPool8:
+    """A pool whose keys and values are held in 8 bits ("int8" or "e4m3") with one power of two for each page and KV head, over a
+    torch-allocated byte buffer (the caller owns the memory)."""
+
+    FORMATS = {"int8": (CHIRON_INT8, torch.int8), "e4m3": (CHIRON_E4M3, torch.float8_e4m3fn)}
+
+    def __init__(self, model, num_blocks, format="int8", memory=None):
+        if format not in self.FORMATS:
+            raise ValueError("format must be one of %s, got %r" % (sorted(self.FORMATS), format))
+        self.model, self.format, self.num_blocks, self.block_size = model, format, index(num_blocks), 16
+        need = int(load().chiron_kv8_pool_bytes(model._h, C.c_int32(self.num_blocks)))
+        if memory is None:
+            memory = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+        self.memory = memory
+        self._h = C.c_void_p()
+        _check(load().chiron_kv8_pool_create(model._h, _ptr(memory), C.c_uint64(memory.numel() * memory.element_size()), C.c_int32(self.num_blocks),
+                                             C.c_int32(self.FORMATS[format][0]), C.byref(self._h)))
+
+    def append_rope(self, layer, k, v, cos, sin, block_table, row_starts, seq_lens, q=None, q_out=None):
+        """KVPool.append_rope, with keys and values rounded to the pool's format."""
+        args, q_out = _new_rows(self.model.cfg, k, v, cos, sin, block_table, row_starts, seq_lens, q, q_out)
+        _check(load().chiron_kv8_append_rope(self._h, index(layer), C.addressof(args[0]), *args[1:], _stream_number()))
+        return q_out
+
+    def gather(self, layer, block_table, seq_idx, pos):
+        """Keys and values, bf16 (exact) [n, n_kv_heads, head_dim], of the tokens at pos[j] of row seq_idx[j] of the block table;
+        zeros where there is no page."""
+        cfg, n = self.model.cfg, seq_idx.numel()
+        if block_table.dim() != 2 or pos.numel() != n:
+            raise ValueError("seq_idx and pos must be alike, the block table must have two dimensions")
+        k = torch.empty((n, cfg.n_kv_heads, cfg.head_dim), dtype=torch.bfloat16, device=seq_idx.device)
+        v = torch.empty_like(k)
+        _check(load().chiron_kv8_gather(self._h, index(layer), _address(block_table, torch.int32), block_table.shape[1], _address(seq_idx, torch.int32),
+                                        _address(pos, torch.int32), n, k.data_ptr() or None, v.data_ptr() or None, _stream_number()))
+        return k, v
+
+    def layer_views(self, layer):
+        """The pool's memory of one layer as torch views without a copy: codes of K [page, token, head, d/16, 16] and of V [page, 4, 4 (token),
+        head, d/64, 4, 16], and exponents int8 [page, head, 2 (K, V)]; a value is code * 2^exponent."""
+        cfg, nb, layer = self.model.cfg, self.num_blocks, index(layer)
+        n, d = cfg.n_kv_heads, cfg.head_dim
+        if not 0 <= layer < cfg.n_layers:
+            raise IndexError("layer %d out of range" % layer)
+        codes = nb * n * 32 * d
+        size = (codes + nb * n * 2 + 255) // 256 * 256
+        mem = self.memory.view(torch.uint8).view(-1)[layer * size:(layer + 1) * size]
+        t = mem[:codes].view(self.FORMATS[self.format][1]).view(nb, n, 2, 16 * d)
+        k = t[:, :, 0].unflatten(2, (d // 16, 16, 16)).permute(0, 3, 1, 2, 4)
+        v = t[:, :, 1].unflatten(2, (d // 64, 4, 16, 4, 4)).permute(0, 3, 6, 1, 2, 5, 4)
+        return k, v, mem[codes:codes + nb * n * 2].view(torch.int8).view(nb, n, 2)
+
+    def close(self):
+        if self._h:
+            load().chiron_kv8_pool_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+RowMaps = namedtuple("RowMaps", "row_starts row_seq pos slots granted")
+
+
+class PageList:
+    """The pages that no request uses: pages int32 [capacity], of which the first count[0] (int32 [1]) count.  PageList.of(num_blocks):
+    all pages of a pool."""
+
+    def __init__(self, pages, count):
+        if pages.dim() != 1 or count.numel() != 1:
+            raise ValueError("pages must have one dimension and count one entry, got %s and %s" % (tuple(pages.shape), tuple(count.shape)))
+        _ptr(pages, torch.int32), _ptr(count, torch.int32)  # raise
+        self.pages, self.count = pages, count
+        self._a = PageListArgs(pages.data_ptr(), count.data_ptr(), pages.numel())
+        self._work = {}  # requests -> 4-byte words of workspace
+
+    @classmethod
+    def of(cls, num_blocks, device="cuda"):
+        return cls(torch.arange(num_blocks, dtype=torch.int32, device=device), torch.full((1,), num_blocks, dtype=torch.int32, device=device))
+
+    def _call(self, block_table, first, second):
+        batch = first.numel()
+        if block_table.dim() != 2 or block_table.shape[0] < batch or (second is not None and second.numel() != batch):
+            raise ValueError("the lengths and the block table must have a row for each of %d requests" % batch)
+        need = self._work.get(batch)
+        if need is None:
+            need = self._work[batch] = load().chiron_kv_pages_workspace_bytes(batch) // 4
+        return batch, first.new_empty(need)
+
+    def grant(self, block_table, seq_lens, new_lens, max_rows):
+        """Pages for new_lens[i] new tokens behind the seq_lens[i] of each request (int32 both), written to the empty columns of block_table
+        [requests, width], and the maps of the rows that they bring.  A request that does not fit into max_rows rows, the list or
+        the table waits: it brings no row.  -> RowMaps: row_starts int32 [requests+1]; row_seq (-1 behind the last row), pos int32 and
+        slots int64 [max_rows]; granted int32 [requests]"""
+        batch, work = self._call(block_table, seq_lens, new_lens)
+        max_rows = index(max_rows)
+        rows = max(max_rows, 0)
+        m = RowMaps(seq_lens.new_empty(batch + 1), seq_lens.new_empty(rows), seq_lens.new_empty(rows), seq_lens.new_empty(rows, dtype=torch.int64),
+                    seq_lens.new_empty(batch))
+        maps = RowMapArgs(*[t.data_ptr() or None for t in m])
+        _check(load().chiron_kv_grant_pages(C.addressof(self._a), _address(block_table, torch.int32), block_table.shape[1], _address(seq_lens, torch.int32),
+                                            _address(new_lens, torch.int32), batch, max_rows, C.addressof(maps), work.data_ptr(), _stream_number()))
+        return m
+
+    def release(self, block_table, first, end=None):
+        """Give back the pages that lie wholly within the positions first[i] .. end[i]-1 (all behind first[i] without `end`) of each request."""
+        batch, work = self._call(block_table, first, end)
+        _check(load().chiron_kv_release_pages(C.addressof(self._a), _address(block_table, torch.int32), block_table.shape[1], _address(first, torch.int32),
+                                              _address(end, torch.int32), batch, work.data_ptr(), _stream_number()))
 
 
 def _check_table(model, block_table, batch):
@@ -545,6 +687,40 @@ def op_paged_attention(model, pool, layer, q, block_table, ctx_lens):
     out = torch.empty_like(q)
     _check(load().chiron_op_paged_attention(model._h, pool._h, index(layer), _address(q, torch.float32), _address(block_table, torch.int32),
                                             _address(ctx_lens, torch.int32), B, _address(out), _stream_number()))
+    return out
+
+
+_rows_work = {}  # heads, head dimension, requests, rows, rows of a request -> 4-byte words of workspace
+
+
+def op_row_attention(pool, layer, q, block_table, row_starts, seq_lens, window=0, n_sinks=0, max_new=None, out=None):
+    """Attention of new rows over a KVPool or a KVPool8 that holds their keys and values already.  q [rows, n_q_heads, head_dim] fp32 or bf16,
+    rotated, rows of any 16-byte stride; request i brings the rows row_starts[i] .. row_starts[i+1]-1 (int32 [requests+1]) at the
+    positions from seq_lens[i] on (int32 [requests]).  A row sees the last `window` positions up to its own (0: all) and the first n_sinks.
+    max_new: no request brings more rows (None: as many as there are).  -> out, q's shape and type; rows of no request are left as they were."""
+    cfg, rows, batch, dtype = pool.model.cfg, q.shape[0], seq_lens.numel(), q.dtype
+    if dtype not in _ROW_TYPES:
+        raise TypeError("expected torch.float32 or torch.bfloat16, got %s" % dtype)
+    if q.dim() != 3:
+        raise ValueError("q must be [rows, heads, %d], got %s" % (cfg.head_dim, tuple(q.shape)))
+    if block_table.dim() != 2 or block_table.shape[0] < batch or row_starts.numel() != batch + 1:
+        raise ValueError("%d requests need %d row starts and as many rows of the block table, got %d and %s" % (
+            batch, batch + 1, row_starts.numel(), tuple(block_table.shape)))
+    heads, max_new = q.shape[1], rows if max_new is None else index(max_new)
+    qp, qs = _rows_of(q, rows, heads, cfg.head_dim, dtype)
+    if out is None:
+        out = torch.empty(q.shape, dtype=dtype, device=q.device)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape %s, got %s" % (tuple(q.shape), tuple(out.shape)))
+    key = heads, cfg.n_kv_heads, cfg.head_dim, batch, rows, max_new
+    need = _rows_work.get(key)
+    if need is None:
+        need = _rows_work[key] = load().chiron_row_attention_workspace_bytes(*key) // 4
+    work = seq_lens.new_empty(need)
+    a = AttnRows(qp or None, _address(out, dtype) or None, qs, _ROW_TYPES[dtype], heads, _address(block_table, torch.int32), _address(row_starts, torch.int32),
+                 _address(seq_lens, torch.int32), block_table.shape[1], batch, rows, max_new, index(window), index(n_sinks))
+    call = load().chiron_op_row_attention8 if isinstance(pool, KVPool8) else load().chiron_op_row_attention
+    _check(call(pool._h, index(layer), C.addressof(a), work.data_ptr() or None, _stream_number()))
     return out
 
 

@@ -1,0 +1,998 @@
+// Attention of new rows over the paged cache, bf16 or 8 bits: causal, within a window and over first tokens that stay visible.  gfx950,
+// wave64.
+//
+// Both kernels hold the scores transposed, tokens as rows and (row, query head) pairs of one KV head as columns, 16 x 16 at a time
+// (v_mfma_f32_16x16x32_bf16): a score tile's registers are then the operand that the product with V wants, the running maximum and sum
+// of a softmax belong to a lane's column, and a row's queries that share a KV head share one pass over its pages.  An 8-bit code is
+// widened to bf16 in registers, exactly; its power of two goes to the score (keys) or the weight (values).
+//
+// fp32 queries enter as three bf16 terms, and so do the weights: 24 bits, which keeps fp32's accuracy.  bf16 queries are one term, and so
+// are their weights.
+#include <algorithm>
+#include <cmath>
+
+#include "cache8.h"
+#include "kv_layout.h"
+
+namespace chiron {
+
+struct RowAttnArgs {
+    const uint8_t* tiles;  // the layer's: [num_blocks][n_kv][K tile, V tile]
+    const int8_t* exps;    // 8-bit pools: [num_blocks][n_kv][K, V]
+    const void* q;
+    void* out;
+    int64_t q_stride;  // elements
+    const int32_t *bt, *row_starts, *seq_lens;
+    int64_t window;
+    int num_blocks, n_kv, G, max_blocks, batch, rows, max_new, n_sinks;
+    float scale_log2e;
+    int few_max;      // requests of at most so many rows are row_few_kernel's, the others row_many_kernel's
+    int tg, pcols;    // tokens that share a pass of row_few_kernel, and the columns of a partial result
+    int passes_max;   // no more passes than this
+    int tt, splits;   // tokens of a tile of row_many_kernel, parts of its pages
+    int32_t* head;    // [0]: passes; then a record of four for each pass: first row, tokens, first partial result, partial results
+    float *part_o, *part_ml;
+    float *many_o, *many_ml;
+};
+
+// ---- what a row sees --------------------------------------------------------------------------------------------
+
+// the pages that the positions p0 .. p1 see together, in order: sink_pages from 0 on, then those from lo_page on, n in all (at least one)
+struct Span {
+    int sink_pages, lo_page, n;
+    __device__ int page(int j) const { return j < sink_pages ? j : lo_page + (j - sink_pages); }
+};
+__device__ __forceinline__ int first_seen(const RowAttnArgs& a, int64_t p) {
+    const int64_t lo = p - a.window + 1;
+    return (int)min(max(lo, (int64_t)0), (int64_t)0x7fffffff);
+}
+__device__ __forceinline__ int last_seen(const RowAttnArgs& a, int64_t p) { return (int)min(p, (int64_t)a.max_blocks * kBlockSize - 1); }
+__device__ __forceinline__ Span span_of(const RowAttnArgs& a, int64_t p0, int64_t p1) {
+    Span s;
+    const int end = last_seen(a, p1) / kBlockSize + 1;
+    s.lo_page = min(first_seen(a, p0) / kBlockSize, end);
+    s.sink_pages = min(a.n_sinks / kBlockSize + (a.n_sinks % kBlockSize != 0), s.lo_page);
+    s.n = max(s.sink_pages + end - s.lo_page, 1);
+    return s;
+}
+
+// the columns of a pass or a wave: tokens at the positions first .. last
+struct Seen {
+    int first_lo, last_lo;  // first position in the window of the first and of the last token
+    int first, last;        // last position that the first and the last token see
+};
+__device__ __forceinline__ Seen seen_of(const RowAttnArgs& a, int64_t p0, int64_t p1) {
+    return Seen{first_seen(a, p0), first_seen(a, p1), last_seen(a, p0), last_seen(a, p1)};
+}
+// every column sees all of the page / some column may see some of it
+__device__ __forceinline__ bool all_seen(const RowAttnArgs& a, const Seen& s, int page) {
+    const int t0 = page * kBlockSize, t1 = t0 + kBlockSize - 1;
+    return page >= 0 && t1 <= s.first && (t0 >= s.last_lo || t1 < a.n_sinks);
+}
+__device__ __forceinline__ bool some_seen(const RowAttnArgs& a, const Seen& s, int page) {
+    const int t0 = page * kBlockSize, t1 = t0 + kBlockSize - 1;
+    return page >= 0 && t0 <= s.last && (t1 >= s.first_lo || t0 < a.n_sinks);
+}
+__device__ __forceinline__ bool sees(const RowAttnArgs& a, int lo, int last, int tok) { return tok <= last && (tok >= lo || tok < a.n_sinks); }
+
+// masks of the bf16 pairs (0, 1) and (2, 3), or of the bytes, of the tokens tok .. tok+3 that some column sees
+__device__ __forceinline__ uint4 seen_masks(const RowAttnArgs& a, const Seen& s, bool there, int tok) {
+    bool v[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = there && sees(a, s.first_lo, s.last, tok + r);
+    const uint32_t bytes = (v[0] ? 0xffu : 0) | (v[1] ? 0xff00u : 0) | (v[2] ? 0xff0000u : 0) | (v[3] ? 0xff000000u : 0);
+    return make_uint4((v[0] ? 0xffffu : 0) | (v[1] ? 0xffff0000u : 0), (v[2] ? 0xffffu : 0) | (v[3] ? 0xffff0000u : 0), bytes, 0);
+}
+
+// ---- operands ---------------------------------------------------------------------------------------------------
+
+template <int FMT>
+__host__ __device__ constexpr int pieces(int D) { return FMT == kFmtBf16 ? D / 32 : D / 64; }  // of 16 bytes per lane: a K or V tile
+// the first of the 8 dims that a lane's operand of the 32 dims of step s holds
+template <int FMT>
+__device__ __forceinline__ int dim_of(int s, int lg) { return FMT == kFmtBf16 ? s * 32 + lg * 8 : s / 2 * 64 + lg * 16 + s % 2 * 8; }
+template <int FMT, int N>
+__device__ __forceinline__ bf16x8 key_operand(const uint4 (&k)[N], int s) {
+    uint4 w;
+    if (FMT == kFmtBf16) w = k[s];
+    else {
+        const uint4 c = k[s / 2];
+        const uint2 a = widen8<FMT>(s % 2 ? c.z : c.x), b = widen8<FMT>(s % 2 ? c.w : c.y);
+        w = make_uint4(a.x, a.y, b.x, b.y);
+    }
+    return *reinterpret_cast<bf16x8*>(&w);
+}
+__device__ __forceinline__ uint32_t word(const uint4& w, int j) { return j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w; }
+// the i-th of the three bf16 terms of v
+__device__ __forceinline__ float term3(float v, int i) {
+    const float hi = bf16_lo(pack_bf16_rne(v, 0.f)), r1 = v - hi, mid = bf16_lo(pack_bf16_rne(r1, 0.f));
+    return i == 0 ? hi : i == 1 ? mid : r1 - mid;
+}
+// NaN and infinities among two bf16: which (as bf16 ones), and the word without them
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+    return ((w & 0x7f80u) == 0x7f80u ? 0x3f80u : 0) | ((w & 0x7f800000u) == 0x7f800000u ? 0x3f800000u : 0);
+}
+__device__ __forceinline__ uint32_t without(uint32_t w, uint32_t ones) { return w & ~((ones & 0x80u ? 0xffffu : 0) | (ones & 0x800000u ? 0xffff0000u : 0)); }
+
+__device__ __forceinline__ floatx4 mfma32(bf16x8 a, bf16x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ floatx4 mfma16(uint2 a, uint2 b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(*reinterpret_cast<short4v*>(&a), *reinterpret_cast<short4v*>(&b), c, 0, 0, 0);
+}
+
+// a request's rows, as the kernels take them: 0 rows where the row starts do not ascend
+struct Request {
+    int r0, n;
+    int64_t old;
+};
+__device__ __forceinline__ Request request(const RowAttnArgs& a, int i) {
+    Request r;
+    r.r0 = a.row_starts[i];
+    const int r1 = a.row_starts[i + 1];
+    r.n = r.r0 < 0 || r1 > a.rows || r1 <= r.r0 ? 0 : min(r1 - r.r0, a.max_new);
+    r.old = max(a.seq_lens[i], 0);
+    return r;
+}
+
+template <int D, bool F32>
+__device__ __forceinline__ void store_row(const RowAttnArgs& a, int64_t row, int qhead, int e, floatx4 o) {
+    const int64_t at = (row * a.n_kv * a.G + qhead) * D + e;
+    if (F32) *reinterpret_cast<floatx4*>((float*)a.out + at) = o;
+    else *reinterpret_cast<uint2*>((uint16_t*)a.out + at) = make_uint2(pack_bf16_rne(o[0], o[1]), pack_bf16_rne(o[2], o[3]));
+}
+
+// ---- requests of a few rows ---------------------------------------------------------------------------------------
+// A pass: up to tg tokens of a request whose heads of one KV head fit the 16 columns; it reads the pages they see once, straight into operand
+// registers.  The pages of all passes, one behind the other, are dealt out in equal shares to the waves of a KV head, whatever the requests'
+// lengths: a wave finds its share from sums over the requests' lengths, 64 at a time, and may end one pass and begin others.  A pass
+// that lies in several shares leaves partial results (maximum, sum, unnormalised output), which row_few_merge_kernel joins; partial result
+// w + v is wave w's of pass v, a number of its own for each pair that exists.
+//
+// CW: columns of a term group.  Three terms of up to 4 columns share one instruction, of up to 8 two.
+constexpr int kFewMinPages = 8;  // of a share
+template <int D, int FMT, bool F32, int CW>
+__global__ __launch_bounds__(256, 2) void row_few_kernel(RowAttnArgs a) {
+    constexpr int KSTEPS = D / 32, P = pieces<FMT>(D), NPG = FMT == kFmtBf16 && D == 128 ? 2 : 4;
+    constexpr int NT = F32 ? 3 : 1, TPI = F32 ? (16 / CW < 3 ? 16 / CW : 3) : 1, NI = (NT + TPI - 1) / TPI;
+    constexpr int TILE = FMT == kFmtBf16 ? 32 * D : 16 * D;  // bytes of a K or V tile
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n_kv = a.n_kv, c = blockIdx.x % n_kv, w = blockIdx.x / n_kv * 4 + wave, W = gridDim.x / n_kv * 4;
+    const int col = lane & 15, lg = lane >> 4, ci = col % CW, grp = col / CW;
+    const int tq = ci / a.G, h = ci - tq * a.G;
+
+    // a lane's request of the 64 from i0 on: pages over its passes, and passes
+    auto look = [&](int i0, Request& r, int& cost, int& np) {
+        cost = np = 0;
+        if (i0 + lane < a.batch) {
+            r = request(a, i0 + lane);
+            if (r.n > 0 && r.n <= a.few_max) {
+                np = (r.n + a.tg - 1) / a.tg;
+                for (int g = 0; g < np; ++g) cost += span_of(a, r.old + g * a.tg, r.old + min((g + 1) * a.tg, r.n) - 1).n;
+            }
+        }
+    };
+    int64_t total = 0;
+    int n_pass = 0;
+    Request rq;
+    int cost, np;
+    for (int i0 = 0; i0 < a.batch; i0 += 64) {
+        look(i0, rq, cost, np);
+        total += wave_total(cost);
+        n_pass += wave_total(np);
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.head[0] = n_pass;
+    int64_t share64 = max((total + W - 1) / W, (int64_t)kFewMinPages);
+    const int share = (int)((share64 + NPG - 1) / NPG * NPG);
+    const int64_t begin = (int64_t)w * share, end = min(begin + share, total);
+    if (begin >= end) return;
+
+    int64_t base = 0, at = begin;
+    int vbase = 0;
+    for (int i0 = 0; i0 < a.batch && at < end; i0 += 64) {
+        look(i0, rq, cost, np);
+        const int incl = wave_scan(cost), vincl = wave_scan(np);
+        const int all = __builtin_amdgcn_readlane(incl, 63);
+        uint64_t ahead = __ballot(base + incl > at && cost > 0);
+        while (ahead && at < end) {
+            const int L = __builtin_ctzll(ahead);
+            ahead &= ahead - 1;
+            const int row0 = __builtin_amdgcn_readlane(rq.r0, L), n = __builtin_amdgcn_readlane(rq.n, L);
+            const int64_t old = __builtin_amdgcn_readlane((int)rq.old, L);
+            const int passes = __builtin_amdgcn_readlane(np, L);
+            int64_t first = base + __builtin_amdgcn_readlane(incl, L) - __builtin_amdgcn_readlane(cost, L);
+            int v = vbase + __builtin_amdgcn_readlane(vincl, L) - passes;
+            for (int g = 0; g < passes && at < end; ++g, ++v) {
+                const int t0 = g * a.tg, tv = min(a.tg, n - t0);
+                const Span span = span_of(a, old + t0, old + t0 + tv - 1);
+                const int64_t pass0 = first;
+                first += span.n;
+                if (first <= at) continue;
+                const int j0 = (int)(at - pass0), j1 = (int)min((int64_t)span.n, end - pass0);
+                at = pass0 + j1;
+                const int seg0 = (int)(pass0 / share), segs = (int)((first - 1) / share) - seg0 + 1;
+                if (j0 == 0 && c == 0 && lane == 0)
+                    *reinterpret_cast<int4*>(a.head + 4 + 4 * (size_t)v) = make_int4(row0 + t0, tv, seg0 + v, segs);
+
+                // ---- the pages j0 .. j1-1 of pass v
+                const int cols = a.G * tv;
+                const bool on = ci < cols;
+                const Seen seen = seen_of(a, old + t0, old + t0 + tv - 1);
+                const int64_t pos = old + t0 + min(tq, tv - 1);
+                const int col_lo = first_seen(a, pos), col_last = last_seen(a, pos);
+                const int32_t* btrow = a.bt + (size_t)(i0 + L) * a.max_blocks;
+
+                // lane l holds entry lbase + l of the span: the page, where it is in the pool, its powers of two
+                int lbase = j0, v_page, v_block, v_exp = 0;
+                auto fetch = [&] {
+                    const int j = lbase + lane;
+                    int pg = j < j1 ? span.page(j) : -1, blk = -1;
+                    if (pg >= 0 && pg < a.max_blocks) blk = btrow[pg];
+                    if (blk < 0 || blk >= a.num_blocks) pg = -1, blk = 0;  // nothing there: page 0 of the pool is read and masked
+                    v_page = pg;
+                    v_block = blk;
+                    if (FMT != kFmtBf16) v_exp = *reinterpret_cast<const uint16_t*>(a.exps + ((int64_t)blk * n_kv + c) * 2);
+                };
+                struct Stage {
+                    uint4 k[NPG][P], v[NPG][P];
+                    int page[NPG], exp[NPG];
+                };
+                auto load = [&](int j, Stage& s) {
+                    if (j - lbase >= 64) {  // uniform; 64 is a multiple of NPG
+                        lbase = j;
+                        fetch();
+                    }
+#pragma unroll
+                    for (int u = 0; u < NPG; ++u) {
+                        const bool there = j + u < j1;
+                        const int l = (j + u - lbase) & 63;
+                        s.page[u] = there ? __builtin_amdgcn_readlane(v_page, l) : -1;
+                        const int blk = there ? __builtin_amdgcn_readlane(v_block, l) : 0;
+                        s.exp[u] = FMT == kFmtBf16 || !there ? 0 : __builtin_amdgcn_readlane(v_exp, l);
+                        const uint8_t* tile = a.tiles + ((int64_t)blk * n_kv + c) * (2 * TILE) + lane * 16;
+#pragma unroll
+                        for (int i = 0; i < P; ++i) {
+                            s.k[u][i] = load_stream_16(tile + i * 1024);
+                            s.v[u][i] = load_stream_16(tile + TILE + i * 1024);
+                        }
+                    }
+                };
+                uint4 qt[NI][KSTEPS];
+                floatx4 o[D / 16];
+#pragma unroll
+                for (int t = 0; t < D / 16; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+                float m_run = -INFINITY, l_run = 0.f;
+
+                auto compute = [&](Stage& s) {
+                    bool full = true;
+#pragma unroll
+                    for (int u = 0; u < NPG; ++u) full = full && all_seen(a, seen, s.page[u]);
+                    floatx4 x[NPG];
+                    float vs[NPG];
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int u = 0; u < NPG; ++u) {
+                        x[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int k = 0; k < KSTEPS; ++k) {
+                            const bf16x8 key = key_operand<FMT>(s.k[u], k);
+#pragma unroll
+                            for (int i = 0; i < NI; ++i) x[u] = mfma32(key, *reinterpret_cast<bf16x8*>(&qt[i][k]), x[u]);
+                        }
+                        float ks = F32 ? 1.f : a.scale_log2e;
+                        vs[u] = 1.f;
+                        if (FMT != kFmtBf16) {
+                            ks *= two_to((int8_t)(s.exp[u] & 0xff));
+                            vs[u] = two_to((int8_t)(s.exp[u] >> 8));
+                        }
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {  // the sum over the term groups, in every column
+                            if (TPI > 1) x[u][r] += row_move<kRor8>(x[u][r]);
+                            if (TPI > 1 && CW <= 4) x[u][r] += row_move<kRor4>(x[u][r]);
+                            if (!F32 || FMT != kFmtBf16) x[u][r] *= ks;
+                        }
+                    }
+                    if (!full) {
+#pragma unroll
+                        for (int u = 0; u < NPG; ++u) {
+                            const bool there = s.page[u] >= 0;
+                            const int tok = max(s.page[u], 0) * kBlockSize + lg * 4;
+                            if (!there) vs[u] = 0.f;
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) x[u][r] = there && sees(a, col_lo, col_last, tok + r) ? x[u][r] : -INFINITY;
+                            // what no column sees may hold anything, NaN included: clear its V so that 0 * V stays 0
+                            const uint4 keep = seen_masks(a, seen, there, tok);
+#pragma unroll
+                            for (int i = 0; i < P; ++i) {
+                                uint4& v = s.v[u][i];
+                                if (FMT == kFmtBf16) v.x &= keep.x, v.y &= keep.y, v.z &= keep.x, v.w &= keep.y;
+                                else v.x &= keep.z, v.y &= keep.z, v.z &= keep.z, v.w &= keep.z;
+                            }
+                        }
+                        // what some columns see and others do not must not reach these: 0 * NaN
+                        if (FMT == kFmtBf16 && tv > 1) {
+                            uint32_t bad = 0;
+#pragma unroll
+                            for (int u = 0; u < NPG; ++u)
+#pragma unroll
+                                for (int i = 0; i < P; ++i)
+                                    bad |= not_finite(s.v[u][i].x) | not_finite(s.v[u][i].y) | not_finite(s.v[u][i].z) | not_finite(s.v[u][i].w);
+                            if (__any(bad != 0)) {
+#pragma unroll
+                                for (int u = 0; u < NPG; ++u) {
+                                    const int tok = max(s.page[u], 0) * kBlockSize + lg * 4;
+                                    uint32_t on4[4];
+#pragma unroll
+                                    for (int r = 0; r < 4; ++r) on4[r] = s.page[u] >= 0 && sees(a, col_lo, col_last, tok + r) ? 0x3f80u : 0;
+                                    const uint2 vis = make_uint2(on4[0] | on4[1] << 16, on4[2] | on4[3] << 16);
+#pragma unroll
+                                    for (int b = 0; b < D / 16; ++b) {
+                                        uint4& v = s.v[u][b / 2 % P];
+                                        uint32_t &w0 = b % 2 ? v.z : v.x, &w1 = b % 2 ? v.w : v.y;
+                                        const uint2 ones = make_uint2(not_finite(w0), not_finite(w1));
+                                        w0 = without(w0, ones.x);
+                                        w1 = without(w1, ones.y);
+                                        const floatx4 met = mfma16(ones, vis, floatx4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                                        for (int r = 0; r < 4; ++r) o[b][r] = met[r] > 0.f ? NAN : o[b][r];
+                                    }
+                                }
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < NPG; ++u)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[u][r]);
+                    mx = fmaxf(mx, __shfl_xor(mx, 16));
+                    mx = fmaxf(mx, __shfl_xor(mx, 32));
+                    const float m_new = fmaxf(m_run, mx), m_use = fmaxf(m_new, -1e30f);  // nothing seen yet: finite exponents, weights 0
+                    const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+                    m_run = m_new;
+                    l_run *= alpha;
+#pragma unroll
+                    for (int t = 0; t < D / 16; ++t) o[t] *= alpha;
+#pragma unroll
+                    for (int u = 0; u < NPG; u += 2) {
+                        float pr[2][4];
+#pragma unroll
+                        for (int z = 0; z < 2; ++z)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                pr[z][r] = __builtin_amdgcn_exp2f(x[u + z][r] - m_use);
+                                l_run += pr[z][r];
+                                if (FMT != kFmtBf16) pr[z][r] *= vs[u + z];
+                            }
+                        uint4 pt[NI];
+#pragma unroll
+                        for (int i = 0; i < NI; ++i) {
+                            float y[2][4];
+#pragma unroll
+                            for (int z = 0; z < 2; ++z)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) {
+                                    const int t = i * TPI + grp;
+                                    y[z][r] = !F32 ? pr[z][r] : TPI == 1 ? term3(pr[z][r], i) : grp >= TPI || t > 2 ? 0.f : term3(pr[z][r], t);
+                                }
+                            pt[i] = make_uint4(pack_bf16_rne(y[0][0], y[0][1]), pack_bf16_rne(y[0][2], y[0][3]), pack_bf16_rne(y[1][0], y[1][1]),
+                                               pack_bf16_rne(y[1][2], y[1][3]));
+                        }
+#pragma unroll
+                        for (int b = 0; b < D / 16; ++b) {
+                            if (FMT == kFmtBf16) {
+                                const uint4 &va = s.v[u][b / 2 % P], &vb = s.v[u + 1][b / 2 % P];
+                                const uint2 v0 = b % 2 ? make_uint2(va.z, va.w) : make_uint2(va.x, va.y);
+                                const uint2 v1 = b % 2 ? make_uint2(vb.z, vb.w) : make_uint2(vb.x, vb.y);
+#pragma unroll
+                                for (int i = 0; i < NI; ++i) {
+                                    o[b] = mfma16(v0, make_uint2(pt[i].x, pt[i].y), o[b]);
+                                    o[b] = mfma16(v1, make_uint2(pt[i].z, pt[i].w), o[b]);
+                                }
+                            } else {
+                                const uint2 v0 = widen8<FMT>(word(s.v[u][b / 4 % P], b % 4)), v1 = widen8<FMT>(word(s.v[u + 1][b / 4 % P], b % 4));
+                                uint4 v = make_uint4(v0.x, v0.y, v1.x, v1.y);
+#pragma unroll
+                                for (int i = 0; i < NI; ++i) o[b] = mfma32(*reinterpret_cast<bf16x8*>(&v), *reinterpret_cast<bf16x8*>(&pt[i]), o[b]);
+                            }
+                        }
+                    }
+                };
+
+                Stage sa, sb;
+                fetch();
+                load(j0, sa);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int s = 0; s < KSTEPS; ++s) {
+                    const int64_t qrow = row0 + t0 + min(tq, tv - 1);
+                    const int64_t qat = qrow * a.q_stride + (int64_t)(c * a.G + h) * D + dim_of<FMT>(s, lg);
+                    if (F32) {
+                        const float* qp = (const float*)a.q + qat;
+                        const float4 y0 = *reinterpret_cast<const float4*>(qp), y1 = *reinterpret_cast<const float4*>(qp + 4);
+                        float y[8] = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
+#pragma unroll
+                        for (int i = 0; i < NI; ++i) {
+                            float z[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const int t = i * TPI + grp;
+                                z[e] = !on || grp >= TPI || t > 2 ? 0.f : term3(y[e] * a.scale_log2e, t);
+                            }
+                            qt[i][s] = make_uint4(pack_bf16_rne(z[0], z[1]), pack_bf16_rne(z[2], z[3]), pack_bf16_rne(z[4], z[5]), pack_bf16_rne(z[6], z[7]));
+                        }
+                    } else {
+                        const uint4 y = *reinterpret_cast<const uint4*>((const uint16_t*)a.q + qat);
+                        qt[0][s] = on ? y : make_uint4(0, 0, 0, 0);
+                    }
+                }
+                for (int j = j0;;) {
+                    if (j + NPG < j1) load(j + NPG, sb);
+                    __builtin_amdgcn_sched_barrier(0);
+                    compute(sa);
+                    __builtin_amdgcn_sched_barrier(0);
+                    j += NPG;
+                    if (j >= j1) break;
+                    if (j + NPG < j1) load(j + NPG, sa);
+                    __builtin_amdgcn_sched_barrier(0);
+                    compute(sb);
+                    __builtin_amdgcn_sched_barrier(0);
+                    j += NPG;
+                    if (j >= j1) break;
+                }
+
+                l_run += __shfl_xor(l_run, 16);
+                l_run += __shfl_xor(l_run, 32);
+                if (TPI > 1) {
+#pragma unroll
+                    for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            o[t][r] += row_move<kRor8>(o[t][r]);
+                            if (CW <= 4) o[t][r] += row_move<kRor4>(o[t][r]);
+                        }
+                }
+                if (grp == 0 && on) {
+                    if (segs == 1) {
+                        const float den = l_run > 0.f || l_run != l_run ? l_run : 1.f;
+#pragma unroll
+                        for (int t = 0; t < D / 16; ++t)
+                            store_row<D, F32>(a, row0 + t0 + tq, c * a.G + h, t * 16 + lg * 4, floatx4{o[t][0] / den, o[t][1] / den, o[t][2] / den, o[t][3] / den});
+                    } else {
+                        const int64_t slot = ((int64_t)(w + v) * n_kv + c) * a.pcols + ci;
+                        if (lg == 0) {
+                            a.part_ml[slot * 2] = fmaxf(m_run, -1e30f);
+                            a.part_ml[slot * 2 + 1] = l_run;
+                        }
+#pragma unroll
+                        for (int t = 0; t < D / 16; ++t) *reinterpret_cast<floatx4*>(a.part_o + slot * D + t * 16 + lg * 4) = o[t];
+                    }
+                }
+            }
+        }
+        base += all;
+        vbase += __builtin_amdgcn_readlane(vincl, 63);
+    }
+}
+
+// joins the partial results of a pass: a workgroup per (pass, KV head, column), in slices of 32 (D = 128) or 16 lanes, in a fixed order
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void row_few_merge_kernel(RowAttnArgs a) {
+    constexpr int LANES = D / 4, S = 256 / LANES;
+    __shared__ floatx4 s_num[S][LANES];
+    __shared__ float s_den[S], s_max[S];
+    const int col = blockIdx.x % a.pcols, vc = blockIdx.x / a.pcols, c = vc % a.n_kv, v = vc / a.n_kv;
+    if (v >= a.head[0]) return;
+    const int4 rec = *reinterpret_cast<const int4*>(a.head + 4 + 4 * (size_t)v);
+    if (rec.w <= 1 || col >= a.G * rec.y) return;
+    const int sl = threadIdx.x / LANES, ln = threadIdx.x % LANES;
+    float M = -1e30f, den = 0.f;
+    floatx4 num = {0.f, 0.f, 0.f, 0.f};
+    for (int j = sl; j < rec.w; j += S) {
+        const int64_t slot = ((int64_t)(rec.z + j) * a.n_kv + c) * a.pcols + col;
+        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + slot * 2);
+        const floatx4 o = *reinterpret_cast<const floatx4*>(a.part_o + slot * D + ln * 4);
+        const float Mn = fmaxf(M, ml.x), f0 = __builtin_amdgcn_exp2f(M - Mn), f1 = __builtin_amdgcn_exp2f(ml.x - Mn);
+        num = num * f0 + o * f1;
+        den = den * f0 + ml.y * f1;
+        M = Mn;
+    }
+    s_num[sl][ln] = num;
+    if (ln == 0) {
+        s_den[sl] = den;
+        s_max[sl] = M;
+    }
+    __syncthreads();
+    if (sl != 0) return;
+#pragma unroll
+    for (int j = 1; j < S; ++j) M = fmaxf(M, s_max[j]);
+    num = floatx4{0.f, 0.f, 0.f, 0.f};
+    den = 0.f;
+#pragma unroll
+    for (int j = 0; j < S; ++j) {
+        const float f = __builtin_amdgcn_exp2f(s_max[j] - M);
+        num += s_num[j][ln] * f;
+        den += s_den[j] * f;
+    }
+    const int tq = col / a.G, h = col - tq * a.G;
+    if (!(den > 0.f) && den == den) den = 1.f;
+    store_row<D, F32>(a, (int64_t)rec.x + tq, c * a.G + h, ln * 4, floatx4{num[0] / den, num[1] / den, num[2] / den, num[3] / den});
+}
+
+// ---- requests of many rows ----------------------------------------------------------------------------------------
+// A workgroup takes a tile of tt tokens x G heads of one KV head, up to 128 columns, 32 of them a wave's, and goes through the pages
+// that they see together, four at a time: each wave brings one page into LDS, as bf16 in operand order, while the four before are multiplied.
+// A column group's maxima, sums and outputs stay in registers.  Tiles with the most pages begin first.  Where there are few tiles
+// the pages of each are dealt to `splits` workgroups.
+constexpr int kManyCols = 128, kManyTiles = 2;  // columns of a workgroup; column tiles of a wave
+struct ManyTile {
+    int r0, t0, tv, req;
+    int64_t old;
+};
+// which tile a slot is: request i owns the slots from row_starts[i]/tt + i on; by a whole wave
+__device__ __forceinline__ bool many_tile(const RowAttnArgs& a, int slot, ManyTile& m) {
+    const int lane = threadIdx.x & 63;
+    int req = -1;
+    for (int i0 = 0; i0 < a.batch; i0 += 64) {
+        const int i = min(i0 + lane, a.batch - 1);
+        const uint64_t begun = __ballot(i0 + lane < a.batch && a.row_starts[i] / a.tt + i <= slot);
+        req += __popcll(begun);
+        if (begun != ~(uint64_t)0) break;
+    }
+    if (req < 0) return false;
+    const Request r = request(a, req);
+    const int tiles = (r.n + a.tt - 1) / a.tt, local = slot - (r.r0 / a.tt + req);
+    if (r.n <= a.few_max || local < 0 || local >= tiles) return false;
+    m.req = req;
+    m.r0 = r.r0;
+    m.old = r.old;
+    m.t0 = (tiles - 1 - local) * a.tt;  // the last tokens see the most
+    m.tv = min(a.tt, r.n - m.t0);
+    return true;
+}
+
+template <int D, int FMT, bool F32>
+__global__ __launch_bounds__(256, F32 ? 1 : 2) void row_many_kernel(RowAttnArgs a) {
+    constexpr int KSTEPS = D / 32, P = pieces<FMT>(D), NB = D / 16, NC = kManyTiles, NT = F32 ? 3 : 1;
+    constexpr int TILE = FMT == kFmtBf16 ? 32 * D : 16 * D;
+    __shared__ uint4 s_k[2][4][KSTEPS][64];  // [buffer][page][step][lane]
+    __shared__ uint4 s_v[2][2][NB][64];      // [buffer][pair of pages][16 dims][lane]: 4 tokens of either page
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n_kv = a.n_kv, c = blockIdx.x % n_kv, rest = blockIdx.x / n_kv, split = rest % a.splits, slot = rest / a.splits;
+    const int col = lane & 15, lg = lane >> 4;
+    ManyTile m;
+    if (!many_tile(a, slot, m)) return;
+    const int live = a.G * m.tv;
+    const Span span = span_of(a, m.old + m.t0, m.old + m.t0 + m.tv - 1);
+    const Seen tile_seen = seen_of(a, m.old + m.t0, m.old + m.t0 + m.tv - 1);
+    const int stages = (span.n + 3) / 4, st0 = (int)((int64_t)stages * split / a.splits), st1 = (int)((int64_t)stages * (split + 1) / a.splits);
+    const int32_t* btrow = a.bt + (size_t)m.req * a.max_blocks;
+
+    // the wave's columns
+    const int wc = wave * 16 * NC;
+    const bool idle = wc >= live;
+    const int64_t pw = m.old + m.t0;
+    const Seen seen = seen_of(a, pw + min(wc / a.G, m.tv - 1), pw + min((wc + 16 * NC - 1) / a.G, m.tv - 1));
+    int col_lo[NC], col_last[NC];
+    uint4 qt[NC][NT][KSTEPS];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+        const int ci = wc + n * 16 + col, tq = min(ci / a.G, m.tv - 1), h = ci % a.G;
+        col_lo[n] = first_seen(a, pw + tq);
+        col_last[n] = last_seen(a, pw + tq);
+#pragma unroll
+        for (int s = 0; s < KSTEPS; ++s) {
+            // 8-bit keys lie in LDS as the bf16 pool's do, step for step
+            const int64_t qat = (int64_t)(m.r0 + m.t0 + tq) * a.q_stride + (int64_t)(c * a.G + h) * D + dim_of<FMT>(s, lg);
+            if (F32) {
+                const float* qp = (const float*)a.q + qat;
+                const float4 y0 = *reinterpret_cast<const float4*>(qp), y1 = *reinterpret_cast<const float4*>(qp + 4);
+                const float y[8] = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    float z[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = ci < live ? term3(y[e] * a.scale_log2e, i) : 0.f;
+                    qt[n][i][s] = make_uint4(pack_bf16_rne(z[0], z[1]), pack_bf16_rne(z[2], z[3]), pack_bf16_rne(z[4], z[5]), pack_bf16_rne(z[6], z[7]));
+                }
+            } else {
+                const uint4 y = *reinterpret_cast<const uint4*>((const uint16_t*)a.q + qat);
+                qt[n][0][s] = ci < live ? y : make_uint4(0, 0, 0, 0);
+            }
+        }
+    }
+    floatx4 o[NC][NB];
+    float m_run[NC], l_run[NC];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+        m_run[n] = -INFINITY;
+        l_run[n] = 0.f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) o[n][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    // lane l holds entry lbase + l of the span
+    int lbase = st0 * 4, v_page, v_block, v_exp = 0;
+    auto fetch = [&] {
+        const int j = lbase + lane;
+        int pg = j < span.n ? span.page(j) : -1, blk = -1;
+        if (pg >= 0 && pg < a.max_blocks) blk = btrow[pg];
+        if (blk < 0 || blk >= a.num_blocks) pg = -1, blk = 0;
+        v_page = pg;
+        v_block = blk;
+        if (FMT != kFmtBf16) v_exp = *reinterpret_cast<const uint16_t*>(a.exps + ((int64_t)blk * n_kv + c) * 2);
+    };
+    uint4 rk[P], rv[P];  // the wave's page of the stage that comes next
+    int r_page = -1, r_exp = 0, pages[4], next_pages[4];
+    auto load = [&](int st) {
+        if (st * 4 - lbase >= 64) {
+            lbase = st * 4;
+            fetch();
+        }
+        const int l = st * 4 - lbase;  // 4 divides 64
+#pragma unroll
+        for (int u = 0; u < 4; ++u) next_pages[u] = __builtin_amdgcn_readlane(v_page, l + u);
+        r_page = __builtin_amdgcn_readlane(v_page, l + wave);
+        r_exp = __builtin_amdgcn_readlane(v_exp, l + wave);
+        const uint8_t* tile = a.tiles + ((int64_t)__builtin_amdgcn_readlane(v_block, l + wave) * n_kv + c) * (2 * TILE) + lane * 16;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            rk[i] = *reinterpret_cast<const uint4*>(tile + i * 1024);
+            rv[i] = *reinterpret_cast<const uint4*>(tile + TILE + i * 1024);
+        }
+    };
+    auto put = [&](int buf) {
+        if (!all_seen(a, tile_seen, r_page)) {  // what no column of the tile sees may hold anything
+            const uint4 keep = seen_masks(a, tile_seen, r_page >= 0, max(r_page, 0) * kBlockSize + lg * 4);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                uint4& v = rv[i];
+                if (FMT == kFmtBf16) v.x &= keep.x, v.y &= keep.y, v.z &= keep.x, v.w &= keep.y;
+                else v.x &= keep.z, v.y &= keep.z, v.z &= keep.z, v.w &= keep.z;
+            }
+        }
+        const float ks = two_to((int8_t)(r_exp & 0xff)), vs = r_page >= 0 ? two_to((int8_t)(r_exp >> 8)) : 0.f;
+        uint2* dv = reinterpret_cast<uint2*>(&s_v[buf][wave / 2][0][lane]) + wave % 2;
+        auto widened = [&](uint32_t w, float scale) {  // exact: the value is a bf16 number
+            const floatx4 f = decode8<FMT>(w) * scale;
+            return make_uint2(__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302),
+                              __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302));
+        };
+#pragma unroll
+        for (int s = 0; s < KSTEPS; ++s) {
+            if (FMT == kFmtBf16) s_k[buf][wave][s][lane] = rk[s % P];
+            else {
+                const uint2 x = widened(word(rk[s / 2], s % 2 * 2), ks), y = widened(word(rk[s / 2], s % 2 * 2 + 1), ks);
+                s_k[buf][wave][s][lane] = make_uint4(x.x, x.y, y.x, y.y);
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            if (FMT == kFmtBf16) {
+                const uint4 v = rv[b / 2 % P];
+                dv[b * 128] = b % 2 ? make_uint2(v.z, v.w) : make_uint2(v.x, v.y);
+            } else dv[b * 128] = widened(word(rv[b / 4], b % 4), vs);
+        }
+    };
+
+    auto compute = [&](int buf) {
+        bool full = true, any = false;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            full = full && all_seen(a, seen, pages[u]);
+            any = any || some_seen(a, seen, pages[u]);
+        }
+        if (idle || !any) return;
+        floatx4 x[NC][4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+#pragma unroll
+            for (int n = 0; n < NC; ++n) x[n][u] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < KSTEPS; ++s) {
+                uint4 kw = s_k[buf][u][s][lane];
+#pragma unroll
+                for (int n = 0; n < NC; ++n)
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) x[n][u] = mfma32(*reinterpret_cast<bf16x8*>(&kw), *reinterpret_cast<bf16x8*>(&qt[n][i][s]), x[n][u]);
+            }
+        }
+        uint32_t vis[NC];  // four bits a page
+#pragma unroll
+        for (int n = 0; n < NC; ++n) vis[n] = 0xffff;
+        if (!full) {
+#pragma unroll
+            for (int n = 0; n < NC; ++n) {
+                vis[n] = 0;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int tok = max(pages[u], 0) * kBlockSize + lg * 4;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const bool v = pages[u] >= 0 && sees(a, col_lo[n], col_last[n], tok + r);
+                        x[n][u][r] = v ? x[n][u][r] : -INFINITY;
+                        vis[n] |= v ? 1u << (4 * u + r) : 0;
+                    }
+                }
+            }
+        }
+        uint4 pt[NC][NT][2];
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[n][u][r]);
+            mx = fmaxf(mx, __shfl_xor(mx, 16));
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            if (!F32) mx *= a.scale_log2e;
+            const float m_new = fmaxf(m_run[n], mx), m_use = fmaxf(m_new, -1e30f);
+            if (__any(m_new > m_run[n])) {
+                const float alpha = __builtin_amdgcn_exp2f(m_run[n] - m_use);
+                l_run[n] *= alpha;
+#pragma unroll
+                for (int b = 0; b < NB; ++b) o[n][b] *= alpha;
+            }
+            m_run[n] = m_new;
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                float p[2][4];
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float s = x[n][2 * z + y][r];
+                        p[y][r] = __builtin_amdgcn_exp2f(F32 ? s - m_use : fmaf(s, a.scale_log2e, -m_use));
+                        l_run[n] += p[y][r];
+                    }
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    float t[2][4];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) t[y][r] = F32 ? term3(p[y][r], i) : p[y][r];
+                    pt[n][i][z] = make_uint4(pack_bf16_rne(t[0][0], t[0][1]), pack_bf16_rne(t[0][2], t[0][3]), pack_bf16_rne(t[1][0], t[1][1]),
+                                             pack_bf16_rne(t[1][2], t[1][3]));
+                }
+            }
+        }
+#pragma unroll
+        for (int z = 0; z < 2; ++z)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                uint4 vw = s_v[buf][z][b][lane];
+                if (FMT == kFmtBf16 && !full) {  // what some columns see and others do not must not reach these: 0 * NaN
+                    const uint4 ones = make_uint4(not_finite(vw.x), not_finite(vw.y), not_finite(vw.z), not_finite(vw.w));
+                    if (__any((ones.x | ones.y | ones.z | ones.w) != 0)) {
+                        vw = make_uint4(without(vw.x, ones.x), without(vw.y, ones.y), without(vw.z, ones.z), without(vw.w, ones.w));
+#pragma unroll
+                        for (int n = 0; n < NC; ++n) {
+                            uint32_t on[4];
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const uint32_t two = vis[n] >> (8 * z + 2 * r) & 3;
+                                on[r] = (two & 1 ? 0x3f80u : 0) | (two & 2 ? 0x3f800000u : 0);
+                            }
+                            uint4 seen4 = make_uint4(on[0], on[1], on[2], on[3]), one4 = ones;
+                            const floatx4 met = mfma32(*reinterpret_cast<bf16x8*>(&one4), *reinterpret_cast<bf16x8*>(&seen4), floatx4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) o[n][b][r] = met[r] > 0.f ? NAN : o[n][b][r];
+                        }
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < NC; ++n)
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) o[n][b] = mfma32(*reinterpret_cast<bf16x8*>(&vw), *reinterpret_cast<bf16x8*>(&pt[n][i][z]), o[n][b]);
+            }
+    };
+
+    if (st0 < st1) {
+        fetch();
+        load(st0);
+        put(0);
+        for (int st = st0; st < st1; ++st) {
+            const int buf = (st - st0) & 1;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) pages[u] = next_pages[u];
+            if (st + 1 < st1) load(st + 1);
+            lds_barrier();  // the stage is whole, and its other buffer is no longer read
+            compute(buf);
+            if (st + 1 < st1) put(buf ^ 1);
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+        l_run[n] += __shfl_xor(l_run[n], 16);
+        l_run[n] += __shfl_xor(l_run[n], 32);
+        const int ci = wc + n * 16 + col, tq = ci / a.G, h = ci - tq * a.G;
+        if (ci >= live) continue;
+        if (a.splits == 1) {
+            const float den = l_run[n] > 0.f || l_run[n] != l_run[n] ? l_run[n] : 1.f;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+                store_row<D, F32>(a, (int64_t)m.r0 + m.t0 + tq, c * a.G + h, b * 16 + lg * 4,
+                                  floatx4{o[n][b][0] / den, o[n][b][1] / den, o[n][b][2] / den, o[n][b][3] / den});
+        } else {
+            const int64_t at = (((int64_t)slot * n_kv + c) * a.splits + split) * kManyCols + ci;
+            if (lg == 0) {
+                a.many_ml[at * 2] = fmaxf(m_run[n], -1e30f);
+                a.many_ml[at * 2 + 1] = l_run[n];
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b) *reinterpret_cast<floatx4*>(a.many_o + at * D + b * 16 + lg * 4) = o[n][b];
+        }
+    }
+}
+
+// joins the parts of a tile: a workgroup per (slot, KV head)
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void row_many_merge_kernel(RowAttnArgs a) {
+    constexpr int LANES = D / 4, S = 256 / LANES;
+    const int c = blockIdx.x % a.n_kv, slot = blockIdx.x / a.n_kv;
+    ManyTile m;
+    if (!many_tile(a, slot, m)) return;
+    const int sl = threadIdx.x / LANES, ln = threadIdx.x % LANES;
+    for (int ci = sl; ci < a.G * m.tv; ci += S) {
+        const int64_t at0 = ((int64_t)slot * a.n_kv + c) * a.splits * kManyCols + ci;
+        float M = -1e30f, den = 0.f;
+        floatx4 num = {0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < a.splits; ++j) {
+            const int64_t at = at0 + (int64_t)j * kManyCols;
+            const float2 ml = *reinterpret_cast<const float2*>(a.many_ml + at * 2);
+            const floatx4 o = *reinterpret_cast<const floatx4*>(a.many_o + at * D + ln * 4);
+            const float Mn = fmaxf(M, ml.x), f0 = __builtin_amdgcn_exp2f(M - Mn), f1 = __builtin_amdgcn_exp2f(ml.x - Mn);
+            num = num * f0 + o * f1;
+            den = den * f0 + ml.y * f1;
+            M = Mn;
+        }
+        if (!(den > 0.f) && den == den) den = 1.f;
+        const int tq = ci / a.G, h = ci - tq * a.G;
+        store_row<D, F32>(a, (int64_t)m.r0 + m.t0 + tq, c * a.G + h, ln * 4, floatx4{num[0] / den, num[1] / den, num[2] / den, num[3] / den});
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------------
+
+// How a call is laid out, from what the host knows
+struct RowShape {
+    int G, tg, few_max, cw, few_wgs, passes_max, tt, slots, splits_max;
+    int64_t rec_bytes, few_ml, few_o, many_ml, many_o;  // bytes
+    int64_t bytes() const { return rec_bytes + few_ml + few_o + many_ml + many_o; }
+};
+static int64_t up16(int64_t x) { return (x + 15) / 16 * 16; }
+static RowShape row_shape(int n_q, int n_kv, int d, int batch, int rows, int max_new) {
+    RowShape s;
+    max_new = std::min(max_new, rows);
+    s.G = n_q / n_kv;
+    s.tg = std::max(1, 16 / s.G);
+    s.few_max = 2 * s.tg;
+    const int cols = s.G * std::min(s.tg, max_new);
+    s.cw = cols <= 4 ? 4 : cols <= 8 ? 8 : 16;
+    s.few_wgs = std::max(1, 2 * kNumCU / n_kv);  // of a KV head
+    s.passes_max = (int)std::min((int64_t)rows, (int64_t)batch * ((std::min(max_new, s.few_max) + s.tg - 1) / s.tg));
+    s.rec_bytes = up16(16 + 16 * (int64_t)s.passes_max);
+    const int64_t parts = (4 * (int64_t)s.few_wgs + s.passes_max) * n_kv * s.cw;
+    s.few_ml = up16(parts * 8);
+    s.few_o = parts * d * 4;
+    s.tt = s.slots = s.splits_max = 0;
+    s.many_ml = s.many_o = 0;
+    if (max_new > s.few_max) {
+        s.tt = kManyCols / s.G;
+        s.slots = rows / s.tt + batch;
+        // workgroups that have something to do, at most: with fewer than two for each compute unit their pages are dealt out
+        const int64_t tiles = (int64_t)rows / s.tt + std::min((int64_t)batch, (int64_t)rows / (s.few_max + 1));
+        s.splits_max = (int)std::min<int64_t>(16, 2 * kNumCU / std::max<int64_t>(1, tiles * n_kv));
+        s.splits_max = std::max(1, s.splits_max);
+        if (s.splits_max > 1) {
+            const int64_t n = (int64_t)s.slots * n_kv * s.splits_max * kManyCols;
+            s.many_ml = up16(n * 8);
+            s.many_o = n * d * 4;
+        }
+    }
+    return s;
+}
+
+template <int D, int FMT, bool F32>
+static void launch_few(const RowAttnArgs& a, const RowShape& s, hipStream_t st) {
+    const dim3 grid((unsigned)(s.few_wgs * a.n_kv));
+    if (!F32 || s.cw == 16) launch(row_few_kernel<D, FMT, F32, 16>, grid, dim3(256), st, a);
+    else if (s.cw == 8) launch(row_few_kernel<D, FMT, F32, F32 ? 8 : 16>, grid, dim3(256), st, a);
+    else launch(row_few_kernel<D, FMT, F32, F32 ? 4 : 16>, grid, dim3(256), st, a);
+    launch(row_few_merge_kernel<D, F32>, dim3((unsigned)((int64_t)s.passes_max * a.n_kv * a.pcols)), dim3(256), st, a);
+}
+template <int D, int FMT, bool F32>
+static void launch_rows(const RowAttnArgs& a, const RowShape& s, hipStream_t st) {
+    if (s.slots) {
+        launch(row_many_kernel<D, FMT, F32>, dim3((unsigned)((int64_t)s.slots * a.splits * a.n_kv)), dim3(256), st, a);
+        if (a.splits > 1) launch(row_many_merge_kernel<D, F32>, dim3((unsigned)(s.slots * a.n_kv)), dim3(256), st, a);
+    }
+    launch_few<D, FMT, F32>(a, s, st);
+}
+template <int FMT>
+static void launch_format(const RowAttnArgs& a, const RowShape& s, int d, bool f32, hipStream_t st) {
+    if (d == 128 && f32) launch_rows<128, FMT, true>(a, s, st);
+    else if (d == 128) launch_rows<128, FMT, false>(a, s, st);
+    else if (f32) launch_rows<64, FMT, true>(a, s, st);
+    else launch_rows<64, FMT, false>(a, s, st);
+}
+
+static int32_t row_attention(const chiron_attn_rows* in, int n_kv, int d, int num_blocks, int format, const void* tiles, const int8_t* exps,
+                             void* workspace, hipStream_t st) {
+    if (in->batch < 0 || in->rows < 0 || in->max_new < 0) return fail(CHIRON_ERR_INVALID_ARG, "row attention: a size is negative");
+    if (in->window < 0 || in->n_sinks < 0) return fail(CHIRON_ERR_INVALID_ARG, "row attention: window %d, n_sinks %d", in->window, in->n_sinks);
+    if (in->dtype != CHIRON_F32 && in->dtype != CHIRON_BF16) return fail(CHIRON_ERR_INVALID_ARG, "row attention: dtype %d is neither CHIRON_F32 nor CHIRON_BF16", in->dtype);
+    if (in->n_q_heads < 1 || in->n_q_heads % n_kv != 0 || in->n_q_heads / n_kv > 16)
+        return fail(CHIRON_ERR_SHAPE, "row attention: %d query heads over %d KV heads: a multiple of them, at most 16 times as many", in->n_q_heads, n_kv);
+    if (in->rows == 0 || in->max_new == 0) return CHIRON_OK;
+    if (in->batch == 0) return fail(CHIRON_ERR_INVALID_ARG, "row attention: %d rows of no request", in->rows);
+    if (!in->q || !in->out || !in->block_table || !in->row_starts || !in->seq_lens)
+        return fail(CHIRON_ERR_INVALID_ARG, "row attention: a pointer argument is null");
+    if (in->max_blocks_per_seq < 1 || in->max_blocks_per_seq > 1 << 26)
+        return fail(CHIRON_ERR_INVALID_ARG, "row attention: max_blocks_per_seq %d is not in 1 .. 2^26", in->max_blocks_per_seq);
+    const int size = in->dtype == CHIRON_F32 ? 4 : 2;
+    if (in->q_stride < (int64_t)in->n_q_heads * d || in->q_stride * size % 16 != 0)
+        return fail(CHIRON_ERR_INVALID_ARG, "row attention: q_stride %lld is smaller than a row or no multiple of 16 bytes", (long long)in->q_stride);
+    if (((uintptr_t)in->q | (uintptr_t)in->out | (uintptr_t)workspace) & 15) return fail(CHIRON_ERR_INVALID_ARG, "row attention: q, out and the workspace must be 16-byte aligned");
+    if (!workspace) return fail(CHIRON_ERR_INVALID_ARG, "row attention: the workspace is null");
+    const RowShape s = row_shape(in->n_q_heads, n_kv, d, in->batch, in->rows, in->max_new);
+    if ((int64_t)s.passes_max * in->max_blocks_per_seq >= (int64_t)1 << 31)
+        return fail(CHIRON_ERR_SHAPE, "row attention: %d requests of up to %d pages are too many for one call", in->batch, in->max_blocks_per_seq);
+    RowAttnArgs a = {};
+    a.tiles = (const uint8_t*)tiles; a.exps = exps;
+    a.q = in->q; a.out = in->out; a.q_stride = in->q_stride;
+    a.bt = in->block_table; a.row_starts = in->row_starts; a.seq_lens = in->seq_lens;
+    a.window = in->window ? in->window : (int64_t)1 << 40;
+    a.num_blocks = num_blocks; a.n_kv = n_kv; a.G = s.G; a.max_blocks = in->max_blocks_per_seq; a.batch = in->batch; a.rows = in->rows;
+    a.max_new = in->max_new; a.n_sinks = in->n_sinks;
+    a.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)d));
+    a.few_max = s.few_max; a.tg = s.tg; a.pcols = s.cw; a.passes_max = s.passes_max; a.tt = s.tt;
+    a.splits = 1;
+    if (s.splits_max > 1) {  // a part has 512 tokens at least, if the window or the table lets a tile see as many
+        int64_t pages = in->max_blocks_per_seq;
+        if (in->window) pages = std::min(pages, ((int64_t)in->window + s.tt) / kBlockSize + in->n_sinks / kBlockSize + 3);
+        a.splits = (int)std::min<int64_t>(s.splits_max, std::max<int64_t>(1, pages / 32));
+    }
+    if ((int64_t)s.slots * a.splits * n_kv > 0x7fffffff || (int64_t)s.passes_max * n_kv * s.cw > 0x7fffffff)
+        return fail(CHIRON_ERR_SHAPE, "row attention: %d rows are too many for one call", in->rows);
+    uint8_t* ws = (uint8_t*)workspace;
+    a.head = (int32_t*)ws;
+    a.part_ml = (float*)(ws + s.rec_bytes);
+    a.part_o = (float*)(ws + s.rec_bytes + s.few_ml);
+    a.many_ml = (float*)(ws + s.rec_bytes + s.few_ml + s.few_o);
+    a.many_o = (float*)(ws + s.rec_bytes + s.few_ml + s.few_o + s.many_ml);
+    const bool f32 = in->dtype == CHIRON_F32;
+    if (format == kFmtBf16) launch_format<kFmtBf16>(a, s, d, f32, st);
+    else if (format == kFmtInt8) launch_format<kFmtInt8>(a, s, d, f32, st);
+    else launch_format<kFmtE4m3>(a, s, d, f32, st);
+    CHIRON_HIP(hipGetLastError());
+    return CHIRON_OK;
+}
+
+}  // namespace chiron
+
+using namespace chiron;
+
+extern "C" {
+
+int64_t chiron_row_attention_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t batch, int32_t rows, int32_t max_new) {
+    if (n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads != 0 || n_q_heads / n_kv_heads > 16 || (head_dim != 64 && head_dim != 128)) return 0;
+    if (batch < 1 || rows < 1 || max_new < 1) return 0;
+    return row_shape(n_q_heads, n_kv_heads, head_dim, batch, rows, max_new).bytes();
+}
+
+int32_t chiron_op_row_attention(const chiron_kvpool* p, int32_t layer, const chiron_attn_rows* in, void* workspace, void* stream) {
+    if (!p || !in) return fail(CHIRON_ERR_INVALID_ARG, "pool or rows is null");
+    if (layer < 0 || layer >= p->d.n_layers) return fail(CHIRON_ERR_INVALID_ARG, "layer %d out of range", layer);
+    return row_attention(in, p->d.n_kv, p->d.d, p->d.num_blocks, kFmtBf16, p->d.base + (int64_t)layer * p->d.layer_stride, nullptr, workspace, (hipStream_t)stream);
+}
+
+int32_t chiron_op_row_attention8(const chiron_kvpool8* p, int32_t layer, const chiron_attn_rows* in, void* workspace, void* stream) {
+    if (!p || !in) return fail(CHIRON_ERR_INVALID_ARG, "pool or rows is null");
+    if (layer < 0 || layer >= p->d.n_layers) return fail(CHIRON_ERR_INVALID_ARG, "layer %d out of range", layer);
+    const uint8_t* base = p->d.base + (int64_t)layer * p->d.layer_stride;
+    return row_attention(in, p->d.n_kv, p->d.d, p->d.num_blocks, p->d.format, base, (const int8_t*)base + p->d.exps_at, workspace, (hipStream_t)stream);
+}
+
+}  // extern "C"
