@@ -58,10 +58,14 @@ __device__ __forceinline__ floatx4 decode8(uint32_t w) {
     return floatx4{__builtin_amdgcn_cvt_f32_fp8((int)w, 0), __builtin_amdgcn_cvt_f32_fp8((int)w, 1), __builtin_amdgcn_cvt_f32_fp8((int)w, 2),
                    __builtin_amdgcn_cvt_f32_fp8((int)w, 3)};
 }
-// the four codes of a word as bf16, without their power of two: exact in either format (int8: at most 7 significant bits and a sign)
+// the four codes of a word, times a power of two, as bf16: exact in either format (int8: at most 7 significant bits and a sign)
 template <int FMT>
-__device__ __forceinline__ uint2 widen8(uint32_t w) {
-    const floatx4 f = decode8<FMT>(w);
+__device__ __forceinline__ uint2 widen8(uint32_t w, float scale) {
+    if (FMT == kFmtE4m3) {
+        const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true);
+        return make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+    }
+    const floatx4 f = decode8<FMT>(w) * scale;
     return make_uint2(__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302),
                       __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302));
 }

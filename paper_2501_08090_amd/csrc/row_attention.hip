@@ -16,6 +16,8 @@
 
 namespace chiron {
 
+typedef int intx4 __attribute__((ext_vector_type(4)));
+
 struct RowAttnArgs {
     const uint8_t* tiles;  // the layer's: [num_blocks][n_kv][K tile, V tile]
     const int8_t* exps;    // 8-bit pools: [num_blocks][n_kv][K, V]
@@ -92,31 +94,94 @@ __host__ __device__ constexpr int pieces(int D) { return FMT == kFmtBf16 ? D / 3
 template <int FMT>
 __device__ __forceinline__ int dim_of(int s, int lg) { return FMT == kFmtBf16 ? s * 32 + lg * 8 : s / 2 * 64 + lg * 16 + s % 2 * 8; }
 template <int FMT, int N>
-__device__ __forceinline__ bf16x8 key_operand(const uint4 (&k)[N], int s) {
+__device__ __forceinline__ bf16x8 key_operand(const uint4 (&k)[N], int s, float scale) {
     uint4 w;
-    if (FMT == kFmtBf16) w = k[s];
+    if (FMT == kFmtBf16) w = k[s % N];
     else {
         const uint4 c = k[s / 2];
-        const uint2 a = widen8<FMT>(s % 2 ? c.z : c.x), b = widen8<FMT>(s % 2 ? c.w : c.y);
+        const uint2 a = widen8<FMT>(s % 2 ? c.z : c.x, scale), b = widen8<FMT>(s % 2 ? c.w : c.y, scale);
         w = make_uint4(a.x, a.y, b.x, b.y);
     }
     return *reinterpret_cast<bf16x8*>(&w);
 }
 __device__ __forceinline__ uint32_t word(const uint4& w, int j) { return j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w; }
-// the i-th of the three bf16 terms of v
-__device__ __forceinline__ float term3(float v, int i) {
-    const float hi = bf16_lo(pack_bf16_rne(v, 0.f)), r1 = v - hi, mid = bf16_lo(pack_bf16_rne(r1, 0.f));
-    return i == 0 ? hi : i == 1 ? mid : r1 - mid;
+// An fp32 number is the sum of three bf16 terms, exactly: the first 8 of its 24 significant bits, the next 8 and the rest, by truncation.
+// What is left of v behind its first t terms; its next term is the upper half of the word.
+__device__ __forceinline__ float upper(float v, uint32_t mask) { return __uint_as_float(__float_as_uint(v) & mask); }
+__device__ __forceinline__ float rest3(float v, int t) {
+    const uint32_t m1 = t > 0 ? 0xffff0000u : 0, m2 = t > 1 ? 0xffff0000u : 0;
+    const float r = v - upper(v, m1);
+    return r - upper(r, m2);
 }
-// NaN and infinities among two bf16: which (as bf16 ones), and the word without them
-__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
-    return ((w & 0x7f80u) == 0x7f80u ? 0x3f80u : 0) | ((w & 0x7f800000u) == 0x7f800000u ? 0x3f800000u : 0);
+__device__ __forceinline__ uint32_t uppers(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302); }
+// NaN and infinities among two bf16: the top bit of each half set where its exponent is all ones; as bf16 ones; and the word without them
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ uint32_t ones_of(uint32_t bad) { return (bad >> 15) * 0x3f80u; }
+__device__ __forceinline__ uint32_t without(uint32_t w, uint32_t bad) { return w & ~((bad >> 15) * 0xffffu); }
+__device__ __forceinline__ uint4 finite_only(const uint4& w) {
+    return make_uint4(without(w.x, not_finite(w.x)), without(w.y, not_finite(w.y)), without(w.z, not_finite(w.z)), without(w.w, not_finite(w.w)));
 }
-__device__ __forceinline__ uint32_t without(uint32_t w, uint32_t ones) { return w & ~((ones & 0x80u ? 0xffffu : 0) | (ones & 0x800000u ? 0xffff0000u : 0)); }
 
+__device__ __forceinline__ intx4 mfma_i8(const uint4& a, const uint4& b, intx4 c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const intx4*>(&a), *reinterpret_cast<const intx4*>(&b), c, 0, 0, 0);
+}
 __device__ __forceinline__ floatx4 mfma32(bf16x8 a, bf16x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ floatx4 mfma16(uint2 a, uint2 b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(*reinterpret_cast<short4v*>(&a), *reinterpret_cast<short4v*>(&b), c, 0, 0, 0);
+}
+
+// Values that are no finite numbers, in a stage of pages of which a column sees some and another does not: 0 * NaN would reach those that do
+// not see them.  The stage's products go on without them, and this, behind the loop over the stages, makes NaN of the dims and columns
+// that have seen one: products of which values they are with which tokens a column sees.
+template <int D, int NC, int NPG>
+__device__ __forceinline__ void mark_not_finite(const RowAttnArgs& a, const Span& span, const Seen& seen, const int32_t* btrow, int c, int j0, int j1, const int (&col_lo)[NC],
+                                                const int (&col_last)[NC], floatx4 (&o)[NC][D / 16]) {
+    const int lane = threadIdx.x & 63, lg = lane >> 4;
+    auto there = [&](int j, int& block) {
+        const int page = j < j1 ? span.page(j) : -1;
+        block = page >= 0 && page < a.max_blocks ? __builtin_amdgcn_readfirstlane(btrow[page]) : -1;
+        return block < 0 || block >= a.num_blocks ? -1 : page;
+    };
+#pragma unroll 1
+    for (int j = j0; j < j1; ++j) {
+        int block;
+        const int page = there(j, block), stage = j0 + (j - j0) / NPG * NPG;
+        if (page < 0) continue;
+        bool full = true;
+#pragma unroll 1
+        for (int u = 0; u < NPG; ++u) {
+            int other;
+            full = full && all_seen(a, seen, there(stage + u, other));
+        }
+        if (full) continue;
+        const int tok = page * kBlockSize + lg * 4;
+        const uint4 keep = seen_masks(a, seen, true, tok);
+        const uint8_t* tile = a.tiles + ((int64_t)block * a.n_kv + c) * (64 * D) + 32 * D + lane * 16;
+        uint2 vis[NC];
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            uint32_t on[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) on[r] = sees(a, col_lo[n], col_last[n], tok + r) ? 0x3f80u : 0;
+            vis[n] = make_uint2(on[0] | on[1] << 16, on[2] | on[3] << 16);
+        }
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            const uint4 v = *reinterpret_cast<const uint4*>(tile + i * 1024);
+            const uint2 even = make_uint2(ones_of(not_finite(v.x & keep.x)), ones_of(not_finite(v.y & keep.y)));
+            const uint2 odd = make_uint2(ones_of(not_finite(v.z & keep.x)), ones_of(not_finite(v.w & keep.y)));
+#pragma unroll
+            for (int n = 0; n < NC; ++n) {
+                const floatx4 x = mfma16(even, vis[n], floatx4{0.f, 0.f, 0.f, 0.f}), y = mfma16(odd, vis[n], floatx4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    o[n][2 * i][r] = x[r] > 0.f ? NAN : o[n][2 * i][r];
+                    o[n][2 * i + 1][r] = y[r] > 0.f ? NAN : o[n][2 * i + 1][r];
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
 }
 
 // a request's rows, as the kernels take them: 0 rows where the row starts do not ascend
@@ -147,18 +212,26 @@ __device__ __forceinline__ void store_row(const RowAttnArgs& a, int64_t row, int
 // that lies in several shares leaves partial results (maximum, sum, unnormalised output), which row_few_merge_kernel joins; partial result
 // w + v is wave w's of pass v, a number of its own for each pair that exists.
 //
-// CW: columns of a term group.  Three terms of up to 4 columns share one instruction, of up to 8 two.
+// CW: columns of a term group.  Three terms of up to 4 columns share one instruction, of up to 8 two.  int8 keys meet the query in
+// three 8-bit digits instead (whole multiples of 2^(f-16), with 2^f the power of two of the head's largest element), on the 8-bit matrix
+// cores: no key is widened, and sums are exact.
 constexpr int kFewMinPages = 8;  // of a share
-template <int D, int FMT, bool F32, int CW>
-__global__ __launch_bounds__(256, 2) void row_few_kernel(RowAttnArgs a) {
-    constexpr int KSTEPS = D / 32, P = pieces<FMT>(D), NPG = FMT == kFmtBf16 && D == 128 ? 2 : 4;
-    constexpr int NT = F32 ? 3 : 1, TPI = F32 ? (16 / CW < 3 ? 16 / CW : 3) : 1, NI = (NT + TPI - 1) / TPI;
-    constexpr int TILE = FMT == kFmtBf16 ? 32 * D : 16 * D;  // bytes of a K or V tile
+// Waves of a SIMD: two, but one where three terms of many columns and bf16 pages of 128 dims do not fit 256 registers.
+__host__ __device__ constexpr int few_waves(int d, int fmt, bool f32, int cw, bool multi) {
+    return fmt == kFmtBf16 && f32 && d == 128 && (cw == 16 || (cw == 8 && multi)) ? 1 : 2;
+}
+template <int D, int FMT, bool F32, int CW, bool MULTI>
+__global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_few_kernel(RowAttnArgs a) {
+    constexpr bool DIGITS = FMT == kFmtInt8, TERMS = DIGITS || F32;
+    constexpr int KSTEPS = D / (DIGITS ? 64 : 32), P = pieces<FMT>(D), NPG = D == 128 && (FMT == kFmtBf16 || (F32 && CW == 16)) ? 2 : 4;
+    constexpr int TPI = TERMS && CW <= 8 ? (CW <= 4 ? 3 : 2) : 1;        // terms of an instruction
+    constexpr int NQ = TERMS ? (3 + TPI - 1) / TPI : 1, NP = F32 ? NQ : 1;  // instructions for those of a query, of a weight
+    constexpr int TILE = FMT == kFmtBf16 ? 32 * D : 16 * D;               // bytes of a K or V tile
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n_kv = a.n_kv, c = blockIdx.x % n_kv, w = blockIdx.x / n_kv * 4 + wave, W = gridDim.x / n_kv * 4;
     const int col = lane & 15, lg = lane >> 4, ci = col % CW, grp = col / CW;
-    const int tq = ci / a.G, h = ci - tq * a.G;
+    const int tq = MULTI ? ci / a.G : 0, h = ci - tq * a.G;
 
     // a lane's request of the 64 from i0 on: pages over its passes, and passes
     auto look = [&](int i0, Request& r, int& cost, int& np) {
@@ -189,7 +262,7 @@ __global__ __launch_bounds__(256, 2) void row_few_kernel(RowAttnArgs a) {
     int64_t base = 0, at = begin;
     int vbase = 0;
     for (int i0 = 0; i0 < a.batch && at < end; i0 += 64) {
-        look(i0, rq, cost, np);
+        if (a.batch > 64) look(i0, rq, cost, np);  // else they are still there
         const int incl = wave_scan(cost), vincl = wave_scan(np);
         const int all = __builtin_amdgcn_readlane(incl, 63);
         uint64_t ahead = __ballot(base + incl > at && cost > 0);
@@ -202,7 +275,7 @@ __global__ __launch_bounds__(256, 2) void row_few_kernel(RowAttnArgs a) {
             int64_t first = base + __builtin_amdgcn_readlane(incl, L) - __builtin_amdgcn_readlane(cost, L);
             int v = vbase + __builtin_amdgcn_readlane(vincl, L) - passes;
             for (int g = 0; g < passes && at < end; ++g, ++v) {
-                const int t0 = g * a.tg, tv = min(a.tg, n - t0);
+                const int t0 = g * a.tg, tv = MULTI ? min(a.tg, n - t0) : 1;
                 const Span span = span_of(a, old + t0, old + t0 + tv - 1);
                 const int64_t pass0 = first;
                 first += span.n;
@@ -214,11 +287,10 @@ __global__ __launch_bounds__(256, 2) void row_few_kernel(RowAttnArgs a) {
                     *reinterpret_cast<int4*>(a.head + 4 + 4 * (size_t)v) = make_int4(row0 + t0, tv, seg0 + v, segs);
 
                 // ---- the pages j0 .. j1-1 of pass v
-                const int cols = a.G * tv;
-                const bool on = ci < cols;
+                const bool on = ci < a.G * tv;
                 const Seen seen = seen_of(a, old + t0, old + t0 + tv - 1);
                 const int64_t pos = old + t0 + min(tq, tv - 1);
-                const int col_lo = first_seen(a, pos), col_last = last_seen(a, pos);
+                const int lo1[1] = {first_seen(a, pos)}, last1[1] = {last_seen(a, pos)};
                 const int32_t* btrow = a.bt + (size_t)(i0 + L) * a.max_blocks;
 
                 // lane l holds entry lbase + l of the span: the page, where it is in the pool, its powers of two
@@ -235,7 +307,7 @@ __global__ __launch_bounds__(256, 2) void row_few_kernel(RowAttnArgs a) {
                 struct Stage {
                     uint4 k[NPG][P], v[NPG][P];
                     int page[NPG], exp[NPG];
-                };
+                } cur, nxt;
                 auto load = [&](int j, Stage& s) {
                     if (j - lbase >= 64) {  // uniform; 64 is a multiple of NPG
                         lbase = j;
@@ -256,89 +328,176 @@ __global__ __launch_bounds__(256, 2) void row_few_kernel(RowAttnArgs a) {
                         }
                     }
                 };
-                uint4 qt[NI][KSTEPS];
-                floatx4 o[D / 16];
+                uint4 qt[NQ][KSTEPS];
+                float qw[NQ];  // what a digit of the lane's term stands for
+                floatx4 oo[1][D / 16], (&o)[D / 16] = oo[0];
 #pragma unroll
                 for (int t = 0; t < D / 16; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
                 float m_run = -INFINITY, l_run = 0.f;
+                bool marked = false;
 
-                auto compute = [&](Stage& s) {
+                fetch();
+                load(j0, cur);
+                __builtin_amdgcn_sched_barrier(0);
+                const int64_t qrow = (row0 + t0 + min(tq, tv - 1)) * a.q_stride + (int64_t)(c * a.G + h) * D;
+                if (DIGITS) {
+                    float y[KSTEPS][16], top = 0.f;
+#pragma unroll
+                    for (int s = 0; s < KSTEPS; ++s) {
+                        const int64_t at = qrow + s * 64 + lg * 16;
+#pragma unroll
+                        for (int e = 0; e < 16; e += 4) {
+                            if (F32) {
+                                const float4 z = *reinterpret_cast<const float4*>((const float*)a.q + at + e);
+                                y[s][e] = z.x, y[s][e + 1] = z.y, y[s][e + 2] = z.z, y[s][e + 3] = z.w;
+                            } else {
+                                const uint2 z = *reinterpret_cast<const uint2*>((const uint16_t*)a.q + at + e);
+                                y[s][e] = bf16_lo(z.x), y[s][e + 1] = bf16_hi(z.x), y[s][e + 2] = bf16_lo(z.y), y[s][e + 3] = bf16_hi(z.y);
+                            }
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) top = fmaxf(top, fabsf(y[s][e + z]));
+                        }
+                    }
+                    top = fmaxf(top, __shfl_xor(top, 16));
+                    top = fmaxf(top, __shfl_xor(top, 32));
+                    // |y| <= 127 * 2^f; a head of zeros, NaN and infinities go by any power (the last two are put back below)
+                    const int f = top > 0.f && top < INFINITY ? min(max(power_of(top), -100), 120) : 0;
+                    const float up = two_to(-f) * 65536.f;
+                    float bad = 0.f;
+#pragma unroll
+                    for (int s = 0; s < KSTEPS; ++s) {
+                        uint32_t d[NQ][4];
+#pragma unroll
+                        for (int i = 0; i < NQ; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) d[i][e] = 0;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            bad += y[s][e] * 0.f;  // 0, or NaN
+                            const int x = (int)rintf(y[s][e] * up);
+                            // low digit first, each -128 .. 127: |x| <= 127 * 65536 leaves -127 .. 127 for the high one
+                            const int d2 = (int8_t)x, x1 = (x - d2) >> 8, d1 = (int8_t)x1, d0 = (x1 - d1) >> 8;
+#pragma unroll
+                            for (int i = 0; i < NQ; ++i) {
+                                const int t = i * TPI + grp;
+                                const int digit = !on || t > 2 || grp >= TPI ? 0 : t == 0 ? d0 : t == 1 ? d1 : d2;
+                                d[i][e / 4] |= (uint32_t)(digit & 0xff) << (e % 4 * 8);
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < NQ; ++i) qt[i][s] = make_uint4(d[i][0], d[i][1], d[i][2], d[i][3]);
+                    }
+                    bad += __shfl_xor(bad, 16);
+                    bad += __shfl_xor(bad, 32);
+#pragma unroll
+                    for (int i = 0; i < NQ; ++i) {
+                        const int t = i * TPI + grp;
+                        qw[i] = two_to(f) * a.scale_log2e * (t == 0 ? 1.f : t == 1 ? 0x1p-8f : 0x1p-16f) + (on ? bad : 0.f);
+                    }
+                } else {
+#pragma unroll
+                    for (int s = 0; s < KSTEPS; ++s) {
+                        const int64_t at = qrow + dim_of<FMT>(s, lg);
+                        if (F32) {
+                            const float4 y0 = *reinterpret_cast<const float4*>((const float*)a.q + at), y1 = *reinterpret_cast<const float4*>((const float*)a.q + at + 4);
+                            const float y[8] = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
+#pragma unroll
+                            for (int i = 0; i < NQ; ++i) {
+                                float z[8];
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    const int t = i * TPI + grp;
+                                    z[e] = !on || grp >= TPI || t > 2 ? 0.f : rest3(y[e] * a.scale_log2e, t);
+                                }
+                                qt[i][s] = make_uint4(uppers(z[0], z[1]), uppers(z[2], z[3]), uppers(z[4], z[5]), uppers(z[6], z[7]));
+                            }
+                        } else {
+                            const uint4 y = *reinterpret_cast<const uint4*>((const uint16_t*)a.q + at);
+                            qt[0][s] = on ? y : make_uint4(0, 0, 0, 0);
+                        }
+                    }
+                }
+
+                for (int j = j0; j < j1; j += NPG) {
+                    if (j + NPG < j1) load(j + NPG, nxt);
+                    __builtin_amdgcn_sched_barrier(0);
                     bool full = true;
 #pragma unroll
-                    for (int u = 0; u < NPG; ++u) full = full && all_seen(a, seen, s.page[u]);
+                    for (int u = 0; u < NPG; ++u) full = full && all_seen(a, seen, cur.page[u]);
                     floatx4 x[NPG];
-                    float vs[NPG];
-                    float mx = -INFINITY;
+                    float ks[NPG], vs[NPG];
 #pragma unroll
                     for (int u = 0; u < NPG; ++u) {
-                        x[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+                        ks[u] = FMT == kFmtBf16 ? 1.f : two_to((int8_t)(cur.exp[u] & 0xff));
+                        vs[u] = FMT == kFmtBf16 ? 1.f : two_to((int8_t)(cur.exp[u] >> 8));
+                        if (DIGITS) {
+                            intx4 y[NQ];
 #pragma unroll
-                        for (int k = 0; k < KSTEPS; ++k) {
-                            const bf16x8 key = key_operand<FMT>(s.k[u], k);
+                            for (int i = 0; i < NQ; ++i) {
+                                y[i] = intx4{0, 0, 0, 0};
 #pragma unroll
-                            for (int i = 0; i < NI; ++i) x[u] = mfma32(key, *reinterpret_cast<bf16x8*>(&qt[i][k]), x[u]);
+                                for (int k = 0; k < KSTEPS; ++k) y[i] = mfma_i8(cur.k[u][k % P], qt[i][k], y[i]);
+                            }
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                x[u][r] = (float)y[0][r] * (qw[0] * ks[u]);
+#pragma unroll
+                                for (int i = 1; i < NQ; ++i) x[u][r] += (float)y[i][r] * (qw[i] * ks[u]);
+                            }
+                        } else {
+                            x[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                            for (int k = 0; k < KSTEPS; ++k) {
+                                const bf16x8 key = key_operand<FMT>(cur.k[u], k, ks[u]);
+#pragma unroll
+                                for (int i = 0; i < NQ; ++i) x[u] = mfma32(key, *reinterpret_cast<bf16x8*>(&qt[i][k]), x[u]);
+                            }
+                            if (!F32) x[u] *= a.scale_log2e;
                         }
-                        float ks = F32 ? 1.f : a.scale_log2e;
-                        vs[u] = 1.f;
-                        if (FMT != kFmtBf16) {
-                            ks *= two_to((int8_t)(s.exp[u] & 0xff));
-                            vs[u] = two_to((int8_t)(s.exp[u] >> 8));
-                        }
+                        if (TPI > 1) {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {  // the sum over the term groups, in every column
-                            if (TPI > 1) x[u][r] += row_move<kRor8>(x[u][r]);
-                            if (TPI > 1 && CW <= 4) x[u][r] += row_move<kRor4>(x[u][r]);
-                            if (!F32 || FMT != kFmtBf16) x[u][r] *= ks;
+                            for (int r = 0; r < 4; ++r) {  // the sum over the term groups, in every column
+                                x[u][r] += row_move<kRor8>(x[u][r]);
+                                if (CW <= 4) x[u][r] += row_move<kRor4>(x[u][r]);
+                            }
                         }
                     }
                     if (!full) {
 #pragma unroll
                         for (int u = 0; u < NPG; ++u) {
-                            const bool there = s.page[u] >= 0;
-                            const int tok = max(s.page[u], 0) * kBlockSize + lg * 4;
+                            const bool there = cur.page[u] >= 0;
+                            const int tok = max(cur.page[u], 0) * kBlockSize + lg * 4;
                             if (!there) vs[u] = 0.f;
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) x[u][r] = there && sees(a, col_lo, col_last, tok + r) ? x[u][r] : -INFINITY;
+                            for (int r = 0; r < 4; ++r) x[u][r] = there && sees(a, lo1[0], last1[0], tok + r) ? x[u][r] : -INFINITY;
                             // what no column sees may hold anything, NaN included: clear its V so that 0 * V stays 0
                             const uint4 keep = seen_masks(a, seen, there, tok);
 #pragma unroll
                             for (int i = 0; i < P; ++i) {
-                                uint4& v = s.v[u][i];
+                                uint4& v = cur.v[u][i];
                                 if (FMT == kFmtBf16) v.x &= keep.x, v.y &= keep.y, v.z &= keep.x, v.w &= keep.y;
                                 else v.x &= keep.z, v.y &= keep.z, v.z &= keep.z, v.w &= keep.z;
                             }
                         }
-                        // what some columns see and others do not must not reach these: 0 * NaN
-                        if (FMT == kFmtBf16 && tv > 1) {
+                        if (FMT == kFmtBf16 && MULTI) {  // 8-bit caches hold none
                             uint32_t bad = 0;
 #pragma unroll
                             for (int u = 0; u < NPG; ++u)
 #pragma unroll
-                                for (int i = 0; i < P; ++i)
-                                    bad |= not_finite(s.v[u][i].x) | not_finite(s.v[u][i].y) | not_finite(s.v[u][i].z) | not_finite(s.v[u][i].w);
-                            if (__any(bad != 0)) {
-#pragma unroll
-                                for (int u = 0; u < NPG; ++u) {
-                                    const int tok = max(s.page[u], 0) * kBlockSize + lg * 4;
-                                    uint32_t on4[4];
-#pragma unroll
-                                    for (int r = 0; r < 4; ++r) on4[r] = s.page[u] >= 0 && sees(a, col_lo, col_last, tok + r) ? 0x3f80u : 0;
-                                    const uint2 vis = make_uint2(on4[0] | on4[1] << 16, on4[2] | on4[3] << 16);
-#pragma unroll
-                                    for (int b = 0; b < D / 16; ++b) {
-                                        uint4& v = s.v[u][b / 2 % P];
-                                        uint32_t &w0 = b % 2 ? v.z : v.x, &w1 = b % 2 ? v.w : v.y;
-                                        const uint2 ones = make_uint2(not_finite(w0), not_finite(w1));
-                                        w0 = without(w0, ones.x);
-                                        w1 = without(w1, ones.y);
-                                        const floatx4 met = mfma16(ones, vis, floatx4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                                        for (int r = 0; r < 4; ++r) o[b][r] = met[r] > 0.f ? NAN : o[b][r];
-                                    }
+                                for (int i = 0; i < P; ++i) {
+                                    const uint4 v = cur.v[u][i];
+                                    bad |= not_finite(v.x) | not_finite(v.y) | not_finite(v.z) | not_finite(v.w);
                                 }
+                            if (__any(bad != 0)) {
+                                marked = true;
+#pragma unroll
+                                for (int u = 0; u < NPG; ++u)
+#pragma unroll
+                                    for (int i = 0; i < P; ++i) cur.v[u][i] = finite_only(cur.v[u][i]);
                             }
                         }
                     }
+                    float mx = x[0][0];
 #pragma unroll
                     for (int u = 0; u < NPG; ++u)
 #pragma unroll
@@ -346,11 +505,13 @@ __global__ __launch_bounds__(256, 2) void row_few_kernel(RowAttnArgs a) {
                     mx = fmaxf(mx, __shfl_xor(mx, 16));
                     mx = fmaxf(mx, __shfl_xor(mx, 32));
                     const float m_new = fmaxf(m_run, mx), m_use = fmaxf(m_new, -1e30f);  // nothing seen yet: finite exponents, weights 0
-                    const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
-                    m_run = m_new;
-                    l_run *= alpha;
+                    if (__any(m_new > m_run)) {
+                        const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+                        l_run *= alpha;
 #pragma unroll
-                    for (int t = 0; t < D / 16; ++t) o[t] *= alpha;
+                        for (int t = 0; t < D / 16; ++t) o[t] *= alpha;
+                    }
+                    m_run = m_new;
 #pragma unroll
                     for (int u = 0; u < NPG; u += 2) {
                         float pr[2][4];
@@ -360,88 +521,54 @@ __global__ __launch_bounds__(256, 2) void row_few_kernel(RowAttnArgs a) {
                             for (int r = 0; r < 4; ++r) {
                                 pr[z][r] = __builtin_amdgcn_exp2f(x[u + z][r] - m_use);
                                 l_run += pr[z][r];
-                                if (FMT != kFmtBf16) pr[z][r] *= vs[u + z];
+                                if (DIGITS) pr[z][r] *= vs[u + z];  // int8 values enter as their codes
                             }
-                        uint4 pt[NI];
+                        uint4 pt[NP];
 #pragma unroll
-                        for (int i = 0; i < NI; ++i) {
-                            float y[2][4];
+                        for (int i = 0; i < NP; ++i) {
+                            if (F32) {
+                                const int t = i * TPI + grp;
+                                const uint32_t keep = TPI > 1 && (t > 2 || grp >= TPI) ? 0 : ~0u;
+                                float y[2][4];
 #pragma unroll
-                            for (int z = 0; z < 2; ++z)
+                                for (int z = 0; z < 2; ++z)
 #pragma unroll
-                                for (int r = 0; r < 4; ++r) {
-                                    const int t = i * TPI + grp;
-                                    y[z][r] = !F32 ? pr[z][r] : TPI == 1 ? term3(pr[z][r], i) : grp >= TPI || t > 2 ? 0.f : term3(pr[z][r], t);
-                                }
-                            pt[i] = make_uint4(pack_bf16_rne(y[0][0], y[0][1]), pack_bf16_rne(y[0][2], y[0][3]), pack_bf16_rne(y[1][0], y[1][1]),
-                                               pack_bf16_rne(y[1][2], y[1][3]));
+                                    for (int r = 0; r < 4; ++r) y[z][r] = rest3(pr[z][r], t);
+                                pt[i] = make_uint4(uppers(y[0][0], y[0][1]) & keep, uppers(y[0][2], y[0][3]) & keep, uppers(y[1][0], y[1][1]) & keep,
+                                                   uppers(y[1][2], y[1][3]) & keep);
+                            } else {
+                                pt[i] = make_uint4(pack_bf16_rne(pr[0][0], pr[0][1]), pack_bf16_rne(pr[0][2], pr[0][3]), pack_bf16_rne(pr[1][0], pr[1][1]),
+                                                   pack_bf16_rne(pr[1][2], pr[1][3]));
+                            }
                         }
 #pragma unroll
                         for (int b = 0; b < D / 16; ++b) {
                             if (FMT == kFmtBf16) {
-                                const uint4 &va = s.v[u][b / 2 % P], &vb = s.v[u + 1][b / 2 % P];
+                                const uint4 &va = cur.v[u][b / 2 % P], &vb = cur.v[u + 1][b / 2 % P];
                                 const uint2 v0 = b % 2 ? make_uint2(va.z, va.w) : make_uint2(va.x, va.y);
                                 const uint2 v1 = b % 2 ? make_uint2(vb.z, vb.w) : make_uint2(vb.x, vb.y);
 #pragma unroll
-                                for (int i = 0; i < NI; ++i) {
+                                for (int i = 0; i < NP; ++i) {
                                     o[b] = mfma16(v0, make_uint2(pt[i].x, pt[i].y), o[b]);
                                     o[b] = mfma16(v1, make_uint2(pt[i].z, pt[i].w), o[b]);
                                 }
                             } else {
-                                const uint2 v0 = widen8<FMT>(word(s.v[u][b / 4 % P], b % 4)), v1 = widen8<FMT>(word(s.v[u + 1][b / 4 % P], b % 4));
+                                const float s0 = DIGITS ? 1.f : vs[u], s1 = DIGITS ? 1.f : vs[u + 1];
+                                const uint2 v0 = widen8<FMT>(word(cur.v[u][b / 4 % P], b % 4), s0), v1 = widen8<FMT>(word(cur.v[u + 1][b / 4 % P], b % 4), s1);
                                 uint4 v = make_uint4(v0.x, v0.y, v1.x, v1.y);
 #pragma unroll
-                                for (int i = 0; i < NI; ++i) o[b] = mfma32(*reinterpret_cast<bf16x8*>(&v), *reinterpret_cast<bf16x8*>(&pt[i]), o[b]);
+                                for (int i = 0; i < NP; ++i) o[b] = mfma32(*reinterpret_cast<bf16x8*>(&v), *reinterpret_cast<bf16x8*>(&pt[i]), o[b]);
                             }
                         }
                     }
-                };
-
-                Stage sa, sb;
-                fetch();
-                load(j0, sa);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int s = 0; s < KSTEPS; ++s) {
-                    const int64_t qrow = row0 + t0 + min(tq, tv - 1);
-                    const int64_t qat = qrow * a.q_stride + (int64_t)(c * a.G + h) * D + dim_of<FMT>(s, lg);
-                    if (F32) {
-                        const float* qp = (const float*)a.q + qat;
-                        const float4 y0 = *reinterpret_cast<const float4*>(qp), y1 = *reinterpret_cast<const float4*>(qp + 4);
-                        float y[8] = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
-#pragma unroll
-                        for (int i = 0; i < NI; ++i) {
-                            float z[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const int t = i * TPI + grp;
-                                z[e] = !on || grp >= TPI || t > 2 ? 0.f : term3(y[e] * a.scale_log2e, t);
-                            }
-                            qt[i][s] = make_uint4(pack_bf16_rne(z[0], z[1]), pack_bf16_rne(z[2], z[3]), pack_bf16_rne(z[4], z[5]), pack_bf16_rne(z[6], z[7]));
-                        }
-                    } else {
-                        const uint4 y = *reinterpret_cast<const uint4*>((const uint16_t*)a.q + qat);
-                        qt[0][s] = on ? y : make_uint4(0, 0, 0, 0);
-                    }
-                }
-                for (int j = j0;;) {
-                    if (j + NPG < j1) load(j + NPG, sb);
                     __builtin_amdgcn_sched_barrier(0);
-                    compute(sa);
-                    __builtin_amdgcn_sched_barrier(0);
-                    j += NPG;
-                    if (j >= j1) break;
-                    if (j + NPG < j1) load(j + NPG, sa);
-                    __builtin_amdgcn_sched_barrier(0);
-                    compute(sb);
-                    __builtin_amdgcn_sched_barrier(0);
-                    j += NPG;
-                    if (j >= j1) break;
+                    cur = nxt;
                 }
 
+                if (FMT == kFmtBf16 && MULTI && marked) mark_not_finite<D, 1, NPG>(a, span, seen, btrow, c, j0, j1, lo1, last1, oo);
                 l_run += __shfl_xor(l_run, 16);
                 l_run += __shfl_xor(l_run, 32);
-                if (TPI > 1) {
+                if (TPI > 1 && F32) {
 #pragma unroll
                     for (int t = 0; t < D / 16; ++t)
 #pragma unroll
@@ -591,8 +718,8 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void row_many_kernel(RowAttnArgs 
                 for (int i = 0; i < NT; ++i) {
                     float z[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) z[e] = ci < live ? term3(y[e] * a.scale_log2e, i) : 0.f;
-                    qt[n][i][s] = make_uint4(pack_bf16_rne(z[0], z[1]), pack_bf16_rne(z[2], z[3]), pack_bf16_rne(z[4], z[5]), pack_bf16_rne(z[6], z[7]));
+                    for (int e = 0; e < 8; ++e) z[e] = ci < live ? rest3(y[e] * a.scale_log2e, i) : 0.f;
+                    qt[n][i][s] = make_uint4(uppers(z[0], z[1]), uppers(z[2], z[3]), uppers(z[4], z[5]), uppers(z[6], z[7]));
                 }
             } else {
                 const uint4 y = *reinterpret_cast<const uint4*>((const uint16_t*)a.q + qat);
@@ -602,6 +729,7 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void row_many_kernel(RowAttnArgs 
     }
     floatx4 o[NC][NB];
     float m_run[NC], l_run[NC];
+    bool marked = false;
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
         m_run[n] = -INFINITY;
@@ -621,7 +749,7 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void row_many_kernel(RowAttnArgs 
         v_block = blk;
         if (FMT != kFmtBf16) v_exp = *reinterpret_cast<const uint16_t*>(a.exps + ((int64_t)blk * n_kv + c) * 2);
     };
-    uint4 rk[P], rv[P];  // the wave's page of the stage that comes next
+    u32x4 rk[P], rv[P];  // the wave's page of the stage that comes next
     int r_page = -1, r_exp = 0, pages[4], next_pages[4];
     auto load = [&](int st) {
         if (st * 4 - lbase >= 64) {
@@ -636,8 +764,8 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void row_many_kernel(RowAttnArgs 
         const uint8_t* tile = a.tiles + ((int64_t)__builtin_amdgcn_readlane(v_block, l + wave) * n_kv + c) * (2 * TILE) + lane * 16;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            rk[i] = *reinterpret_cast<const uint4*>(tile + i * 1024);
-            rv[i] = *reinterpret_cast<const uint4*>(tile + TILE + i * 1024);
+            rk[i] = *reinterpret_cast<const u32x4*>(tile + i * 1024);
+            rv[i] = *reinterpret_cast<const u32x4*>(tile + TILE + i * 1024);
         }
     };
     auto put = [&](int buf) {
@@ -645,32 +773,25 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void row_many_kernel(RowAttnArgs 
             const uint4 keep = seen_masks(a, tile_seen, r_page >= 0, max(r_page, 0) * kBlockSize + lg * 4);
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                uint4& v = rv[i];
-                if (FMT == kFmtBf16) v.x &= keep.x, v.y &= keep.y, v.z &= keep.x, v.w &= keep.y;
-                else v.x &= keep.z, v.y &= keep.z, v.z &= keep.z, v.w &= keep.z;
+                rv[i] &= FMT == kFmtBf16 ? u32x4{keep.x, keep.y, keep.x, keep.y} : u32x4{keep.z, keep.z, keep.z, keep.z};
             }
         }
         const float ks = two_to((int8_t)(r_exp & 0xff)), vs = r_page >= 0 ? two_to((int8_t)(r_exp >> 8)) : 0.f;
         uint2* dv = reinterpret_cast<uint2*>(&s_v[buf][wave / 2][0][lane]) + wave % 2;
-        auto widened = [&](uint32_t w, float scale) {  // exact: the value is a bf16 number
-            const floatx4 f = decode8<FMT>(w) * scale;
-            return make_uint2(__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302),
-                              __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302));
-        };
 #pragma unroll
         for (int s = 0; s < KSTEPS; ++s) {
-            if (FMT == kFmtBf16) s_k[buf][wave][s][lane] = rk[s % P];
+            if (FMT == kFmtBf16) *reinterpret_cast<u32x4*>(&s_k[buf][wave][s][lane]) = rk[s % P];
             else {
-                const uint2 x = widened(word(rk[s / 2], s % 2 * 2), ks), y = widened(word(rk[s / 2], s % 2 * 2 + 1), ks);
+                const uint2 x = widen8<FMT>(rk[s / 2][s % 2 * 2], ks), y = widen8<FMT>(rk[s / 2][s % 2 * 2 + 1], ks);
                 s_k[buf][wave][s][lane] = make_uint4(x.x, x.y, y.x, y.y);
             }
         }
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             if (FMT == kFmtBf16) {
-                const uint4 v = rv[b / 2 % P];
-                dv[b * 128] = b % 2 ? make_uint2(v.z, v.w) : make_uint2(v.x, v.y);
-            } else dv[b * 128] = widened(word(rv[b / 4], b % 4), vs);
+                const u32x4 v = rv[b / 2 % P];
+                dv[b * 128] = b % 2 ? make_uint2(v[2], v[3]) : make_uint2(v[0], v[1]);
+            } else dv[b * 128] = widen8<FMT>(rv[b / 4][b % 4], vs);
         }
     };
 
@@ -696,24 +817,15 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void row_many_kernel(RowAttnArgs 
                     for (int i = 0; i < NT; ++i) x[n][u] = mfma32(*reinterpret_cast<bf16x8*>(&kw), *reinterpret_cast<bf16x8*>(&qt[n][i][s]), x[n][u]);
             }
         }
-        uint32_t vis[NC];  // four bits a page
-#pragma unroll
-        for (int n = 0; n < NC; ++n) vis[n] = 0xffff;
         if (!full) {
 #pragma unroll
-            for (int n = 0; n < NC; ++n) {
-                vis[n] = 0;
+            for (int n = 0; n < NC; ++n)
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     const int tok = max(pages[u], 0) * kBlockSize + lg * 4;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const bool v = pages[u] >= 0 && sees(a, col_lo[n], col_last[n], tok + r);
-                        x[n][u][r] = v ? x[n][u][r] : -INFINITY;
-                        vis[n] |= v ? 1u << (4 * u + r) : 0;
-                    }
+                    for (int r = 0; r < 4; ++r) x[n][u][r] = pages[u] >= 0 && sees(a, col_lo[n], col_last[n], tok + r) ? x[n][u][r] : -INFINITY;
                 }
-            }
         }
         uint4 pt[NC][NT][2];
 #pragma unroll
@@ -747,13 +859,17 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void row_many_kernel(RowAttnArgs 
                     }
 #pragma unroll
                 for (int i = 0; i < NT; ++i) {
-                    float t[2][4];
+                    if (F32) {
+                        float t[2][4];
 #pragma unroll
-                    for (int y = 0; y < 2; ++y)
+                        for (int y = 0; y < 2; ++y)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) t[y][r] = F32 ? term3(p[y][r], i) : p[y][r];
-                    pt[n][i][z] = make_uint4(pack_bf16_rne(t[0][0], t[0][1]), pack_bf16_rne(t[0][2], t[0][3]), pack_bf16_rne(t[1][0], t[1][1]),
-                                             pack_bf16_rne(t[1][2], t[1][3]));
+                            for (int r = 0; r < 4; ++r) t[y][r] = rest3(p[y][r], i);
+                        pt[n][i][z] = make_uint4(uppers(t[0][0], t[0][1]), uppers(t[0][2], t[0][3]), uppers(t[1][0], t[1][1]), uppers(t[1][2], t[1][3]));
+                    } else {
+                        pt[n][i][z] = make_uint4(pack_bf16_rne(p[0][0], p[0][1]), pack_bf16_rne(p[0][2], p[0][3]), pack_bf16_rne(p[1][0], p[1][1]),
+                                                 pack_bf16_rne(p[1][2], p[1][3]));
+                    }
                 }
             }
         }
@@ -762,24 +878,9 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void row_many_kernel(RowAttnArgs 
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 uint4 vw = s_v[buf][z][b][lane];
-                if (FMT == kFmtBf16 && !full) {  // what some columns see and others do not must not reach these: 0 * NaN
-                    const uint4 ones = make_uint4(not_finite(vw.x), not_finite(vw.y), not_finite(vw.z), not_finite(vw.w));
-                    if (__any((ones.x | ones.y | ones.z | ones.w) != 0)) {
-                        vw = make_uint4(without(vw.x, ones.x), without(vw.y, ones.y), without(vw.z, ones.z), without(vw.w, ones.w));
-#pragma unroll
-                        for (int n = 0; n < NC; ++n) {
-                            uint32_t on[4];
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                const uint32_t two = vis[n] >> (8 * z + 2 * r) & 3;
-                                on[r] = (two & 1 ? 0x3f80u : 0) | (two & 2 ? 0x3f800000u : 0);
-                            }
-                            uint4 seen4 = make_uint4(on[0], on[1], on[2], on[3]), one4 = ones;
-                            const floatx4 met = mfma32(*reinterpret_cast<bf16x8*>(&one4), *reinterpret_cast<bf16x8*>(&seen4), floatx4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) o[n][b][r] = met[r] > 0.f ? NAN : o[n][b][r];
-                        }
-                    }
+                if (FMT == kFmtBf16 && !full && __any((not_finite(vw.x) | not_finite(vw.y) | not_finite(vw.z) | not_finite(vw.w)) != 0)) {
+                    marked = true;
+                    vw = finite_only(vw);
                 }
 #pragma unroll
                 for (int n = 0; n < NC; ++n)
@@ -801,6 +902,7 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void row_many_kernel(RowAttnArgs 
             compute(buf);
             if (st + 1 < st1) put(buf ^ 1);
         }
+        if (FMT == kFmtBf16 && marked) mark_not_finite<D, NC, 4>(a, span, seen, btrow, c, st0 * 4, min(st1 * 4, span.n), col_lo, col_last, o);
     }
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
@@ -894,12 +996,13 @@ static RowShape row_shape(int n_q, int n_kv, int d, int batch, int rows, int max
     return s;
 }
 
-template <int D, int FMT, bool F32>
+template <int D, int FMT, bool F32, bool MULTI>
 static void launch_few(const RowAttnArgs& a, const RowShape& s, hipStream_t st) {
+    constexpr bool TERMS = F32 || FMT == kFmtInt8;
     const dim3 grid((unsigned)(s.few_wgs * a.n_kv));
-    if (!F32 || s.cw == 16) launch(row_few_kernel<D, FMT, F32, 16>, grid, dim3(256), st, a);
-    else if (s.cw == 8) launch(row_few_kernel<D, FMT, F32, F32 ? 8 : 16>, grid, dim3(256), st, a);
-    else launch(row_few_kernel<D, FMT, F32, F32 ? 4 : 16>, grid, dim3(256), st, a);
+    if (!TERMS || s.cw == 16) launch(row_few_kernel<D, FMT, F32, 16, MULTI>, grid, dim3(256), st, a);
+    else if (s.cw == 8) launch(row_few_kernel<D, FMT, F32, TERMS ? 8 : 16, MULTI>, grid, dim3(256), st, a);
+    else launch(row_few_kernel<D, FMT, F32, TERMS ? 4 : 16, MULTI>, grid, dim3(256), st, a);
     launch(row_few_merge_kernel<D, F32>, dim3((unsigned)((int64_t)s.passes_max * a.n_kv * a.pcols)), dim3(256), st, a);
 }
 template <int D, int FMT, bool F32>
@@ -908,7 +1011,8 @@ static void launch_rows(const RowAttnArgs& a, const RowShape& s, hipStream_t st)
         launch(row_many_kernel<D, FMT, F32>, dim3((unsigned)((int64_t)s.slots * a.splits * a.n_kv)), dim3(256), st, a);
         if (a.splits > 1) launch(row_many_merge_kernel<D, F32>, dim3((unsigned)(s.slots * a.n_kv)), dim3(256), st, a);
     }
-    launch_few<D, FMT, F32>(a, s, st);
+    if (a.max_new > 1) launch_few<D, FMT, F32, true>(a, s, st);
+    else launch_few<D, FMT, F32, false>(a, s, st);
 }
 template <int FMT>
 static void launch_format(const RowAttnArgs& a, const RowShape& s, int d, bool f32, hipStream_t st) {
