@@ -10,6 +10,7 @@
 // are their weights.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "cache8.h"
 #include "kv_layout.h"
@@ -60,22 +61,18 @@ __device__ __forceinline__ Span span_of(const RowAttnArgs& a, int64_t p0, int64_
 
 // the columns of a pass or a wave: tokens at the positions first .. last
 struct Seen {
-    int first_lo, last_lo;  // first position in the window of the first and of the last token
-    int first, last;        // last position that the first and the last token see
+    int first_lo, last;                // first position in the window of the first token; last position that the last one sees
+    int full_from, full_to, full_sinks;  // pages that every column sees all of: from .. to, and those below sinks
 };
+constexpr int kNoPage = 0x7fffffff;  // an entry that is no page: behind all of them
 __device__ __forceinline__ Seen seen_of(const RowAttnArgs& a, int64_t p0, int64_t p1) {
-    return Seen{first_seen(a, p0), first_seen(a, p1), last_seen(a, p0), last_seen(a, p1)};
+    return Seen{first_seen(a, p0), last_seen(a, p1), first_seen(a, p1) / kBlockSize + (first_seen(a, p1) % kBlockSize != 0),
+                (last_seen(a, p0) + 1) / kBlockSize - 1, a.n_sinks / kBlockSize};
 }
-// every column sees all of the page / some column may see some of it
-__device__ __forceinline__ bool all_seen(const RowAttnArgs& a, const Seen& s, int page) {
-    const int t0 = page * kBlockSize, t1 = t0 + kBlockSize - 1;
-    return page >= 0 && t1 <= s.first && (t0 >= s.last_lo || t1 < a.n_sinks);
+__device__ __forceinline__ bool all_seen(const Seen& s, int page) { return (page <= s.full_to) & ((page >= s.full_from) | (page < s.full_sinks)); }
+__device__ __forceinline__ bool sees(const RowAttnArgs& a, int lo, int last, int tok) {
+    return (tok <= last) & ((tok >= lo) | (tok < a.n_sinks));
 }
-__device__ __forceinline__ bool some_seen(const RowAttnArgs& a, const Seen& s, int page) {
-    const int t0 = page * kBlockSize, t1 = t0 + kBlockSize - 1;
-    return page >= 0 && t0 <= s.last && (t1 >= s.first_lo || t0 < a.n_sinks);
-}
-__device__ __forceinline__ bool sees(const RowAttnArgs& a, int lo, int last, int tok) { return tok <= last && (tok >= lo || tok < a.n_sinks); }
 
 // masks of the bf16 pairs (0, 1) and (2, 3), or of the bytes, of the tokens tok .. tok+3 that some column sees
 __device__ __forceinline__ uint4 seen_masks(const RowAttnArgs& a, const Seen& s, bool there, int tok) {
@@ -85,6 +82,10 @@ __device__ __forceinline__ uint4 seen_masks(const RowAttnArgs& a, const Seen& s,
     const uint32_t bytes = (v[0] ? 0xffu : 0) | (v[1] ? 0xff00u : 0) | (v[2] ? 0xff0000u : 0) | (v[3] ? 0xff000000u : 0);
     return make_uint4((v[0] ? 0xffffu : 0) | (v[1] ? 0xffff0000u : 0), (v[2] ? 0xffffu : 0) | (v[3] ? 0xffff0000u : 0), bytes, 0);
 }
+
+// What a softmax's weights are relative to follows the running maximum only when that has grown by more than this many powers of two: weights
+// and their sums stay below 2^8 times their number, in floating point as exact as below 1, and outputs are scaled once or twice a row.
+constexpr float kSlack = 8.f;
 
 // ---- operands ---------------------------------------------------------------------------------------------------
 
@@ -138,20 +139,20 @@ __device__ __forceinline__ void mark_not_finite(const RowAttnArgs& a, const Span
                                                 const int (&col_last)[NC], floatx4 (&o)[NC][D / 16]) {
     const int lane = threadIdx.x & 63, lg = lane >> 4;
     auto there = [&](int j, int& block) {
-        const int page = j < j1 ? span.page(j) : -1;
-        block = page >= 0 && page < a.max_blocks ? __builtin_amdgcn_readfirstlane(btrow[page]) : -1;
-        return block < 0 || block >= a.num_blocks ? -1 : page;
+        const int page = j < j1 ? span.page(j) : kNoPage;
+        block = page < a.max_blocks ? __builtin_amdgcn_readfirstlane(btrow[page]) : -1;
+        return block < 0 || block >= a.num_blocks ? kNoPage : page;
     };
 #pragma unroll 1
     for (int j = j0; j < j1; ++j) {
         int block;
         const int page = there(j, block), stage = j0 + (j - j0) / NPG * NPG;
-        if (page < 0) continue;
+        if (page == kNoPage) continue;
         bool full = true;
 #pragma unroll 1
         for (int u = 0; u < NPG; ++u) {
             int other;
-            full = full && all_seen(a, seen, there(stage + u, other));
+            full = full && all_seen(seen, there(stage + u, other));
         }
         if (full) continue;
         const int tok = page * kBlockSize + lg * 4;
@@ -297,9 +298,9 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                 int lbase = j0, v_page, v_block, v_exp = 0;
                 auto fetch = [&] {
                     const int j = lbase + lane;
-                    int pg = j < j1 ? span.page(j) : -1, blk = -1;
-                    if (pg >= 0 && pg < a.max_blocks) blk = btrow[pg];
-                    if (blk < 0 || blk >= a.num_blocks) pg = -1, blk = 0;  // nothing there: page 0 of the pool is read and masked
+                    int pg = j < j1 ? span.page(j) : kNoPage, blk = -1;
+                    if (pg < a.max_blocks) blk = btrow[pg];
+                    if (blk < 0 || blk >= a.num_blocks) pg = kNoPage, blk = 0;  // nothing there: page 0 of the pool is read and masked
                     v_page = pg;
                     v_block = blk;
                     if (FMT != kFmtBf16) v_exp = *reinterpret_cast<const uint16_t*>(a.exps + ((int64_t)blk * n_kv + c) * 2);
@@ -317,7 +318,7 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                     for (int u = 0; u < NPG; ++u) {
                         const bool there = j + u < j1;
                         const int l = (j + u - lbase) & 63;
-                        s.page[u] = there ? __builtin_amdgcn_readlane(v_page, l) : -1;
+                        s.page[u] = there ? __builtin_amdgcn_readlane(v_page, l) : kNoPage;
                         const int blk = there ? __builtin_amdgcn_readlane(v_block, l) : 0;
                         s.exp[u] = FMT == kFmtBf16 || !there ? 0 : __builtin_amdgcn_readlane(v_exp, l);
                         const uint8_t* tile = a.tiles + ((int64_t)blk * n_kv + c) * (2 * TILE) + lane * 16;
@@ -333,7 +334,7 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                 floatx4 oo[1][D / 16], (&o)[D / 16] = oo[0];
 #pragma unroll
                 for (int t = 0; t < D / 16; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-                float m_run = -INFINITY, l_run = 0.f;
+                float m_ref = -INFINITY, l_run = 0.f;
                 bool marked = false;
 
                 fetch();
@@ -423,7 +424,7 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                     __builtin_amdgcn_sched_barrier(0);
                     bool full = true;
 #pragma unroll
-                    for (int u = 0; u < NPG; ++u) full = full && all_seen(a, seen, cur.page[u]);
+                    for (int u = 0; u < NPG; ++u) full &= all_seen(seen, cur.page[u]);
                     floatx4 x[NPG];
                     float ks[NPG], vs[NPG];
 #pragma unroll
@@ -465,8 +466,8 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                     if (!full) {
 #pragma unroll
                         for (int u = 0; u < NPG; ++u) {
-                            const bool there = cur.page[u] >= 0;
-                            const int tok = max(cur.page[u], 0) * kBlockSize + lg * 4;
+                            const bool there = cur.page[u] != kNoPage;
+                            const int tok = (there ? cur.page[u] : 0) * kBlockSize + lg * 4;
                             if (!there) vs[u] = 0.f;
 #pragma unroll
                             for (int r = 0; r < 4; ++r) x[u][r] = there && sees(a, lo1[0], last1[0], tok + r) ? x[u][r] : -INFINITY;
@@ -502,16 +503,25 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                     for (int u = 0; u < NPG; ++u)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[u][r]);
-                    mx = fmaxf(mx, __shfl_xor(mx, 16));
-                    mx = fmaxf(mx, __shfl_xor(mx, 32));
-                    const float m_new = fmaxf(m_run, mx), m_use = fmaxf(m_new, -1e30f);  // nothing seen yet: finite exponents, weights 0
-                    if (__any(m_new > m_run)) {
-                        const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+                    const bool grown = __any(mx > m_ref + kSlack);
+                    float alpha = 1.f;
+                    if (grown) {
+                        mx = fmaxf(mx, __shfl_xor(mx, 16));
+                        mx = fmaxf(mx, __shfl_xor(mx, 32));
+                        const float m_new = fmaxf(m_ref, mx);
+                        alpha = __builtin_amdgcn_exp2f(m_ref - fmaxf(m_new, -1e30f));
+                        m_ref = m_new;
                         l_run *= alpha;
-#pragma unroll
-                        for (int t = 0; t < D / 16; ++t) o[t] *= alpha;
                     }
-                    m_run = m_new;
+#pragma unroll
+                    for (int t = 0; t < D / 16; t += 4) {  // four blocks to a branch: the compiler holds what a branch changes twice
+                        if (grown) {
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) o[t + z] *= alpha;
+                        }
+                        asm volatile("");
+                    }
+                    const float m_use = fmaxf(m_ref, -1e30f);  // nothing seen yet: finite exponents, weights 0
 #pragma unroll
                     for (int u = 0; u < NPG; u += 2) {
                         float pr[2][4];
@@ -579,14 +589,14 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                 }
                 if (grp == 0 && on) {
                     if (segs == 1) {
-                        const float den = l_run > 0.f || l_run != l_run ? l_run : 1.f;
+                        const float by = 1.f / (l_run > 0.f || l_run != l_run ? l_run : 1.f);
 #pragma unroll
                         for (int t = 0; t < D / 16; ++t)
-                            store_row<D, F32>(a, row0 + t0 + tq, c * a.G + h, t * 16 + lg * 4, floatx4{o[t][0] / den, o[t][1] / den, o[t][2] / den, o[t][3] / den});
+                            store_row<D, F32>(a, row0 + t0 + tq, c * a.G + h, t * 16 + lg * 4, o[t] * by);
                     } else {
                         const int64_t slot = ((int64_t)(w + v) * n_kv + c) * a.pcols + ci;
                         if (lg == 0) {
-                            a.part_ml[slot * 2] = fmaxf(m_run, -1e30f);
+                            a.part_ml[slot * 2] = fmaxf(m_ref, -1e30f);
                             a.part_ml[slot * 2 + 1] = l_run;
                         }
 #pragma unroll
@@ -649,7 +659,7 @@ __global__ __launch_bounds__(256) void row_few_merge_kernel(RowAttnArgs a) {
 // that they see together, four at a time: each wave brings one page into LDS, as bf16 in operand order, while the four before are multiplied.
 // A column group's maxima, sums and outputs stay in registers.  Tiles with the most pages begin first.  Where there are few tiles
 // the pages of each are dealt to `splits` workgroups.
-constexpr int kManyCols = 128, kManyTiles = 2;  // columns of a workgroup; column tiles of a wave
+constexpr int kManyTiles = 2, kManyCols = 64 * kManyTiles;  // column tiles of a wave; columns of a workgroup
 struct ManyTile {
     int r0, t0, tv, req;
     int64_t old;
@@ -677,11 +687,15 @@ __device__ __forceinline__ bool many_tile(const RowAttnArgs& a, int slot, ManyTi
 }
 
 template <int D, int FMT, bool F32>
-__global__ __launch_bounds__(256, F32 ? 1 : 2) void row_many_kernel(RowAttnArgs a) {
+__global__ __launch_bounds__(256, F32 ? 2 : 3) void row_many_kernel(RowAttnArgs a) {
     constexpr int KSTEPS = D / 32, P = pieces<FMT>(D), NB = D / 16, NC = kManyTiles, NT = F32 ? 3 : 1;
     constexpr int TILE = FMT == kFmtBf16 ? 32 * D : 16 * D;
-    __shared__ uint4 s_k[2][4][KSTEPS][64];  // [buffer][page][step][lane]
-    __shared__ uint4 s_v[2][2][NB][64];      // [buffer][pair of pages][16 dims][lane]: 4 tokens of either page
+    // What a wave brings of a stage: pieces of K (KEYS of them), and of V a piece (bf16) or half of one (8 bits) of both pages
+    constexpr int KEYS = (2 * P + 3) / 4, VALUES = FMT == kFmtBf16 ? P : 2 * P;
+    __shared__ uint4 s_k[2][2][KSTEPS][64];  // [buffer][page][step][lane]
+    __shared__ uint4 s_v[2][NB][64];         // [buffer][16 dims][lane]: 4 tokens of either page
+    __shared__ int s_marked;                 // some value was no finite number
+    if (threadIdx.x == 0) s_marked = 0;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n_kv = a.n_kv, c = blockIdx.x % n_kv, rest = blockIdx.x / n_kv, split = rest % a.splits, slot = rest / a.splits;
@@ -691,7 +705,7 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void row_many_kernel(RowAttnArgs 
     const int live = a.G * m.tv;
     const Span span = span_of(a, m.old + m.t0, m.old + m.t0 + m.tv - 1);
     const Seen tile_seen = seen_of(a, m.old + m.t0, m.old + m.t0 + m.tv - 1);
-    const int stages = (span.n + 3) / 4, st0 = (int)((int64_t)stages * split / a.splits), st1 = (int)((int64_t)stages * (split + 1) / a.splits);
+    const int stages = (span.n + 1) / 2, st0 = (int)((int64_t)stages * split / a.splits), st1 = (int)((int64_t)stages * (split + 1) / a.splits);
     const int32_t* btrow = a.bt + (size_t)m.req * a.max_blocks;
 
     // the wave's columns
@@ -728,199 +742,274 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void row_many_kernel(RowAttnArgs 
         }
     }
     floatx4 o[NC][NB];
-    float m_run[NC], l_run[NC];
-    bool marked = false;
+    float m_ref[NC];
+    floatx4 l_run[NC];  // fp32: the lane's own tokens' sum in [0]; bf16: all tokens', of the rounded weights, by a product with ones
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
-        m_run[n] = -INFINITY;
-        l_run[n] = 0.f;
+        m_ref[n] = -INFINITY;
+        l_run[n] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int b = 0; b < NB; ++b) o[n][b] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
 
     // lane l holds entry lbase + l of the span
-    int lbase = st0 * 4, v_page, v_block, v_exp = 0;
+    int lbase = st0 * 2, v_page, v_block, v_exp = 0;
     auto fetch = [&] {
         const int j = lbase + lane;
-        int pg = j < span.n ? span.page(j) : -1, blk = -1;
-        if (pg >= 0 && pg < a.max_blocks) blk = btrow[pg];
-        if (blk < 0 || blk >= a.num_blocks) pg = -1, blk = 0;
+        int pg = j < span.n ? span.page(j) : kNoPage, blk = -1;
+        if (pg < a.max_blocks) blk = btrow[pg];
+        if (blk < 0 || blk >= a.num_blocks) pg = kNoPage, blk = 0;
         v_page = pg;
         v_block = blk;
-        if (FMT != kFmtBf16) v_exp = *reinterpret_cast<const uint16_t*>(a.exps + ((int64_t)blk * n_kv + c) * 2);
+        if (FMT != kFmtBf16) {
+            v_exp = *reinterpret_cast<const uint16_t*>(a.exps + ((int64_t)blk * n_kv + c) * 2);
+            if (pg == kNoPage) v_exp = 0;  // whatever page 0 has: its values are cleared
+        }
     };
-    u32x4 rk[P], rv[P];  // the wave's page of the stage that comes next
-    int r_page = -1, r_exp = 0, pages[4], next_pages[4];
-    auto load = [&](int st) {
-        if (st * 4 - lbase >= 64) {
-            lbase = st * 4;
+    u32x4 rk[FMT == kFmtBf16 ? 1 : KEYS], rv[2];  // what the wave brings of the stage that comes next
+    int exps[2] = {0, 0}, cur_exps[2], pages[2], next_pages[2];
+    const int v_unit = wave - (4 - VALUES);  // below 0: no V
+    auto load = [&](int st, int buf) {
+        if (st * 2 - lbase >= 64) {
+            lbase = st * 2;
             fetch();
         }
-        const int l = st * 4 - lbase;  // 4 divides 64
+        const int l = st * 2 - lbase;  // 2 divides 64
+        const uint8_t* tile[2];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) next_pages[u] = __builtin_amdgcn_readlane(v_page, l + u);
-        r_page = __builtin_amdgcn_readlane(v_page, l + wave);
-        r_exp = __builtin_amdgcn_readlane(v_exp, l + wave);
-        const uint8_t* tile = a.tiles + ((int64_t)__builtin_amdgcn_readlane(v_block, l + wave) * n_kv + c) * (2 * TILE) + lane * 16;
+        for (int u = 0; u < 2; ++u) {
+            next_pages[u] = __builtin_amdgcn_readlane(v_page, l + u);
+            exps[u] = __builtin_amdgcn_readlane(v_exp, l + u);
+            tile[u] = a.tiles + ((int64_t)__builtin_amdgcn_readlane(v_block, l + u) * n_kv + c) * (2 * TILE);
+        }
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-            rk[i] = *reinterpret_cast<const u32x4*>(tile + i * 1024);
-            rv[i] = *reinterpret_cast<const u32x4*>(tile + TILE + i * 1024);
+        for (int i = 0; i < KEYS; ++i) {
+            const int k = wave * KEYS + i, page = k / P, piece = k % P;
+            if (k < 2 * P) {  // uniform
+                const uint8_t* src = (page ? tile[1] : tile[0]) + piece * 1024 + lane * 16;
+                if (FMT == kFmtBf16) global_to_lds_16(src, lds_address(&s_k[buf][page][piece][0]));
+                else rk[i] = *reinterpret_cast<const u32x4*>(src);
+            }
+        }
+        if (v_unit >= 0) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint8_t* src = tile[u] + TILE + lane * 16;
+                if (FMT == kFmtBf16) rv[u] = *reinterpret_cast<const u32x4*>(src + v_unit * 1024);
+                else {
+                    const uint2 half = *reinterpret_cast<const uint2*>(src + v_unit / 2 * 1024 + v_unit % 2 * 8);
+                    rv[u][0] = half.x;
+                    rv[u][1] = half.y;
+                }
+            }
         }
     };
     auto put = [&](int buf) {
-        if (!all_seen(a, tile_seen, r_page)) {  // what no column of the tile sees may hold anything
-            const uint4 keep = seen_masks(a, tile_seen, r_page >= 0, max(r_page, 0) * kBlockSize + lg * 4);
+        if (FMT != kFmtBf16) {
 #pragma unroll
-            for (int i = 0; i < P; ++i) {
-                rv[i] &= FMT == kFmtBf16 ? u32x4{keep.x, keep.y, keep.x, keep.y} : u32x4{keep.z, keep.z, keep.z, keep.z};
+            for (int i = 0; i < KEYS; ++i) {
+                const int k = wave * KEYS + i, page = k / P, piece = k % P;
+                if (k < 2 * P) {
+                    const float ks = FMT == kFmtE4m3 ? two_to((int8_t)((page ? exps[1] : exps[0]) & 0xff)) : 1.f;
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const uint2 x = widen8<FMT>(rk[i][2 * s], ks), y = widen8<FMT>(rk[i][2 * s + 1], ks);
+                        s_k[buf][page][2 * piece + s][lane] = make_uint4(x.x, x.y, y.x, y.y);
+                    }
+                }
             }
         }
-        const float ks = two_to((int8_t)(r_exp & 0xff)), vs = r_page >= 0 ? two_to((int8_t)(r_exp >> 8)) : 0.f;
-        uint2* dv = reinterpret_cast<uint2*>(&s_v[buf][wave / 2][0][lane]) + wave % 2;
+        if (v_unit < 0) return;
+        float vs[2] = {1.f, 1.f};
 #pragma unroll
-        for (int s = 0; s < KSTEPS; ++s) {
-            if (FMT == kFmtBf16) *reinterpret_cast<u32x4*>(&s_k[buf][wave][s][lane]) = rk[s % P];
+        for (int u = 0; u < 2; ++u) {
+            if (FMT == kFmtE4m3) vs[u] = two_to((int8_t)(exps[u] >> 8));
+            if (!all_seen(tile_seen, next_pages[u])) {  // what no column of the tile sees may hold anything
+                const bool there = next_pages[u] != kNoPage;
+                const uint4 keep = seen_masks(a, tile_seen, there, (there ? next_pages[u] : 0) * kBlockSize + lg * 4);
+                rv[u] &= FMT == kFmtBf16 ? u32x4{keep.x, keep.y, keep.x, keep.y} : u32x4{keep.z, keep.z, keep.z, keep.z};
+                if (FMT == kFmtBf16) {
+                    const uint32_t bad = not_finite(rv[u][0]) | not_finite(rv[u][1]) | not_finite(rv[u][2]) | not_finite(rv[u][3]);
+                    if (__any(bad != 0)) {
+                        s_marked = 1;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) rv[u][e] = without(rv[u][e], not_finite(rv[u][e]));
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {  // two blocks of 16 dims
+            if (FMT == kFmtBf16) s_v[buf][2 * v_unit + b][lane] = make_uint4(rv[0][2 * b], rv[0][2 * b + 1], rv[1][2 * b], rv[1][2 * b + 1]);
             else {
-                const uint2 x = widen8<FMT>(rk[s / 2][s % 2 * 2], ks), y = widen8<FMT>(rk[s / 2][s % 2 * 2 + 1], ks);
-                s_k[buf][wave][s][lane] = make_uint4(x.x, x.y, y.x, y.y);
+                const uint2 x = widen8<FMT>(rv[0][b], vs[0]), y = widen8<FMT>(rv[1][b], vs[1]);
+                s_v[buf][2 * v_unit + b][lane] = make_uint4(x.x, x.y, y.x, y.y);
             }
-        }
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            if (FMT == kFmtBf16) {
-                const u32x4 v = rv[b / 2 % P];
-                dv[b * 128] = b % 2 ? make_uint2(v[2], v[3]) : make_uint2(v[0], v[1]);
-            } else dv[b * 128] = widen8<FMT>(rv[b / 4][b % 4], vs);
         }
     };
 
     auto compute = [&](int buf) {
-        bool full = true, any = false;
+        if (idle) return;
+        // int8 codes are multiplied as they are: the keys' power of two goes to the scores, the values' to the weights, and out of their sum again
+        constexpr bool INT8 = FMT == kFmtInt8, SCALED = INT8 || !F32;
+        float ks[2], ev[2], vdown[2];
+        uint32_t one[2] = {0x3f803f80u, 0x3f803f80u};
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            full = full && all_seen(a, seen, pages[u]);
-            any = any || some_seen(a, seen, pages[u]);
+        for (int u = 0; u < 2; ++u) {
+            ks[u] = F32 ? 1.f : a.scale_log2e;
+            if (INT8) {
+                const int e = (int8_t)(cur_exps[u] >> 8);
+                ks[u] *= two_to((int8_t)(cur_exps[u] & 0xff));
+                ev[u] = (float)e;
+                vdown[u] = two_to(-e);
+                one[u] = (uint32_t)(127 - e) << 23 | (uint32_t)(127 - e) << 7;
+            }
         }
-        if (idle || !any) return;
-        floatx4 x[NC][4];
+        floatx4 x[NC][2];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int s = 0; s < KSTEPS; ++s)
 #pragma unroll
-            for (int n = 0; n < NC; ++n) x[n][u] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < KSTEPS; ++s) {
+            for (int u = 0; u < 2; ++u) {
                 uint4 kw = s_k[buf][u][s][lane];
 #pragma unroll
                 for (int n = 0; n < NC; ++n)
 #pragma unroll
-                    for (int i = 0; i < NT; ++i) x[n][u] = mfma32(*reinterpret_cast<bf16x8*>(&kw), *reinterpret_cast<bf16x8*>(&qt[n][i][s]), x[n][u]);
+                    for (int i = 0; i < NT; ++i)
+                        x[n][u] = mfma32(*reinterpret_cast<bf16x8*>(&kw), *reinterpret_cast<bf16x8*>(&qt[n][i][s]),
+                                         s == 0 && i == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : x[n][u]);
             }
-        }
-        if (!full) {
 #pragma unroll
-            for (int n = 0; n < NC; ++n)
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int tok = max(pages[u], 0) * kBlockSize + lg * 4;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) x[n][u][r] = pages[u] >= 0 && sees(a, col_lo[n], col_last[n], tok + r) ? x[n][u][r] : -INFINITY;
-                }
-        }
-        uint4 pt[NC][NT][2];
-#pragma unroll
-        for (int n = 0; n < NC; ++n) {
-            float mx = -INFINITY;
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[n][u][r]);
-            mx = fmaxf(mx, __shfl_xor(mx, 16));
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            if (!F32) mx *= a.scale_log2e;
-            const float m_new = fmaxf(m_run[n], mx), m_use = fmaxf(m_new, -1e30f);
-            if (__any(m_new > m_run[n])) {
-                const float alpha = __builtin_amdgcn_exp2f(m_run[n] - m_use);
-                l_run[n] *= alpha;
-#pragma unroll
-                for (int b = 0; b < NB; ++b) o[n][b] *= alpha;
-            }
-            m_run[n] = m_new;
-#pragma unroll
-            for (int z = 0; z < 2; ++z) {
-                float p[2][4];
-#pragma unroll
-                for (int y = 0; y < 2; ++y)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float s = x[n][2 * z + y][r];
-                        p[y][r] = __builtin_amdgcn_exp2f(F32 ? s - m_use : fmaf(s, a.scale_log2e, -m_use));
-                        l_run[n] += p[y][r];
-                    }
-#pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    if (F32) {
-                        float t[2][4];
-#pragma unroll
-                        for (int y = 0; y < 2; ++y)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) t[y][r] = rest3(p[y][r], i);
-                        pt[n][i][z] = make_uint4(uppers(t[0][0], t[0][1]), uppers(t[0][2], t[0][3]), uppers(t[1][0], t[1][1]), uppers(t[1][2], t[1][3]));
-                    } else {
-                        pt[n][i][z] = make_uint4(pack_bf16_rne(p[0][0], p[0][1]), pack_bf16_rne(p[0][2], p[0][3]), pack_bf16_rne(p[1][0], p[1][1]),
-                                                 pack_bf16_rne(p[1][2], p[1][3]));
-                    }
-                }
-            }
-        }
-#pragma unroll
-        for (int z = 0; z < 2; ++z)
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                uint4 vw = s_v[buf][z][b][lane];
-                if (FMT == kFmtBf16 && !full && __any((not_finite(vw.x) | not_finite(vw.y) | not_finite(vw.z) | not_finite(vw.w)) != 0)) {
-                    marked = true;
-                    vw = finite_only(vw);
-                }
+        for (int u = 0; u < 2; ++u)
+            if (!all_seen(seen, pages[u])) {
+                const bool there = pages[u] != kNoPage;
+                const int tok = (there ? pages[u] : 0) * kBlockSize + lg * 4;
 #pragma unroll
                 for (int n = 0; n < NC; ++n)
 #pragma unroll
-                    for (int i = 0; i < NT; ++i) o[n][b] = mfma32(*reinterpret_cast<bf16x8*>(&vw), *reinterpret_cast<bf16x8*>(&pt[n][i][z]), o[n][b]);
+                    for (int r = 0; r < 4; ++r) x[n][u][r] = there && sees(a, col_lo[n], col_last[n], tok + r) ? x[n][u][r] : -INFINITY;
             }
+        float top[NC];
+        bool above = false;
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            top[n] = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const float t = fmaxf(fmaxf(x[n][u][0], x[n][u][1]), fmaxf(x[n][u][2], x[n][u][3]));
+                top[n] = fmaxf(top[n], SCALED ? t * ks[u] : t);
+            }
+            above |= top[n] > m_ref[n] + kSlack;
+        }
+        const bool grown = __any(above);
+        float alpha[NC];
+        if (grown) {
+#pragma unroll
+            for (int n = 0; n < NC; ++n) {
+                top[n] = fmaxf(top[n], __shfl_xor(top[n], 16));
+                top[n] = fmaxf(top[n], __shfl_xor(top[n], 32));
+                const float m_new = fmaxf(m_ref[n], top[n]);
+                alpha[n] = __builtin_amdgcn_exp2f(m_ref[n] - fmaxf(m_new, -1e30f));
+                m_ref[n] = m_new;
+                l_run[n] *= alpha[n];
+            }
+        }
+        // four blocks to a branch: the compiler holds what a branch changes twice
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+#pragma unroll
+            for (int b = 0; b < NB; b += 4) {
+                if (grown) {
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) o[n][b + z] *= alpha[n];
+                }
+                asm volatile("");
+            }
+        uint4 pt[NC][NT];
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            const float m_use = fmaxf(m_ref[n], -1e30f);  // nothing seen yet: finite exponents, weights 0
+            float p[2][4];
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const float off = INT8 ? ev[y] - m_use : -m_use;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float s = x[n][y][r];
+                    p[y][r] = __builtin_amdgcn_exp2f(SCALED ? fmaf(s, ks[y], off) : s + off);
+                    if (F32) l_run[n][0] += INT8 ? p[y][r] * vdown[y] : p[y][r];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                if (F32) {
+                    float t[2][4];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) t[y][r] = rest3(p[y][r], i);
+                    pt[n][i] = make_uint4(uppers(t[0][0], t[0][1]), uppers(t[0][2], t[0][3]), uppers(t[1][0], t[1][1]), uppers(t[1][2], t[1][3]));
+                } else {
+                    pt[n][i] = make_uint4(pack_bf16_rne(p[0][0], p[0][1]), pack_bf16_rne(p[0][2], p[0][3]), pack_bf16_rne(p[1][0], p[1][1]),
+                                          pack_bf16_rne(p[1][2], p[1][3]));
+                    uint4 ones = make_uint4(one[0], one[0], one[1], one[1]);
+                    l_run[n] = mfma32(*reinterpret_cast<bf16x8*>(&ones), *reinterpret_cast<bf16x8*>(&pt[n][i]), l_run[n]);
+                }
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            uint4 vw = s_v[buf][b][lane];
+#pragma unroll
+            for (int n = 0; n < NC; ++n)
+#pragma unroll
+                for (int i = 0; i < NT; ++i) o[n][b] = mfma32(*reinterpret_cast<bf16x8*>(&vw), *reinterpret_cast<bf16x8*>(&pt[n][i]), o[n][b]);
+        }
     };
 
     if (st0 < st1) {
         fetch();
-        load(st0);
+        load(st0, 0);
+        lds_barrier();  // s_marked is 0
         put(0);
         for (int st = st0; st < st1; ++st) {
             const int buf = (st - st0) & 1;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) pages[u] = next_pages[u];
-            if (st + 1 < st1) load(st + 1);
-            lds_barrier();  // the stage is whole, and its other buffer is no longer read
+            for (int u = 0; u < 2; ++u) {
+                pages[u] = next_pages[u];
+                cur_exps[u] = exps[u];
+            }
+            if (FMT == kFmtBf16) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the keys that went to LDS by themselves
+            lds_barrier();                                                        // the stage is whole, and its other buffer is no longer read
+            load(min(st + 1, st1 - 1), buf ^ 1);  // without a branch, so that nobody waits for it before it is put
             compute(buf);
             if (st + 1 < st1) put(buf ^ 1);
         }
-        if (FMT == kFmtBf16 && marked) mark_not_finite<D, NC, 4>(a, span, seen, btrow, c, st0 * 4, min(st1 * 4, span.n), col_lo, col_last, o);
+        // the last load has gone to LDS that nobody reads; it ends before the workgroup gives it up
+        if (FMT == kFmtBf16) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            lds_barrier();
+            if (s_marked) mark_not_finite<D, NC, 1>(a, span, tile_seen, btrow, c, st0 * 2, min(st1 * 2, span.n), col_lo, col_last, o);
+        }
     }
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
-        l_run[n] += __shfl_xor(l_run[n], 16);
-        l_run[n] += __shfl_xor(l_run[n], 32);
+        float l = l_run[n][0];
+        if (F32) {
+            l += __shfl_xor(l, 16);
+            l += __shfl_xor(l, 32);
+        }
         const int ci = wc + n * 16 + col, tq = ci / a.G, h = ci - tq * a.G;
         if (ci >= live) continue;
         if (a.splits == 1) {
-            const float den = l_run[n] > 0.f || l_run[n] != l_run[n] ? l_run[n] : 1.f;
+            const float by = 1.f / (l > 0.f || l != l ? l : 1.f);
 #pragma unroll
             for (int b = 0; b < NB; ++b)
-                store_row<D, F32>(a, (int64_t)m.r0 + m.t0 + tq, c * a.G + h, b * 16 + lg * 4,
-                                  floatx4{o[n][b][0] / den, o[n][b][1] / den, o[n][b][2] / den, o[n][b][3] / den});
+                store_row<D, F32>(a, (int64_t)m.r0 + m.t0 + tq, c * a.G + h, b * 16 + lg * 4, o[n][b] * by);
         } else {
             const int64_t at = (((int64_t)slot * n_kv + c) * a.splits + split) * kManyCols + ci;
             if (lg == 0) {
-                a.many_ml[at * 2] = fmaxf(m_run[n], -1e30f);
-                a.many_ml[at * 2 + 1] = l_run[n];
+                a.many_ml[at * 2] = fmaxf(m_ref[n], -1e30f);
+                a.many_ml[at * 2 + 1] = l;
             }
 #pragma unroll
             for (int b = 0; b < NB; ++b) *reinterpret_cast<floatx4*>(a.many_o + at * D + b * 16 + lg * 4) = o[n][b];
@@ -983,10 +1072,16 @@ static RowShape row_shape(int n_q, int n_kv, int d, int batch, int rows, int max
     if (max_new > s.few_max) {
         s.tt = kManyCols / s.G;
         s.slots = rows / s.tt + batch;
-        // workgroups that have something to do, at most: with fewer than two for each compute unit their pages are dealt out
+        // workgroups that have something to do, at most: their pages are dealt out where the compute unit that gets most of them has many more than
+        // the mean (a part more costs about 2 %)
         const int64_t tiles = (int64_t)rows / s.tt + std::min((int64_t)batch, (int64_t)rows / (s.few_max + 1));
-        s.splits_max = (int)std::min<int64_t>(16, 2 * kNumCU / std::max<int64_t>(1, tiles * n_kv));
-        s.splits_max = std::max(1, s.splits_max);
+        s.splits_max = 1;
+        double best = 1e30;
+        const double alone = (double)std::max<int64_t>(1, tiles * n_kv) / kNumCU;
+        for (int k = 1; k <= (alone < 4 ? 16 : 1); ++k) {
+            const double per = alone * k, cost = std::ceil(per) / per * (1.0 + 0.02 * (k - 1));
+            if (cost < best - 1e-9) best = cost, s.splits_max = k;
+        }
         if (s.splits_max > 1) {
             const int64_t n = (int64_t)s.slots * n_kv * s.splits_max * kManyCols;
             s.many_ml = up16(n * 8);
