@@ -206,7 +206,7 @@ typedef struct {
  * waiting).  A call repeated on its own result grants the same rows and takes no page.
  *   block_table  dev int32 [batch, max_blocks_per_seq], in and out;  seq_lens, new_lens  dev int32 [batch]
  *   workspace    dev, chiron_kv_pages_workspace_bytes(batch) bytes, 16-byte aligned, caller-owned, in use until the stream has passed
- * max_blocks_per_seq <= 2^26. */
+ * max_blocks_per_seq <= 2^26, max_rows <= 2^30. */
 int64_t chiron_kv_pages_workspace_bytes(int32_t batch);
 int32_t chiron_kv_grant_pages(const chiron_page_list *list /* host */, int32_t *block_table, int32_t max_blocks_per_seq,
                               const int32_t *seq_lens, const int32_t *new_lens, int32_t batch, int32_t max_rows,

@@ -1058,7 +1058,7 @@ static RowShape row_shape(int n_q, int n_kv, int d, int batch, int rows, int max
     max_new = std::min(max_new, rows);
     s.G = n_q / n_kv;
     s.tg = std::max(1, 16 / s.G);
-    s.few_max = 2 * s.tg;
+    s.few_max = 4 * s.tg;
     const int cols = s.G * std::min(s.tg, max_new);
     s.cw = cols <= 4 ? 4 : cols <= 8 ? 8 : 16;
     s.few_wgs = std::max(1, 2 * kNumCU / n_kv);  // of a KV head

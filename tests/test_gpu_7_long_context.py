@@ -60,7 +60,8 @@ def check_grant(m, bt_gpu, bt, lst, pages, old, new, rows):
 
 @pytest.mark.parametrize("batch,width,free,rows_share", (
     (1, 1, 1.0, 1.0), (1, 40, 1.0, 1.0), (7, 5, 1.0, 1.0), (64, 33, 0.02, 1.0), (65, 17, 1.0, 0.4), (200, 9, 0.05, 0.7), (1024, 3, 0.3, 1.0),
-    (1025, 3, 1.0, 0.9), (1501, 130, 0.2, 1.0), (2500, 4, 0.01, 0.5), (3, 2000, 1.0, 1.0), (130, 600, 0.5, 1.0)))
+    (1025, 3, 1.0, 0.9), (1501, 130, 0.2, 1.0), (2500, 4, 0.01, 0.5), (3, 2000, 1.0, 1.0), (130, 600, 0.5, 1.0),
+    (64, 512, 0.3, 1.0), (63, 521, 0.3, 0.8), (1024, 33, 0.3, 1.0), (5000, 2, 0.5, 0.9), (1000, 32, 1.0, 1.0)))
 def test_pages(batch, width, free, rows_share):
     bt, pages, n, keep, new = table_case(batch, width, batch * 7 + width, free=free)
     rows = int(rows_share * new.sum()) + 3

@@ -50,6 +50,7 @@ def maps(row_starts=FAKE):
     ({}, FAKE, 4, FAKE, None, 1, 1, {}, FAKE, INVALID),
     ({}, FAKE, 4, FAKE, FAKE, -1, 1, {}, FAKE, INVALID),
     ({}, FAKE, 4, FAKE, FAKE, 1, -1, {}, FAKE, INVALID),
+    ({}, FAKE, 4, FAKE, FAKE, 1, (1 << 30) + 1, {}, FAKE, SHAPE),
     ({}, FAKE, 4, FAKE, FAKE, 1, 1, dict(row_starts=None), FAKE, INVALID),
     ({}, FAKE, 4, FAKE, FAKE, 1, 1, {}, None, INVALID),
     ({}, FAKE, 4, FAKE, FAKE, 1, 1, {}, FAKE + 8, INVALID),
