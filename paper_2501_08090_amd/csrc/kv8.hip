@@ -22,6 +22,16 @@ __device__ __forceinline__ uint32_t coarser(uint32_t w, float down) {
     return encode8<FMT>(f[0], f[1], f[2], f[3]);
 }
 
+// the largest of a wave's values, none below 0
+__device__ __forceinline__ float wave_max(float v) {
+    v = fmaxf(v, row_move<kRor8>(v));
+    v = fmaxf(v, row_move<kRor4>(v));
+    v = fmaxf(v, row_move<kRor2>(v));
+    v = fmaxf(v, row_move<kRor1>(v));
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+
 // workgroups 0 .. page_wgs-1: four (page slot, KV head) each; the others: queries
 template <int D, int FMT, bool F32, bool VEC>
 __global__ __launch_bounds__(256) void append8_rope_kernel(Append8Args a) {
@@ -43,7 +53,13 @@ __global__ __launch_bounds__(256) void append8_rope_kernel(Append8Args a) {
     int8_t* exps = exps8(a.pool, a.layer, np.block, kvh);
 
     // Everything that the page needs is on its way before the first of it is used: rows outside the request are replaced by its first or
-    // last, so that no load hangs on a branch.
+    // last, so that no load hangs on a branch.  First what the page has: its powers of two, and the words of V that keep old bytes.
+    const uint32_t had_exps = *reinterpret_cast<const uint16_t*>(exps);
+    uint4 had[H];
+    if (t0 > 0 || t1 < kBlockSize) {
+#pragma unroll
+        for (int b = 0; b < H; ++b) had[b] = *reinterpret_cast<const uint4*>(vtile + v8_off(4 * (lane >> 4), 64 * b + (lane & 15)));
+    }
     // V: lane = (dim l of 16, four tokens 4u ..); word b holds the dims 64b + 16j + l, j = 0 .. 3, of these tokens
     const int l = lane & 15, u = lane >> 4;
     float vx[H][4][4];
@@ -80,7 +96,7 @@ __global__ __launch_bounds__(256) void append8_rope_kernel(Append8Args a) {
                 ky[p][i] = is_new ? bounded8(w.b) : 0.f;
             }
     }
-    const int ek_old = t0 > 0 ? exps[0] : kMinExp8, ev_old = t0 > 0 ? exps[1] : kMinExp8;
+    const int ek_old = t0 > 0 ? (int8_t)(had_exps & 0xff) : kMinExp8, ev_old = t0 > 0 ? (int8_t)(had_exps >> 8) : kMinExp8;
 
     float top = 0.f, vtop = 0.f;
 #pragma unroll
@@ -97,11 +113,8 @@ __global__ __launch_bounds__(256) void append8_rope_kernel(Append8Args a) {
                 vx[b][j][i] = is_new ? bounded8(vx[b][j][i]) : 0.f;
                 vtop = fmaxf(vtop, fabsf(vx[b][j][i]));
             }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        top = fmaxf(top, __shfl_xor(top, o));
-        vtop = fmaxf(vtop, __shfl_xor(vtop, o));
-    }
+    top = wave_max(top);
+    vtop = wave_max(vtop);
     const int ek = max(ek_old, power8<FMT>(top)), ev = max(ev_old, power8<FMT>(vtop));
     const float kup = two_to(-ek), vup = two_to(-ev);
     // (a step that grew by more than 2^126 leaves nothing of an old code)
@@ -135,8 +148,7 @@ __global__ __launch_bounds__(256) void append8_rope_kernel(Append8Args a) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = encode8<FMT>(vx[b][j][0] * vup, vx[b][j][1] * vup, vx[b][j][2] * vup, vx[b][j][3] * vup);
             if (fresh != ~0u) {
-                const uint4 had = *dst;
-                const uint32_t h[4] = {had.x, had.y, had.z, had.w};
+                const uint32_t h[4] = {had[b].x, had[b].y, had[b].z, had[b].w};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const uint32_t kept = ev > ev_old ? (coarser<FMT>(h[j], vdown) & upto0) | (h[j] & ~upto0) : h[j];
@@ -178,8 +190,9 @@ __global__ __launch_bounds__(256) void gather8_kernel(Pool8Desc pool, int layer,
         k = *reinterpret_cast<const uint4*>(tile + k8_off(t, p * 16));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint8_t* src = tile + 16 * pool.d + v8_off(t, 64 * b + l0 + i);
-            v[i] = src[0] | src[4] << 8 | src[8] << 16 | (uint32_t)src[12] << 24;
+            const uint4 w = *reinterpret_cast<const uint4*>(tile + 16 * pool.d + v8_off(t & ~3, 64 * b + l0 + i));
+            const int down = (t & 3) * 8;
+            v[i] = (w.x >> down & 0xff) | (w.y >> down & 0xff) << 8 | (w.z >> down & 0xff) << 16 | (w.w >> down) << 24;
         }
     }
     uint16_t *kd = k_out + th * pool.d + p * 16, *vd = v_out + th * pool.d + 64 * b + l0;
