@@ -214,8 +214,8 @@ __device__ __forceinline__ void store_row(const RowAttnArgs& a, int64_t row, int
 // w + v is wave w's of pass v, a number of its own for each pair that exists.
 //
 // CW: columns of a term group.  Three terms of up to 4 columns share one instruction, of up to 8 two.  int8 keys meet the query in
-// three 8-bit digits instead (whole multiples of 2^(f-16), with 2^f the power of two of the head's largest element), on the 8-bit matrix
-// cores: no key is widened, and sums are exact.
+// four 8-bit digits instead (whole multiples of 2^(f-24), with 2^f the power of two of the head's largest element: what is no smaller than
+// 2^-7 of that is exact), on the 8-bit matrix cores: no key is widened, and sums are exact.
 constexpr int kFewMinPages = 8;  // of a share
 // Waves of a SIMD: two, but one where three terms of many columns and bf16 pages of 128 dims do not fit 256 registers.
 __host__ __device__ constexpr int few_waves(int d, int fmt, bool f32, int cw, bool multi) {
@@ -223,10 +223,12 @@ __host__ __device__ constexpr int few_waves(int d, int fmt, bool f32, int cw, bo
 }
 template <int D, int FMT, bool F32, int CW, bool MULTI>
 __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_few_kernel(RowAttnArgs a) {
-    constexpr bool DIGITS = FMT == kFmtInt8, TERMS = DIGITS || F32;
-    constexpr int KSTEPS = D / (DIGITS ? 64 : 32), P = pieces<FMT>(D), NPG = D == 128 && (FMT == kFmtBf16 || (F32 && CW == 16)) ? 2 : 4;
-    constexpr int TPI = TERMS && CW <= 8 ? (CW <= 4 ? 3 : 2) : 1;        // terms of an instruction
-    constexpr int NQ = TERMS ? (3 + TPI - 1) / TPI : 1, NP = F32 ? NQ : 1;  // instructions for those of a query, of a weight
+    constexpr bool DIGITS = FMT == kFmtInt8;
+    constexpr int KSTEPS = D / (DIGITS ? 64 : 32), P = pieces<FMT>(D), NPG = D == 128 && (FMT == kFmtBf16 || (CW == 16 && (F32 || DIGITS))) ? 2 : 4;
+    // terms of an instruction, and instructions, of a weight and of a query
+    constexpr int TPP = F32 && CW <= 8 ? (CW <= 4 ? 3 : 2) : 1, NP = F32 ? (3 + TPP - 1) / TPP : 1;
+    constexpr int TPQ = DIGITS ? 16 / CW : TPP, NQ = DIGITS ? 4 / TPQ : NP;
+    constexpr float kDigits = TPQ == 1 ? 0x1p-8f : 0x1p-16f;  // from one instruction's digits to the next one's
     constexpr int TILE = FMT == kFmtBf16 ? 32 * D : 16 * D;               // bytes of a K or V tile
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -330,7 +332,7 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                     }
                 };
                 uint4 qt[NQ][KSTEPS];
-                float qw[NQ];  // what a digit of the lane's term stands for
+                float qw = 0.f;  // what a digit of the lane's first term stands for
                 floatx4 oo[1][D / 16], (&o)[D / 16] = oo[0];
 #pragma unroll
                 for (int t = 0; t < D / 16; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -343,6 +345,7 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                 const int64_t qrow = (row0 + t0 + min(tq, tv - 1)) * a.q_stride + (int64_t)(c * a.G + h) * D;
                 if (DIGITS) {
                     float y[KSTEPS][16], top = 0.f;
+                    bool odd = false;
 #pragma unroll
                     for (int s = 0; s < KSTEPS; ++s) {
                         const int64_t at = qrow + s * 64 + lg * 16;
@@ -356,45 +359,46 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                                 y[s][e] = bf16_lo(z.x), y[s][e + 1] = bf16_hi(z.x), y[s][e + 2] = bf16_lo(z.y), y[s][e + 3] = bf16_hi(z.y);
                             }
 #pragma unroll
-                            for (int z = 0; z < 4; ++z) top = fmaxf(top, fabsf(y[s][e + z]));
+                            for (int z = 0; z < 4; ++z) {
+                                top = fmaxf(top, fabsf(y[s][e + z]));
+                                odd |= !(fabsf(y[s][e + z]) < INFINITY);
+                            }
                         }
                     }
                     top = fmaxf(top, __shfl_xor(top, 16));
                     top = fmaxf(top, __shfl_xor(top, 32));
                     // |y| <= 127 * 2^f; a head of zeros, NaN and infinities go by any power (the last two are put back below)
                     const int f = top > 0.f && top < INFINITY ? min(max(power_of(top), -100), 120) : 0;
-                    const float up = two_to(-f) * 65536.f;
-                    float bad = 0.f;
+                    const float up = two_to(-f) * 0x1p24f;
 #pragma unroll
-                    for (int s = 0; s < KSTEPS; ++s) {
-                        uint32_t d[NQ][4];
+                    for (int s = 0; s < KSTEPS; ++s)
 #pragma unroll
-                        for (int i = 0; i < NQ; ++i)
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t w[4] = {0, 0, 0, 0};  // four elements' digits, high ones first
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) d[i][e] = 0;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            bad += y[s][e] * 0.f;  // 0, or NaN
-                            const int x = (int)rintf(y[s][e] * up);
-                            // low digit first, each -128 .. 127: |x| <= 127 * 65536 leaves -127 .. 127 for the high one
-                            const int d2 = (int8_t)x, x1 = (x - d2) >> 8, d1 = (int8_t)x1, d0 = (x1 - d1) >> 8;
+                            for (int z = 0; z < 4; ++z) {
+                                const int x = on ? (int)rintf(y[s][4 * e + z] * up) : 0;
+                                // low digit first, each -128 .. 127: |x| <= 127 * 2^24 leaves -127 .. 127 for the high one
+                                const int d3 = (int8_t)x, x2 = (x - d3) >> 8, d2 = (int8_t)x2, x1 = (x2 - d2) >> 8, d1 = (int8_t)x1, d0 = (x1 - d1) >> 8;
+                                w[0] |= (uint32_t)(d0 & 0xff) << (8 * z);
+                                w[1] |= (uint32_t)(d1 & 0xff) << (8 * z);
+                                w[2] |= (uint32_t)(d2 & 0xff) << (8 * z);
+                                w[3] |= (uint32_t)(d3 & 0xff) << (8 * z);
+                            }
 #pragma unroll
                             for (int i = 0; i < NQ; ++i) {
-                                const int t = i * TPI + grp;
-                                const int digit = !on || t > 2 || grp >= TPI ? 0 : t == 0 ? d0 : t == 1 ? d1 : d2;
-                                d[i][e / 4] |= (uint32_t)(digit & 0xff) << (e % 4 * 8);
+                                const int t = i * TPQ + grp;
+                                const uint32_t v = t == 0 ? w[0] : t == 1 ? w[1] : t == 2 ? w[2] : w[3];
+                                if (e == 0) qt[i][s].x = v;
+                                else if (e == 1) qt[i][s].y = v;
+                                else if (e == 2) qt[i][s].z = v;
+                                else qt[i][s].w = v;
                             }
                         }
-#pragma unroll
-                        for (int i = 0; i < NQ; ++i) qt[i][s] = make_uint4(d[i][0], d[i][1], d[i][2], d[i][3]);
-                    }
+                    float bad = odd ? NAN : 0.f;
                     bad += __shfl_xor(bad, 16);
                     bad += __shfl_xor(bad, 32);
-#pragma unroll
-                    for (int i = 0; i < NQ; ++i) {
-                        const int t = i * TPI + grp;
-                        qw[i] = two_to(f) * a.scale_log2e * (t == 0 ? 1.f : t == 1 ? 0x1p-8f : 0x1p-16f) + (on ? bad : 0.f);
-                    }
+                    qw = two_to(f) * a.scale_log2e * two_to(-8 * grp) + (on ? bad : 0.f);
                 } else {
 #pragma unroll
                     for (int s = 0; s < KSTEPS; ++s) {
@@ -407,8 +411,8 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                                 float z[8];
 #pragma unroll
                                 for (int e = 0; e < 8; ++e) {
-                                    const int t = i * TPI + grp;
-                                    z[e] = !on || grp >= TPI || t > 2 ? 0.f : rest3(y[e] * a.scale_log2e, t);
+                                    const int t = i * TPP + grp;
+                                    z[e] = !on || grp >= TPP || t > 2 ? 0.f : rest3(y[e] * a.scale_log2e, t);
                                 }
                                 qt[i][s] = make_uint4(uppers(z[0], z[1]), uppers(z[2], z[3]), uppers(z[4], z[5]), uppers(z[6], z[7]));
                             }
@@ -441,9 +445,10 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                             }
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
-                                x[u][r] = (float)y[0][r] * (qw[0] * ks[u]);
+                                float v = (float)y[NQ - 1][r];
 #pragma unroll
-                                for (int i = 1; i < NQ; ++i) x[u][r] += (float)y[i][r] * (qw[i] * ks[u]);
+                                for (int i = NQ - 2; i >= 0; --i) v = fmaf(v, kDigits, (float)y[i][r]);
+                                x[u][r] = v * (qw * ks[u]);
                             }
                         } else {
                             x[u] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -455,7 +460,7 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                             }
                             if (!F32) x[u] *= a.scale_log2e;
                         }
-                        if (TPI > 1) {
+                        if (TPQ > 1) {
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {  // the sum over the term groups, in every column
                                 x[u][r] += row_move<kRor8>(x[u][r]);
@@ -537,8 +542,8 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
 #pragma unroll
                         for (int i = 0; i < NP; ++i) {
                             if (F32) {
-                                const int t = i * TPI + grp;
-                                const uint32_t keep = TPI > 1 && (t > 2 || grp >= TPI) ? 0 : ~0u;
+                                const int t = i * TPP + grp;
+                                const uint32_t keep = TPP > 1 && (t > 2 || grp >= TPP) ? 0 : ~0u;
                                 float y[2][4];
 #pragma unroll
                                 for (int z = 0; z < 2; ++z)
@@ -578,7 +583,7 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                 if (FMT == kFmtBf16 && MULTI && marked) mark_not_finite<D, 1, NPG>(a, span, seen, btrow, c, j0, j1, lo1, last1, oo);
                 l_run += __shfl_xor(l_run, 16);
                 l_run += __shfl_xor(l_run, 32);
-                if (TPI > 1 && F32) {
+                if (TPP > 1 && F32) {
 #pragma unroll
                     for (int t = 0; t < D / 16; ++t)
 #pragma unroll
