@@ -29,7 +29,7 @@ struct RowAttnArgs {
     int64_t window;
     int num_blocks, n_kv, G, max_blocks, batch, rows, max_new, n_sinks;
     float scale_log2e;
-    int few_max;      // requests of at most so many rows are row_few_kernel's, the others row_many_kernel's
+    int few_max;      // requests of at most so many rows are row_few_kernel's (0: none), the others row_many_kernel's
     int tg, pcols;    // tokens that share a pass of row_few_kernel, and the columns of a partial result
     int passes_max;   // no more passes than this
     int tt, splits;   // tokens of a tile of row_many_kernel, parts of its pages
@@ -104,6 +104,12 @@ __device__ __forceinline__ bf16x8 key_operand(const uint4 (&k)[N], int s, float 
         w = make_uint4(a.x, a.y, b.x, b.y);
     }
     return *reinterpret_cast<bf16x8*>(&w);
+}
+// the largest of three, of four (of NaN and a number the number), without the instructions that the compiler puts before a maximum
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
 }
 __device__ __forceinline__ uint32_t word(const uint4& w, int j) { return j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w; }
 // An fp32 number is the sum of three bf16 terms, exactly: the first 8 of its 24 significant bits, the next 8 and the rest, by truncation.
@@ -183,6 +189,12 @@ __device__ __forceinline__ void mark_not_finite(const RowAttnArgs& a, const Span
             __builtin_amdgcn_sched_barrier(0);
         }
     }
+}
+
+// 16 bytes per lane from base + offset straight into LDS, as in device_util.h, with a scalar base
+__device__ __forceinline__ void global_to_lds_16(const uint8_t* base, uint32_t offset, uint32_t lds_addr) {
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds_addr);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
 }
 
 // a request's rows, as the kernels take them: 0 rows where the row starts do not ascend
@@ -774,6 +786,7 @@ __global__ __launch_bounds__(256, F32 ? 2 : 3) void row_many_kernel(RowAttnArgs 
     u32x4 rk[FMT == kFmtBf16 ? 1 : KEYS], rv[2];  // what the wave brings of the stage that comes next
     int exps[2] = {0, 0}, cur_exps[2], pages[2], next_pages[2];
     const int v_unit = wave - (4 - VALUES);  // below 0: no V
+    const uint32_t lane16 = lane * 16u;      // beside a scalar base
     auto load = [&](int st, int buf) {
         if (st * 2 - lbase >= 64) {
             lbase = st * 2;
@@ -791,18 +804,18 @@ __global__ __launch_bounds__(256, F32 ? 2 : 3) void row_many_kernel(RowAttnArgs 
         for (int i = 0; i < KEYS; ++i) {
             const int k = wave * KEYS + i, page = k / P, piece = k % P;
             if (k < 2 * P) {  // uniform
-                const uint8_t* src = (page ? tile[1] : tile[0]) + piece * 1024 + lane * 16;
-                if (FMT == kFmtBf16) global_to_lds_16(src, lds_address(&s_k[buf][page][piece][0]));
-                else rk[i] = *reinterpret_cast<const u32x4*>(src);
+                const uint8_t* src = (page ? tile[1] : tile[0]) + piece * 1024;
+                if (FMT == kFmtBf16) global_to_lds_16(src, lane16, lds_address(&s_k[buf][page][piece][0]));
+                else rk[i] = *reinterpret_cast<const u32x4*>(src + lane16);
             }
         }
         if (v_unit >= 0) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const uint8_t* src = tile[u] + TILE + lane * 16;
-                if (FMT == kFmtBf16) rv[u] = *reinterpret_cast<const u32x4*>(src + v_unit * 1024);
+                const uint8_t* src = tile[u] + TILE;
+                if (FMT == kFmtBf16) rv[u] = *reinterpret_cast<const u32x4*>(src + v_unit * 1024 + lane16);
                 else {
-                    const uint2 half = *reinterpret_cast<const uint2*>(src + v_unit / 2 * 1024 + v_unit % 2 * 8);
+                    const uint2 half = *reinterpret_cast<const uint2*>(src + (v_unit / 2 * 1024 + v_unit % 2 * 8) + lane16);
                     rv[u][0] = half.x;
                     rv[u][1] = half.y;
                 }
@@ -897,11 +910,11 @@ __global__ __launch_bounds__(256, F32 ? 2 : 3) void row_many_kernel(RowAttnArgs 
         bool above = false;
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
-            top[n] = -INFINITY;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const float t = fmaxf(fmaxf(x[n][u][0], x[n][u][1]), fmaxf(x[n][u][2], x[n][u][3]));
-                top[n] = fmaxf(top[n], SCALED ? t * ks[u] : t);
+            const floatx4 y = x[n][0], z = x[n][1];
+            if (INT8) top[n] = fmaxf(max3(max3(y[0], y[1], y[2]), y[3], y[3]) * ks[0], max3(max3(z[0], z[1], z[2]), z[3], z[3]) * ks[1]);
+            else {
+                top[n] = max3(max3(max3(y[0], y[1], y[2]), y[3], z[0]), max3(z[1], z[2], z[3]), -INFINITY);
+                if (SCALED) top[n] *= a.scale_log2e;
             }
             above |= top[n] > m_ref[n] + kSlack;
         }
@@ -1111,6 +1124,7 @@ static void launch_rows(const RowAttnArgs& a, const RowShape& s, hipStream_t st)
         launch(row_many_kernel<D, FMT, F32>, dim3((unsigned)((int64_t)s.slots * a.splits * a.n_kv)), dim3(256), st, a);
         if (a.splits > 1) launch(row_many_merge_kernel<D, F32>, dim3((unsigned)(s.slots * a.n_kv)), dim3(256), st, a);
     }
+    if (a.few_max == 0) return;
     if (a.max_new > 1) launch_few<D, FMT, F32, true>(a, s, st);
     else launch_few<D, FMT, F32, false>(a, s, st);
 }
@@ -1152,6 +1166,8 @@ static int32_t row_attention(const chiron_attn_rows* in, int n_kv, int d, int nu
     a.max_new = in->max_new; a.n_sinks = in->n_sinks;
     a.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)d));
     a.few_max = s.few_max; a.tg = s.tg; a.pcols = s.cw; a.passes_max = s.passes_max; a.tt = s.tt;
+    // one request that may bring many rows goes by tiles even if it brings few: the two launches for few rows cost 9 us
+    if (s.slots && in->batch == 1) a.few_max = 0;
     a.splits = 1;
     if (s.splits_max > 1) {  // a part has 512 tokens at least, if the window or the table lets a tile see as many
         int64_t pages = in->max_blocks_per_seq;
