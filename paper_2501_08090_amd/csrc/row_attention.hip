@@ -668,7 +668,7 @@ __global__ __launch_bounds__(256) void row_few_merge_kernel(RowAttnArgs a) {
     }
     const int tq = col / a.G, h = col - tq * a.G;
     if (!(den > 0.f) && den == den) den = 1.f;
-    store_row<D, F32>(a, (int64_t)rec.x + tq, c * a.G + h, ln * 4, floatx4{num[0] / den, num[1] / den, num[2] / den, num[3] / den});
+    store_row<D, F32>(a, (int64_t)rec.x + tq, c * a.G + h, ln * 4, num * (1.f / den));
 }
 
 // ---- requests of many rows ----------------------------------------------------------------------------------------
@@ -1035,31 +1035,40 @@ __global__ __launch_bounds__(256, F32 ? 2 : 3) void row_many_kernel(RowAttnArgs 
     }
 }
 
-// joins the parts of a tile: a workgroup per (slot, KV head)
+// joins the parts of a tile: a workgroup per (slot, KV head, 8 or 16 columns), a quarter of a wave or half of one to a column
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void row_many_merge_kernel(RowAttnArgs a) {
-    constexpr int LANES = D / 4, S = 256 / LANES;
-    const int c = blockIdx.x % a.n_kv, slot = blockIdx.x / a.n_kv;
+    constexpr int LANES = D / 4, S = 256 / LANES, GROUPS = kManyCols / S;
+    const int g = blockIdx.x % GROUPS, rest = blockIdx.x / GROUPS, c = rest % a.n_kv, slot = rest / a.n_kv;
     ManyTile m;
     if (!many_tile(a, slot, m)) return;
-    const int sl = threadIdx.x / LANES, ln = threadIdx.x % LANES;
-    for (int ci = sl; ci < a.G * m.tv; ci += S) {
-        const int64_t at0 = ((int64_t)slot * a.n_kv + c) * a.splits * kManyCols + ci;
-        float M = -1e30f, den = 0.f;
-        floatx4 num = {0.f, 0.f, 0.f, 0.f};
-        for (int j = 0; j < a.splits; ++j) {
-            const int64_t at = at0 + (int64_t)j * kManyCols;
-            const float2 ml = *reinterpret_cast<const float2*>(a.many_ml + at * 2);
-            const floatx4 o = *reinterpret_cast<const floatx4*>(a.many_o + at * D + ln * 4);
-            const float Mn = fmaxf(M, ml.x), f0 = __builtin_amdgcn_exp2f(M - Mn), f1 = __builtin_amdgcn_exp2f(ml.x - Mn);
-            num = num * f0 + o * f1;
-            den = den * f0 + ml.y * f1;
-            M = Mn;
+    const int ci = g * S + threadIdx.x / LANES, ln = threadIdx.x % LANES;
+    if (ci >= a.G * m.tv) return;
+    const int64_t at0 = ((int64_t)slot * a.n_kv + c) * a.splits * kManyCols + ci;
+    float M = -1e30f, den = 0.f;
+    floatx4 num = {0.f, 0.f, 0.f, 0.f};
+    constexpr int kAtOnce = 4;  // parts whose loads are on their way together
+    for (int j0 = 0; j0 < a.splits; j0 += kAtOnce) {
+        float2 ml[kAtOnce];
+        floatx4 o[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int64_t at = at0 + (int64_t)min(j0 + u, a.splits - 1) * kManyCols;
+            ml[u] = *reinterpret_cast<const float2*>(a.many_ml + at * 2);
+            o[u] = *reinterpret_cast<const floatx4*>(a.many_o + at * D + ln * 4);
         }
-        if (!(den > 0.f) && den == den) den = 1.f;
-        const int tq = ci / a.G, h = ci - tq * a.G;
-        store_row<D, F32>(a, (int64_t)m.r0 + m.t0 + tq, c * a.G + h, ln * 4, floatx4{num[0] / den, num[1] / den, num[2] / den, num[3] / den});
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            if (j0 + u < a.splits) {
+                const float Mn = fmaxf(M, ml[u].x), f0 = __builtin_amdgcn_exp2f(M - Mn), f1 = __builtin_amdgcn_exp2f(ml[u].x - Mn);
+                num = num * f0 + o[u] * f1;
+                den = den * f0 + ml[u].y * f1;
+                M = Mn;
+            }
     }
+    if (!(den > 0.f) && den == den) den = 1.f;
+    const int tq = ci / a.G, h = ci - tq * a.G;
+    store_row<D, F32>(a, (int64_t)m.r0 + m.t0 + tq, c * a.G + h, ln * 4, num * (1.f / den));
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------
@@ -1071,12 +1080,12 @@ struct RowShape {
     int64_t bytes() const { return rec_bytes + few_ml + few_o + many_ml + many_o; }
 };
 static int64_t up16(int64_t x) { return (x + 15) / 16 * 16; }
-static RowShape row_shape(int n_q, int n_kv, int d, int batch, int rows, int max_new) {
+static RowShape row_shape(int n_q, int n_kv, int d, int batch, int rows, int max_new, int passes) {
     RowShape s;
     max_new = std::min(max_new, rows);
     s.G = n_q / n_kv;
     s.tg = std::max(1, 16 / s.G);
-    s.few_max = 4 * s.tg;
+    s.few_max = passes * s.tg;
     const int cols = s.G * std::min(s.tg, max_new);
     s.cw = cols <= 4 ? 4 : cols <= 8 ? 8 : 16;
     s.few_wgs = std::max(1, 2 * kNumCU / n_kv);  // of a KV head
@@ -1109,6 +1118,18 @@ static RowShape row_shape(int n_q, int n_kv, int d, int batch, int rows, int max
     return s;
 }
 
+// Up to how many passes a request is row_few_kernel's.  us by passes / by tiles: 32 requests of 4000 tokens, 4 heads to a KV head of 128: fp32 over int8 at
+// 2 passes 104 / 165, 4 141 / 172, 8 239 / 312; fp32 over bf16 188 / 192, 222 / 194, 342 / 346; bf16 over int8 102 / 107, 135 / 115, 205 / 199; bf16 over bf16
+// at 2 183 / 141.  8 heads to a KV head of 64: bf16 over bf16 33 / 45, 55 / 30; bf16 over e4m3 26 / 45, 37 / 32.  One request of 8000 tokens, whose tiles leave
+// most compute units idle: 128 dims, 8 passes, fp32 over int8 38 / 48, bf16 over int8 36 / 36; over bf16 fp32 at 4 43 / 47, at 8 58 / 50, bf16 at 2 23 / 32, at
+// 4 35 / 33; 64 dims at 8 passes 17 to 20 / 25 to 33.
+constexpr int kMostPasses = 8;
+static int few_passes(const chiron_attn_rows* in, int n_kv, int d, int format) {
+    const bool wide = format == kFmtBf16 && d == 128, f32 = in->dtype == CHIRON_F32;
+    if ((int64_t)in->batch * n_kv <= kNumCU / 8) return !wide ? kMostPasses : f32 ? 4 : 2;
+    return f32 && format != kFmtBf16 ? kMostPasses : wide && !f32 ? 1 : 2;
+}
+
 template <int D, int FMT, bool F32, bool MULTI>
 static void launch_few(const RowAttnArgs& a, const RowShape& s, hipStream_t st) {
     constexpr bool TERMS = F32 || FMT == kFmtInt8;
@@ -1122,7 +1143,7 @@ template <int D, int FMT, bool F32>
 static void launch_rows(const RowAttnArgs& a, const RowShape& s, hipStream_t st) {
     if (s.slots) {
         launch(row_many_kernel<D, FMT, F32>, dim3((unsigned)((int64_t)s.slots * a.splits * a.n_kv)), dim3(256), st, a);
-        if (a.splits > 1) launch(row_many_merge_kernel<D, F32>, dim3((unsigned)(s.slots * a.n_kv)), dim3(256), st, a);
+        if (a.splits > 1) launch(row_many_merge_kernel<D, F32>, dim3((unsigned)((int64_t)s.slots * a.n_kv * (kManyCols * D / 1024))), dim3(256), st, a);
     }
     if (a.few_max == 0) return;
     if (a.max_new > 1) launch_few<D, FMT, F32, true>(a, s, st);
@@ -1154,7 +1175,7 @@ static int32_t row_attention(const chiron_attn_rows* in, int n_kv, int d, int nu
         return fail(CHIRON_ERR_INVALID_ARG, "row attention: q_stride %lld is smaller than a row or no multiple of 16 bytes", (long long)in->q_stride);
     if (((uintptr_t)in->q | (uintptr_t)in->out | (uintptr_t)workspace) & 15) return fail(CHIRON_ERR_INVALID_ARG, "row attention: q, out and the workspace must be 16-byte aligned");
     if (!workspace) return fail(CHIRON_ERR_INVALID_ARG, "row attention: the workspace is null");
-    const RowShape s = row_shape(in->n_q_heads, n_kv, d, in->batch, in->rows, in->max_new);
+    const RowShape s = row_shape(in->n_q_heads, n_kv, d, in->batch, in->rows, in->max_new, few_passes(in, n_kv, d, format));
     if ((int64_t)s.passes_max * in->max_blocks_per_seq >= (int64_t)1 << 31)
         return fail(CHIRON_ERR_SHAPE, "row attention: %d requests of up to %d pages are too many for one call", in->batch, in->max_blocks_per_seq);
     RowAttnArgs a = {};
@@ -1169,12 +1190,12 @@ static int32_t row_attention(const chiron_attn_rows* in, int n_kv, int d, int nu
     // one request that may bring many rows goes by tiles even if it brings few: the two launches for few rows cost 9 us
     if (s.slots && in->batch == 1) a.few_max = 0;
     a.splits = 1;
-    if (s.splits_max > 1) {  // a part has 512 tokens at least, if the window or the table lets a tile see as many
+    if (s.splits_max > 1) {  // a part has 256 tokens at least, if the window or the table lets a tile see as many
         int64_t pages = in->max_blocks_per_seq;
         if (in->window) pages = std::min(pages, ((int64_t)in->window + s.tt) / kBlockSize + in->n_sinks / kBlockSize + 3);
-        a.splits = (int)std::min<int64_t>(s.splits_max, std::max<int64_t>(1, pages / 32));
+        a.splits = (int)std::min<int64_t>(s.splits_max, std::max<int64_t>(1, pages / 16));
     }
-    if ((int64_t)s.slots * a.splits * n_kv > 0x7fffffff || (int64_t)s.passes_max * n_kv * s.cw > 0x7fffffff)
+    if ((int64_t)s.slots * std::max(a.splits, 16) * n_kv > 0x7fffffff || (int64_t)s.passes_max * n_kv * s.cw > 0x7fffffff)
         return fail(CHIRON_ERR_SHAPE, "row attention: %d rows are too many for one call", in->rows);
     uint8_t* ws = (uint8_t*)workspace;
     a.head = (int32_t*)ws;
@@ -1199,7 +1220,9 @@ extern "C" {
 int64_t chiron_row_attention_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t batch, int32_t rows, int32_t max_new) {
     if (n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads != 0 || n_q_heads / n_kv_heads > 16 || (head_dim != 64 && head_dim != 128)) return 0;
     if (batch < 1 || rows < 1 || max_new < 1) return 0;
-    return row_shape(n_q_heads, n_kv_heads, head_dim, batch, rows, max_new).bytes();
+    int64_t most = 0;  // whatever the pool and the type are
+    for (int passes = 1; passes <= kMostPasses; passes *= 2) most = std::max(most, row_shape(n_q_heads, n_kv_heads, head_dim, batch, rows, max_new, passes).bytes());
+    return most;
 }
 
 int32_t chiron_op_row_attention(const chiron_kvpool* p, int32_t layer, const chiron_attn_rows* in, void* workspace, void* stream) {

@@ -348,6 +348,27 @@ def test_long(fmt, dtype):
     check_rows(4, 1, 64, [5000, 1], [40, 20], fmt, dtype, window=2500, sinks=3, seed=4)
 
 
+@pytest.mark.parametrize("fmt", ("bf16", "int8", "e4m3"))
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+def test_tokens_on_both_sides_of_a_prompt(fmt, dtype):
+    """every count of passes up to the first tiles, in calls of few and of many requests (which draw that line elsewhere)"""
+    for n_q, n_kv, d in ((4, 1, 128), (16, 2, 64)):
+        tg = 16 // (n_q // n_kv)
+        new = [tg * p + e for p in (1, 2, 4, 8) for e in (0, 1)] + [1, 8 * tg - 1]
+        old = [40 * i + 7 for i in range(len(new))]
+        check_rows(n_q, n_kv, d, old, new, fmt, dtype, window=90, sinks=18, seed=21)
+        check_rows(n_q, n_kv, d, old * 4, new * 4, fmt, dtype, seed=22)
+        check_rows(n_q, n_kv, d, old[-1:], new[7:8], fmt, dtype, seed=23)
+
+
+@pytest.mark.parametrize("fmt", ("bf16", "int8"))
+def test_one_request_in_padded_rows(fmt):
+    """the rows' count and what is promised about it say more than the request has"""
+    for new in (0, 1, 5, 50):
+        check_rows(4, 1, 128, [50], [new], fmt, torch.bfloat16, spare_rows=299, seed=new)
+        check_rows(4, 1, 128, [700], [new], fmt, torch.float32, window=100, sinks=3, max_new=200, spare_rows=299, seed=new + 1)
+
+
 @pytest.mark.parametrize("batch", (63, 64, 65, 200))
 def test_many_requests(batch):
     rng = np.random.default_rng(batch)
