@@ -715,6 +715,8 @@ def op_row_attention(pool, layer, q, block_table, row_starts, seq_lens, window=0
     key = heads, cfg.n_kv_heads, cfg.head_dim, batch, rows, max_new
     need = _rows_work.get(key)
     if need is None:
+        if len(_rows_work) >= 4096:
+            _rows_work.clear()
         need = _rows_work[key] = load().chiron_row_attention_workspace_bytes(*key) // 4
     work = seq_lens.new_empty(need)
     a = AttnRows(qp or None, _address(out, dtype) or None, qs, _ROW_TYPES[dtype], heads, _address(block_table, torch.int32), _address(row_starts, torch.int32),

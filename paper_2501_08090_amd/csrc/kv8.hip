@@ -4,6 +4,10 @@
 // codes in pieces of 8 bytes (K) and 16 (V).  A page that held tokens before keeps the larger power of two; only if that has
 // grown are its old codes read, divided and rounded again.  Division by a power of two and the rounding are exact operations, so what is
 // stored follows from the rotated values alone.
+//
+// Bound by memory where there are many rows: 16384 fp32 rows of 32 + 2 x 8 heads of 128 120 to 124 us, 700 MB at 5.7 TB/s, most of them the queries'; 5003 bf16 rows 28 to
+// 33 us; 64 single tokens 7.7 us, a chain of loads (row starts, table entry, page, all at once from there on).  The read-back reads V's four tokens of a
+// word for one, 4 us for 64 tokens, 27 for 16384.
 #include <new>
 
 #include "append_rows.h"

@@ -228,7 +228,14 @@ __device__ __forceinline__ void store_row(const RowAttnArgs& a, int64_t row, int
 // CW: columns of a term group.  Three terms of up to 4 columns share one instruction, of up to 8 two.  int8 keys meet the query in
 // four 8-bit digits instead (whole multiples of 2^(f-24), with 2^f the power of two of the head's largest element: what is no smaller than
 // 2^-7 of that is exact), on the 8-bit matrix cores: no key is widened, and sums are exact.
-constexpr int kFewMinPages = 8;  // of a share
+//
+// Bound by memory where the caches are long: 32 requests of 24k to 32k tokens, 32 heads over 8 KV heads of 128, e4m3, fp32 queries 286 to 292 us, 6.5
+// TB/s; over bf16 pages with a window of 4096 87 to 90 us, 6.1 TB/s.  One request of 8192 tokens takes 13 us and the join 5: launch, a chain of loads
+// (row starts, table, page) and the partial results.  61 requests of up to 5000 tokens that bring up to 5, 16 heads over 2 of 64, e4m3: 27 us and 5.
+//
+// A share's least pages, us with 4 / 8 / 16: one request of 500 tokens 12.5 / 13.9 / 16.4, of 2000 13.6 / 14.4 / 17.0, of 8000 18.0 / 16.5 / 17.7, eight of 2000
+// over bf16 pages 22.1 / 20.7 / 24.4: with fewer there are more partial results to join, with more the chain is longer.
+constexpr int kFewMinPages = 8;
 // Waves of a SIMD: two, but one where three terms of many columns and bf16 pages of 128 dims do not fit 256 registers.
 __host__ __device__ constexpr int few_waves(int d, int fmt, bool f32, int cw, bool multi) {
     return fmt == kFmtBf16 && f32 && d == 128 && (cw == 16 || (cw == 8 && multi)) ? 1 : 2;
@@ -673,9 +680,15 @@ __global__ __launch_bounds__(256) void row_few_merge_kernel(RowAttnArgs a) {
 
 // ---- requests of many rows ----------------------------------------------------------------------------------------
 // A workgroup takes a tile of tt tokens x G heads of one KV head, up to 128 columns, 32 of them a wave's, and goes through the pages
-// that they see together, four at a time: each wave brings one page into LDS, as bf16 in operand order, while the four before are multiplied.
+// that they see together in stages of two: the next stage's come into LDS, as bf16 in operand order, while this one's are multiplied.
 // A column group's maxima, sums and outputs stay in registers.  Tiles with the most pages begin first.  Where there are few tiles
 // the pages of each are dealt to `splits` workgroups.
+//
+// Bound by the latency of a stage (barrier, LDS reads, the softmax between two products) and the vector units more than by the matrix cores, which
+// are busy 28 % of the time (vector units 40 %): a prompt of 8192 tokens within a window of 1024, 32 heads over 8 KV heads of 128, bf16 181 us, 0.71
+// PFLOP/s of the 1.41 that a large product reaches here; three chunks of 500 to 1100 tokens behind 12k tokens of int8 pages 581 to 607 us, 0.8 PFLOP/s.  Two pages
+// a stage leave registers and LDS for three waves of a SIMD: the chunks 617 us, and 803 with four pages and two waves.  Splitting the chunks' pages 609 us,
+// not splitting them 666; 29 mixed requests in fp32 within a window of 777 75.1 and 78.7.
 constexpr int kManyTiles = 2, kManyCols = 64 * kManyTiles;  // column tiles of a wave; columns of a workgroup
 struct ManyTile {
     int r0, t0, tv, req;
@@ -1175,6 +1188,9 @@ static int32_t row_attention(const chiron_attn_rows* in, int n_kv, int d, int nu
         return fail(CHIRON_ERR_INVALID_ARG, "row attention: q_stride %lld is smaller than a row or no multiple of 16 bytes", (long long)in->q_stride);
     if (((uintptr_t)in->q | (uintptr_t)in->out | (uintptr_t)workspace) & 15) return fail(CHIRON_ERR_INVALID_ARG, "row attention: q, out and the workspace must be 16-byte aligned");
     if (!workspace) return fail(CHIRON_ERR_INVALID_ARG, "row attention: the workspace is null");
+    const uint64_t q0 = (uint64_t)(uintptr_t)in->q, o0 = (uint64_t)(uintptr_t)in->out, row = (uint64_t)in->n_q_heads * d * size;
+    if (q0 < o0 + (uint64_t)in->rows * row && o0 < q0 + (uint64_t)(in->rows - 1) * (uint64_t)in->q_stride * size + row)
+        return fail(CHIRON_ERR_INVALID_ARG, "row attention: out overlaps q, which other workgroups still read");
     const RowShape s = row_shape(in->n_q_heads, n_kv, d, in->batch, in->rows, in->max_new, few_passes(in, n_kv, d, format));
     if ((int64_t)s.passes_max * in->max_blocks_per_seq >= (int64_t)1 << 31)
         return fail(CHIRON_ERR_SHAPE, "row attention: %d requests of up to %d pages are too many for one call", in->batch, in->max_blocks_per_seq);
@@ -1187,7 +1203,8 @@ static int32_t row_attention(const chiron_attn_rows* in, int n_kv, int d, int nu
     a.max_new = in->max_new; a.n_sinks = in->n_sinks;
     a.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)d));
     a.few_max = s.few_max; a.tg = s.tg; a.pcols = s.cw; a.passes_max = s.passes_max; a.tt = s.tt;
-    // one request that may bring many rows goes by tiles even if it brings few: the two launches for few rows cost 9 us
+    // one request that may bring many rows goes by tiles even if it brings few: the two launches for few rows cost 9 us; one that then brings a single
+    // row pays a tile's padding
     if (s.slots && in->batch == 1) a.few_max = 0;
     a.splits = 1;
     if (s.splits_max > 1) {  // a part has 256 tokens at least, if the window or the table lets a tile see as many

@@ -454,6 +454,11 @@ def test_row_attention_refusals():
             B.op_row_attention(c.pool, 0, q, bt, starts, old, **kw)
     with pytest.raises(ValueError):
         B.op_row_attention(c.pool, 0, q, bt, starts, old, out=q[:1])
+    wide = torch.zeros((4, 4, 64), device="cuda")
+    for out in (wide[:2], wide[1:3]):  # out over q, which other workgroups still read
+        with pytest.raises(B.ChironError):
+            B.op_row_attention(c.pool, 0, wide[:2], bt, starts, old, out=out)
+    B.op_row_attention(c.pool, 0, wide[:2], bt, starts, old, out=wide[2:])
     with pytest.raises(B.ChironError):
         B.op_row_attention(c.pool, 0, q, bt[:0], ints([0]), old[:0])
     empty = q[:0]
