@@ -230,7 +230,7 @@ __device__ __forceinline__ void store_row(const RowAttnArgs& a, int64_t row, int
 // 2^-7 of that is exact), on the 8-bit matrix cores: no key is widened, and sums are exact.
 //
 // Bound by memory where the caches are long: 32 requests of 24k to 32k tokens, 32 heads over 8 KV heads of 128, e4m3, fp32 queries 286 to 292 us, 6.5
-// TB/s; over bf16 pages with a window of 4096 87 to 90 us, 6.1 TB/s.  One request of 8192 tokens takes 13 us and the join 5: launch, a chain of loads
+// TB/s; over bf16 pages with a window of 4096 87 to 90 us, 6.1 TB/s.  One request of 8192 tokens takes 13 us and the join 4: launch, a chain of loads
 // (row starts, table, page) and the partial results.  61 requests of up to 5000 tokens that bring up to 5, 16 heads over 2 of 64, e4m3: 27 us and 5.
 //
 // A share's least pages, us with 4 / 8 / 16: one request of 500 tokens 12.5 / 13.9 / 16.4, of 2000 13.6 / 14.4 / 17.0, of 8000 18.0 / 16.5 / 17.7, eight of 2000
@@ -328,7 +328,7 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                 };
                 struct Stage {
                     uint4 k[NPG][P], v[NPG][P];
-                    int page[NPG], exp[NPG];
+                    int page[NPG];
                 } cur, nxt;
                 auto load = [&](int j, Stage& s) {
                     if (j - lbase >= 64) {  // uniform; 64 is a multiple of NPG
@@ -341,7 +341,6 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                         const int l = (j + u - lbase) & 63;
                         s.page[u] = there ? __builtin_amdgcn_readlane(v_page, l) : kNoPage;
                         const int blk = there ? __builtin_amdgcn_readlane(v_block, l) : 0;
-                        s.exp[u] = FMT == kFmtBf16 || !there ? 0 : __builtin_amdgcn_readlane(v_exp, l);
                         const uint8_t* tile = a.tiles + ((int64_t)blk * n_kv + c) * (2 * TILE) + lane * 16;
 #pragma unroll
                         for (int i = 0; i < P; ++i) {
@@ -443,6 +442,10 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                 }
 
                 for (int j = j0; j < j1; j += NPG) {
+                    // the powers of two that load() may overwrite; taken here, no page's load waits for them
+                    int exps[NPG];
+#pragma unroll
+                    for (int u = 0; u < NPG; ++u) exps[u] = FMT == kFmtBf16 || j + u >= j1 ? 0 : __builtin_amdgcn_readlane(v_exp, (j + u - lbase) & 63);
                     if (j + NPG < j1) load(j + NPG, nxt);
                     __builtin_amdgcn_sched_barrier(0);
                     bool full = true;
@@ -452,8 +455,8 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                     float ks[NPG], vs[NPG];
 #pragma unroll
                     for (int u = 0; u < NPG; ++u) {
-                        ks[u] = FMT == kFmtBf16 ? 1.f : two_to((int8_t)(cur.exp[u] & 0xff));
-                        vs[u] = FMT == kFmtBf16 ? 1.f : two_to((int8_t)(cur.exp[u] >> 8));
+                        ks[u] = FMT == kFmtBf16 ? 1.f : two_to((int8_t)(exps[u] & 0xff));
+                        vs[u] = FMT == kFmtBf16 ? 1.f : two_to((int8_t)(exps[u] >> 8));
                         if (DIGITS) {
                             intx4 y[NQ];
 #pragma unroll
@@ -641,20 +644,30 @@ __global__ __launch_bounds__(256) void row_few_merge_kernel(RowAttnArgs a) {
     __shared__ floatx4 s_num[S][LANES];
     __shared__ float s_den[S], s_max[S];
     const int col = blockIdx.x % a.pcols, vc = blockIdx.x / a.pcols, c = vc % a.n_kv, v = vc / a.n_kv;
-    if (v >= a.head[0]) return;
-    const int4 rec = *reinterpret_cast<const int4*>(a.head + 4 + 4 * (size_t)v);
-    if (rec.w <= 1 || col >= a.G * rec.y) return;
+    const int n_pass = a.head[0];
+    const int4 rec = *reinterpret_cast<const int4*>(a.head + 4 + 4 * (size_t)v);  // asked for beside the count; behind it whatever lies there
+    if (v >= n_pass || rec.w <= 1 || col >= a.G * rec.y) return;
     const int sl = threadIdx.x / LANES, ln = threadIdx.x % LANES;
     float M = -1e30f, den = 0.f;
     floatx4 num = {0.f, 0.f, 0.f, 0.f};
-    for (int j = sl; j < rec.w; j += S) {
-        const int64_t slot = ((int64_t)(rec.z + j) * a.n_kv + c) * a.pcols + col;
-        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + slot * 2);
-        const floatx4 o = *reinterpret_cast<const floatx4*>(a.part_o + slot * D + ln * 4);
-        const float Mn = fmaxf(M, ml.x), f0 = __builtin_amdgcn_exp2f(M - Mn), f1 = __builtin_amdgcn_exp2f(ml.x - Mn);
-        num = num * f0 + o * f1;
-        den = den * f0 + ml.y * f1;
-        M = Mn;
+    constexpr int kAtOnce = 4;  // parts whose loads are on their way together
+    for (int j0 = sl; j0 < rec.w; j0 += S * kAtOnce) {
+        float2 ml[kAtOnce];
+        floatx4 o[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int64_t slot = ((int64_t)(rec.z + min(j0 + u * S, rec.w - 1)) * a.n_kv + c) * a.pcols + col;
+            ml[u] = *reinterpret_cast<const float2*>(a.part_ml + slot * 2);
+            o[u] = *reinterpret_cast<const floatx4*>(a.part_o + slot * D + ln * 4);
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            if (j0 + u * S < rec.w) {
+                const float Mn = fmaxf(M, ml[u].x), f0 = __builtin_amdgcn_exp2f(M - Mn), f1 = __builtin_amdgcn_exp2f(ml[u].x - Mn);
+                num = num * f0 + o[u] * f1;
+                den = den * f0 + ml[u].y * f1;
+                M = Mn;
+            }
     }
     s_num[sl][ln] = num;
     if (ln == 0) {
