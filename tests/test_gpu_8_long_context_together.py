@@ -105,6 +105,7 @@ def workload(fmt, n_q=8, n_kv=2, d=64, batch=5, width=40, seed=3, rows_of=(1, 1,
     m = model(n_q, n_kv, d, width)
     blocks = batch * width
     pool = pool_of(m, blocks, fmt)
+    pool.memory.zero_()  # rows may see slots that nothing was appended to
     bt = ints(rng.permutation(blocks).reshape(batch, width))
     total = sum(rows_of)
     starts = ints(np.concatenate([[0], np.cumsum(rows_of)]))
