@@ -111,6 +111,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
+// A product that is rounded before it is added to another lane's.  Fused into the sum, a lane's own would enter unrounded and a + b and b + a differ: the
+// term groups of a column would cut different weights into terms, and a weight near the end of a term lose 2^-16 of itself.
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
 __device__ __forceinline__ uint32_t word(const uint4& w, int j) { return j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w; }
 // An fp32 number is the sum of three bf16 terms, exactly: the first 8 of its 24 significant bits, the next 8 and the rest, by truncation.
 // What is left of v behind its first t terms; its next term is the upper half of the word.
@@ -470,7 +476,7 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                                 float v = (float)y[NQ - 1][r];
 #pragma unroll
                                 for (int i = NQ - 2; i >= 0; --i) v = fmaf(v, kDigits, (float)y[i][r]);
-                                x[u][r] = v * (qw * ks[u]);
+                                x[u][r] = rounded_product(v, qw * ks[u]);  // every group adds the same numbers below
                             }
                         } else {
                             x[u] = floatx4{0.f, 0.f, 0.f, 0.f};

@@ -349,6 +349,31 @@ def test_long(fmt, dtype):
 
 
 @pytest.mark.parametrize("fmt", ("bf16", "int8", "e4m3"))
+@pytest.mark.parametrize("n_q,n_kv,d,new", ((32, 8, 128, 1), (8, 8, 64, 1), (16, 2, 64, 1), (8, 4, 128, 2), (8, 2, 128, 40)))
+def test_weights_add_up(fmt, n_q, n_kv, d, new):
+    """Values that are all 1: what is divided is the divisor, whatever the scores.  n weights, none below 0, are added with n roundings at most on
+    either side, the three terms of a weight and the term groups with three more, and the quotient has two: (2n + 8) 2^-24."""
+    rng = np.random.default_rng(n_q + d + new)
+    old = (np.arange(64) % 15 + 1).tolist()
+    total = [o + new for o in old]
+    bt, blocks = L.tables(total, 5)
+    c = L.Cache(n_kv, d, blocks, fmt)
+    n = sum(total)
+    k = torch.from_numpy(rng.standard_normal((n, n_kv, d))).float().cuda()
+    starts = np.concatenate([[0], np.cumsum(total)]).astype(np.int32)
+    cos, sin = torch.ones((n, d // 2), device="cuda"), torch.zeros((n, d // 2), device="cuda")
+    c.pool.append_rope(0, k, torch.ones_like(k), cos, sin, L.dev(bt), L.dev(starts), ints([0] * 64))
+    rows = np.arange(65, dtype=np.int32) * new
+    for scale in (0.5, 1.5, 3.0):
+        q = torch.from_numpy(rng.standard_normal((64 * new, n_q, d)) * scale).float().cuda()
+        say("weights", fmt, n_q, n_kv, d, new, scale)
+        got = B.op_row_attention(c.pool, 0, q, L.dev(bt), L.dev(rows), ints(old), max_new=new).double().cpu().numpy()
+        seen = np.concatenate([o + 1 + np.arange(new) for o in old])
+        err = abs(got - 1.0).max(axis=(1, 2))
+        assert (err <= (2 * seen + 8) * 2.0 ** -24).all(), float((err / ((2 * seen + 8) * 2.0 ** -24)).max())
+
+
+@pytest.mark.parametrize("fmt", ("bf16", "int8", "e4m3"))
 @pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
 def test_tokens_on_both_sides_of_a_prompt(fmt, dtype):
     """every count of passes up to the first tiles, in calls of few and of many requests (which draw that line elsewhere)"""
