@@ -259,7 +259,8 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n_kv = a.n_kv, c = blockIdx.x % n_kv, w = blockIdx.x / n_kv * 4 + wave, W = gridDim.x / n_kv * 4;
     const int col = lane & 15, lg = lane >> 4, ci = col % CW, grp = col / CW;
-    const int tq = MULTI ? ci / a.G : 0, h = ci - tq * a.G;
+    // columns behind the group's heads take the last one's place: what they load lies in q
+    const int tq = MULTI ? ci / a.G : 0, h = MULTI ? ci - tq * a.G : min(ci, a.G - 1);
 
     // a lane's request of the 64 from i0 on: pages over its passes, and passes
     auto look = [&](int i0, Request& r, int& cost, int& np) {

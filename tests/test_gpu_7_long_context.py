@@ -414,6 +414,31 @@ def test_pages_that_are_not_there(fmt, dtype):
     check_rows(4, 2, 64, [30, 10, 90], [50, 1, 20], fmt, dtype, window=16, clip=3, seed=5)
 
 
+@pytest.mark.parametrize("fmt", ("bf16", "int8", "e4m3"))
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+def test_queries_that_end_where_their_memory_does(fmt, dtype):
+    """the last rows of an allocation of its own, of heads that do not fill the columns of a pass: the same as anywhere else"""
+    rng = np.random.default_rng(31)
+    for n_q, n_kv, d in ((16, 8, 128), (8, 8, 64), (6, 2, 64), (10, 2, 128), (7, 1, 64)):
+        for new in (1, 3, 40):
+            old = [31 + i for i in range(10)]
+            total = [o + new for o in old]
+            bt, blocks = L.tables(total, 3)
+            c = L.Cache(n_kv, d, blocks, fmt)
+            c.fill(bt, total, rng)
+            n = 10 * new * n_q * d
+            q = torch.from_numpy(rng.standard_normal(n)).to(dtype).cuda()
+            memory = torch.zeros((32 << 20) // q.element_size(), dtype=dtype, device="cuda")  # whole pages of the allocator, and nothing behind
+            memory[-n:] = q
+            starts = ints(np.arange(11) * new)
+            say("end", fmt, dtype, n_q, n_kv, d, new)
+            want = B.op_row_attention(c.pool, 0, q.view(-1, n_q, d), L.dev(bt), starts, ints(old), window=38, max_new=new)
+            got = B.op_row_attention(c.pool, 0, memory[-n:].view(-1, n_q, d), L.dev(bt), starts, ints(old), window=38, max_new=new)
+            torch.cuda.synchronize()
+            assert torch.equal(got, want)
+            del memory
+
+
 @pytest.mark.parametrize("kw", (dict(max_new=1), dict(max_new=3), dict(max_new=20), dict(spare_rows=9), dict(layer=1, layers=3), dict(stride=8), dict(hot=30.0)))
 def test_row_arguments(kw):
     for fmt, dtype in (("bf16", torch.float32), ("int8", torch.bfloat16)):
