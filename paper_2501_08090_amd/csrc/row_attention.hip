@@ -262,8 +262,9 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
     // columns behind the group's heads take the last one's place: what they load lies in q
     const int tq = MULTI ? ci / a.G : 0, h = MULTI ? ci - tq * a.G : min(ci, a.G - 1);
 
-    // a lane's request of the 64 from i0 on: pages over its passes, and passes
-    auto look = [&](int i0, Request& r, int& cost, int& np) {
+    // a lane's request of the 64 from i0 on, behind `before` passes: pages over its passes, and passes.  Requests whose passes have no record, of row starts
+    // that do not ascend, are left out.
+    auto look = [&](int i0, int before, Request& r, int& cost, int& np) {
         cost = np = 0;
         if (i0 + lane < a.batch) {
             r = request(a, i0 + lane);
@@ -272,13 +273,14 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                 for (int g = 0; g < np; ++g) cost += span_of(a, r.old + g * a.tg, r.old + min((g + 1) * a.tg, r.n) - 1).n;
             }
         }
+        if (before + wave_scan(np) > a.passes_max) cost = np = 0;
     };
     int64_t total = 0;
     int n_pass = 0;
     Request rq;
     int cost, np;
     for (int i0 = 0; i0 < a.batch; i0 += 64) {
-        look(i0, rq, cost, np);
+        look(i0, n_pass, rq, cost, np);
         total += wave_total(cost);
         n_pass += wave_total(np);
     }
@@ -291,7 +293,7 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
     int64_t base = 0, at = begin;
     int vbase = 0;
     for (int i0 = 0; i0 < a.batch && at < end; i0 += 64) {
-        if (a.batch > 64) look(i0, rq, cost, np);  // else they are still there
+        if (a.batch > 64) look(i0, vbase, rq, cost, np);  // else they are still there
         const int incl = wave_scan(cost), vincl = wave_scan(np);
         const int all = __builtin_amdgcn_readlane(incl, 63);
         uint64_t ahead = __ballot(base + incl > at && cost > 0);

@@ -6,6 +6,8 @@ rounded, which numpy does alike: it is equal too.  Attention: logits that are of
 with s from the products' own magnitudes; the exponentials 2^-20 and the fp32 sums of n weights over four lanes and a tree, of weights
 and of weighted values, (n / 4 + 40) 2^-24 each.  With bf16 queries a weight is rounded to bf16, 2^-8 of itself and so at most 2^-8 of the
 weighted average of |v|, and the result by 2^-8 of itself."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -437,6 +439,34 @@ def test_queries_that_end_where_their_memory_does(fmt, dtype):
             torch.cuda.synchronize()
             assert torch.equal(got, want)
             del memory
+
+
+@pytest.mark.parametrize("fmt", ("bf16", "int8", "e4m3"))
+def test_row_starts_that_do_not_ascend(fmt):
+    """more requests claim rows than there are: nothing is written but rows of out and the workspace"""
+    n_q, n_kv, d, batch, rows = 8, 2, 64, 200, 4
+    c = L.Cache(n_kv, d, batch, fmt)
+    bt = ints(np.arange(batch).reshape(batch, 1))
+    k = torch.ones((batch * 16, n_kv, d), device="cuda")
+    c.pool.append_rope(0, k, k, torch.ones((batch * 16, d // 2), device="cuda"), torch.zeros((batch * 16, d // 2), device="cuda"), bt,
+                       ints(np.arange(batch + 1) * 16), ints([0] * batch))
+    for dtype in (torch.float32, torch.bfloat16):
+        for starts in ([0, 4] * 100 + [0], [0, 1] * 100 + [0], [0, 4, 0, 2] * 50 + [4], [-1, 3] * 100 + [9], [4] * 201, [3, 2, 1, 0] * 50 + [4]):
+            for max_new in (4, 1):
+                say("starts", fmt, dtype, starts[:5], max_new)
+                q = torch.ones((rows, n_q, d), dtype=dtype, device="cuda")
+                out = torch.full((3 * rows, n_q, d), 7.5, dtype=dtype, device="cuda")
+                need = B.load().chiron_row_attention_workspace_bytes(n_q, n_kv, d, batch, rows, max_new)
+                work = torch.full((need + 65536,), 0x5A, dtype=torch.uint8, device="cuda")
+                table, old = ints(starts), ints([12] * batch)
+                a = B.AttnRows(q.data_ptr(), out[rows:2 * rows].data_ptr(), n_q * d, B.CHIRON_F32 if dtype == torch.float32 else B.CHIRON_BF16, n_q, bt.data_ptr(),
+                               table.data_ptr(), old.data_ptr(), 1, batch, rows, max_new, 0, 0)
+                call = B.load().chiron_op_row_attention if fmt == "bf16" else B.load().chiron_op_row_attention8
+                assert call(c.pool._h, 0, C.addressof(a), work.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
+                torch.cuda.synchronize()
+                assert (work[need:] == 0x5A).all() and (out[:rows] == 7.5).all() and (out[2 * rows:] == 7.5).all()
+                got = out[rows:2 * rows].float()
+                assert ((got == 7.5) | ((got - 1).abs() < 1e-2)).all()
 
 
 @pytest.mark.parametrize("kw", (dict(max_new=1), dict(max_new=3), dict(max_new=20), dict(spare_rows=9), dict(layer=1, layers=3), dict(stride=8), dict(hot=30.0)))
