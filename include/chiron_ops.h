@@ -122,8 +122,8 @@ int32_t chiron_op_sparse_attention(chiron_model *m, const chiron_kvpool *p, int3
  * (behind a request's last token, out of every window) may be anything.  NaN and infinities in a key that a row sees leave its outputs
  * of that KV head undefined, in a value the same dim of these, in q its own head's, and reach no other row.
  *   in           host, read during the call
- *     dtype      CHIRON_F32: q and out fp32, products in three bf16 terms (fp32's accuracy); CHIRON_BF16: q and out bf16, one
- *                term, weights rounded to bf16 (errors of the order of out's own rounding), scores, sums and the softmax in fp32
+ *     dtype      CHIRON_F32: q and out fp32, products in three bf16 terms (fp32's accuracy); CHIRON_BF16: q and out bf16, q
+ *                one term, weights in 8 bits or more (errors of the order of out's own rounding), scores, sums and the softmax in fp32
  *     q, out     dev [rows][n_q_heads][head_dim], 16-byte aligned; q rows q_stride elements apart (16-byte multiples), heads and dims
  *                contiguous; out contiguous, not overlapping q
  *     n_q_heads  a multiple of the pool's KV heads, at most 16 times as many

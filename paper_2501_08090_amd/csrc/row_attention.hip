@@ -6,8 +6,9 @@
 // of a softmax belong to a lane's column, and a row's queries that share a KV head share one pass over its pages.  An 8-bit code is
 // widened to bf16 in registers, exactly; its power of two goes to the score (keys) or the weight (values).
 //
-// fp32 queries enter as three bf16 terms, and so do the weights: 24 bits, which keeps fp32's accuracy.  bf16 queries are one term, and so
-// are their weights.
+// fp32 queries enter as three bf16 terms, and so do the weights: 24 bits, which keeps fp32's accuracy.  bf16 queries are one term,
+// their weights two where requests bring few rows (memory is what those wait for: the same time) and one, rounded, in prompts (whose errors are
+// then up to 1.4 times those of out's own rounding; a second term would be a second product with V).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -251,8 +252,8 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
     constexpr bool DIGITS = FMT == kFmtInt8;
     constexpr int KSTEPS = D / (DIGITS ? 64 : 32), P = pieces<FMT>(D), NPG = D == 128 && (FMT == kFmtBf16 || (CW == 16 && (F32 || DIGITS))) ? 2 : 4;
     // terms of an instruction, and instructions, of a weight and of a query
-    constexpr int TPP = F32 && CW <= 8 ? (CW <= 4 ? 3 : 2) : 1, NP = F32 ? (3 + TPP - 1) / TPP : 1;
-    constexpr int TPQ = DIGITS ? 16 / CW : TPP, NQ = DIGITS ? 4 / TPQ : NP;
+    constexpr int TPP = F32 && CW <= 8 ? (CW <= 4 ? 3 : 2) : 1, NP = F32 ? (3 + TPP - 1) / TPP : 2;
+    constexpr int TPQ = DIGITS ? 16 / CW : TPP, NQ = DIGITS ? 4 / TPQ : F32 ? NP : 1;
     constexpr float kDigits = TPQ == 1 ? 0x1p-8f : 0x1p-16f;  // from one instruction's digits to the next one's
     constexpr int TILE = FMT == kFmtBf16 ? 32 * D : 16 * D;               // bytes of a K or V tile
     const int lane = threadIdx.x & 63;
@@ -572,20 +573,16 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                         uint4 pt[NP];
 #pragma unroll
                         for (int i = 0; i < NP; ++i) {
-                            if (F32) {
-                                const int t = i * TPP + grp;
-                                const uint32_t keep = TPP > 1 && (t > 2 || grp >= TPP) ? 0 : ~0u;
-                                float y[2][4];
+                            // with bf16 queries two terms, 16 bits: one of 8 would add as much error as out's own rounding where a row has few columns
+                            const int t = TPP > 1 ? i * TPP + grp : i;
+                            const uint32_t keep = TPP > 1 && (t > 2 || grp >= TPP) ? 0 : ~0u;
+                            float y[2][4];
 #pragma unroll
-                                for (int z = 0; z < 2; ++z)
+                            for (int z = 0; z < 2; ++z)
 #pragma unroll
-                                    for (int r = 0; r < 4; ++r) y[z][r] = rest3(pr[z][r], t);
-                                pt[i] = make_uint4(uppers(y[0][0], y[0][1]) & keep, uppers(y[0][2], y[0][3]) & keep, uppers(y[1][0], y[1][1]) & keep,
-                                                   uppers(y[1][2], y[1][3]) & keep);
-                            } else {
-                                pt[i] = make_uint4(pack_bf16_rne(pr[0][0], pr[0][1]), pack_bf16_rne(pr[0][2], pr[0][3]), pack_bf16_rne(pr[1][0], pr[1][1]),
-                                                   pack_bf16_rne(pr[1][2], pr[1][3]));
-                            }
+                                for (int r = 0; r < 4; ++r) y[z][r] = rest3(pr[z][r], t);
+                            pt[i] = make_uint4(uppers(y[0][0], y[0][1]) & keep, uppers(y[0][2], y[0][3]) & keep, uppers(y[1][0], y[1][1]) & keep,
+                                               uppers(y[1][2], y[1][3]) & keep);
                         }
 #pragma unroll
                         for (int b = 0; b < D / 16; ++b) {
@@ -1154,7 +1151,7 @@ static RowShape row_shape(int n_q, int n_kv, int d, int batch, int rows, int max
 }
 
 // Up to how many passes a request is row_few_kernel's.  us by passes / by tiles: 32 requests of 4000 tokens, 4 heads to a KV head of 128: fp32 over int8 at
-// 2 passes 104 / 165, 4 141 / 172, 8 239 / 312; fp32 over bf16 188 / 192, 222 / 194, 342 / 346; bf16 over int8 102 / 107, 135 / 115, 205 / 199; bf16 over bf16
+// 2 passes 104 / 165, 4 141 / 172, 8 239 / 312; fp32 over bf16 188 / 192, 222 / 194, 342 / 346; bf16 over int8 103 / 107, 137 / 115, 224 / 198; bf16 over bf16
 // at 2 183 / 141.  8 heads to a KV head of 64: bf16 over bf16 33 / 45, 55 / 30; bf16 over e4m3 26 / 45, 37 / 32.  One request of 8000 tokens, whose tiles leave
 // most compute units idle: 128 dims, 8 passes, fp32 over int8 38 / 48, bf16 over int8 36 / 36; over bf16 fp32 at 4 43 / 47, at 8 58 / 50, bf16 at 2 23 / 32, at
 // 4 35 / 33; 64 dims at 8 passes 17 to 20 / 25 to 33.
