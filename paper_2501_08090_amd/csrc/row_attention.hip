@@ -713,25 +713,34 @@ struct ManyTile {
     int r0, t0, tv, req;
     int64_t old;
 };
-// which tile a slot is: request i owns the slots from row_starts[i]/tt + i on; by a whole wave
+// Which tile a slot is, by a whole wave: of the requests of more than few_max rows the k-th owns the slots from row_starts/tt + k on.  Its tiles end before
+// the next one's begin (x/tt + n/tt rounded up is at most (x+n)/tt + 1), and there are no more of them than rows/(few_max+1), so that neither requests of few
+// rows nor those without rows take a slot.
 __device__ __forceinline__ bool many_tile(const RowAttnArgs& a, int slot, ManyTile& m) {
     const int lane = threadIdx.x & 63;
-    int req = -1;
+    int before = 0, local = -1;
     for (int i0 = 0; i0 < a.batch; i0 += 64) {
-        const int i = min(i0 + lane, a.batch - 1);
-        const uint64_t begun = __ballot(i0 + lane < a.batch && a.row_starts[i] / a.tt + i <= slot);
-        req += __popcll(begun);
-        if (begun != ~(uint64_t)0) break;
+        Request r = request(a, min(i0 + lane, a.batch - 1));
+        const bool many = i0 + lane < a.batch && r.n > a.few_max;
+        const uint64_t all = __ballot(many);
+        const int at = r.r0 / a.tt + before + __popcll(all & (((uint64_t)1 << lane) - 1));
+        const uint64_t begun = __ballot(many && at <= slot);
+        if (begun) {  // the last of them
+            const int L = 63 - __builtin_clzll(begun);
+            m.req = i0 + L;
+            m.r0 = __builtin_amdgcn_readlane(r.r0, L);
+            m.tv = __builtin_amdgcn_readlane(r.n, L);
+            m.old = __builtin_amdgcn_readlane((int)r.old, L);
+            local = slot - __builtin_amdgcn_readlane(at, L);
+        }
+        if (begun != all) break;
+        before += __popcll(all);
     }
-    if (req < 0) return false;
-    const Request r = request(a, req);
-    const int tiles = (r.n + a.tt - 1) / a.tt, local = slot - (r.r0 / a.tt + req);
-    if (r.n <= a.few_max || local < 0 || local >= tiles) return false;
-    m.req = req;
-    m.r0 = r.r0;
-    m.old = r.old;
+    if (local < 0) return false;
+    const int tiles = (m.tv + a.tt - 1) / a.tt;
+    if (local >= tiles) return false;
     m.t0 = (tiles - 1 - local) * a.tt;  // the last tokens see the most
-    m.tv = min(a.tt, r.n - m.t0);
+    m.tv = min(a.tt, m.tv - m.t0);
     return true;
 }
 
@@ -1130,13 +1139,12 @@ static RowShape row_shape(int n_q, int n_kv, int d, int batch, int rows, int max
     s.many_ml = s.many_o = 0;
     if (max_new > s.few_max) {
         s.tt = kManyCols / s.G;
-        s.slots = rows / s.tt + batch;
-        // workgroups that have something to do, at most: their pages are dealt out where the compute unit that gets most of them has many more than
-        // the mean (a part more costs about 2 %)
-        const int64_t tiles = (int64_t)rows / s.tt + std::min((int64_t)batch, (int64_t)rows / (s.few_max + 1));
+        // tiles, at most: as many slots.  Their pages are dealt out where the compute unit that gets most of them has many more than the mean (a part more
+        // costs about 2 %)
+        s.slots = (int)((int64_t)rows / s.tt + std::min((int64_t)batch, (int64_t)rows / (s.few_max + 1)));
         s.splits_max = 1;
         double best = 1e30;
-        const double alone = (double)std::max<int64_t>(1, tiles * n_kv) / kNumCU;
+        const double alone = (double)(int64_t)s.slots * n_kv / kNumCU;
         for (int k = 1; k <= (alone < 4 ? 16 : 1); ++k) {
             const double per = alone * k, cost = std::ceil(per) / per * (1.0 + 0.02 * (k - 1));
             if (cost < best - 1e-9) best = cost, s.splits_max = k;
