@@ -131,7 +131,8 @@ int32_t chiron_op_sparse_attention(chiron_model *m, const chiron_kvpool *p, int3
  *   row_starts dev int32 [batch+1], ascending from 0 to at most rows (rows behind the last request are left as they were, as are some
  *                of row starts that do not ascend);  seq_lens dev int32 [batch], tokens cached before these (negative: 0)
  *   block_table  dev int32 [batch, max_blocks_per_seq], max_blocks_per_seq <= 2^26
- *   workspace    dev, chiron_row_attention_workspace_bytes() bytes, 16-byte aligned, caller-owned, in use until the stream has passed */
+ *   workspace    dev, chiron_row_attention_workspace_bytes() bytes, 16-byte aligned, caller-owned, in use until the stream has passed.  What it
+ *                gives for some batch, rows and max_new is enough for every call in which none of them is larger (up to 256 MiB of it for the parts of tiles) */
 typedef struct {
     const void *q;
     void *out;

@@ -10,6 +10,7 @@
 // their weights two where requests bring few rows (memory is what those wait for: the same time) and one, rounded, in prompts (whose errors are
 // then up to 1.4 times those of out's own rounding; a second term would be a second product with V).
 #include <algorithm>
+#include <array>
 #include <cmath>
 #include <type_traits>
 
@@ -1120,7 +1121,34 @@ struct RowShape {
     int64_t rec_bytes, few_ml, few_o, many_ml, many_o;  // bytes
     int64_t bytes() const { return rec_bytes + few_ml + few_o + many_ml + many_o; }
 };
+// Parts of a tile's pages, for that many workgroups (tile and KV head): the pages are dealt out where the compute unit that gets most workgroups has many more
+// than the mean (a part more costs about 2 %).
+constexpr int kSplitBelow = 4 * kNumCU;  // workgroups from which they never are
+static int splits_for(int64_t wgs) {
+    if (wgs >= kSplitBelow) return 1;
+    int most = 1;
+    double best = 1e30;
+    for (int k = 1; k <= 16; ++k) {
+        const double per = (double)wgs / kNumCU * k, cost = std::ceil(per) / per * (1.0 + 0.02 * (k - 1));
+        if (cost < best - 1e-9) best = cost, most = k;
+    }
+    return most;
+}
+// the parts that calls of up to so many workgroups keep: fewer workgroups may be dealt out further and keep more
+static int64_t parts_upto(int64_t wgs) {
+    static const std::array<int, kSplitBelow> most = [] {
+        std::array<int, kSplitBelow> m;
+        m[0] = 0;
+        for (int w = 1; w < kSplitBelow; ++w) {
+            const int k = splits_for(w);
+            m[w] = std::max(m[w - 1], k > 1 ? w * k : 0);
+        }
+        return m;
+    }();
+    return most[std::min<int64_t>(wgs, kSplitBelow - 1)];
+}
 static int64_t up16(int64_t x) { return (x + 15) / 16 * 16; }
+// its sizes have room for every call whose batch, rows and max_new are no larger
 static RowShape row_shape(int n_q, int n_kv, int d, int batch, int rows, int max_new, int passes) {
     RowShape s;
     max_new = std::min(max_new, rows);
@@ -1139,21 +1167,11 @@ static RowShape row_shape(int n_q, int n_kv, int d, int batch, int rows, int max
     s.many_ml = s.many_o = 0;
     if (max_new > s.few_max) {
         s.tt = kManyCols / s.G;
-        // tiles, at most: as many slots.  Their pages are dealt out where the compute unit that gets most of them has many more than the mean (a part more
-        // costs about 2 %)
-        s.slots = (int)((int64_t)rows / s.tt + std::min((int64_t)batch, (int64_t)rows / (s.few_max + 1)));
-        s.splits_max = 1;
-        double best = 1e30;
-        const double alone = (double)(int64_t)s.slots * n_kv / kNumCU;
-        for (int k = 1; k <= (alone < 4 ? 16 : 1); ++k) {
-            const double per = alone * k, cost = std::ceil(per) / per * (1.0 + 0.02 * (k - 1));
-            if (cost < best - 1e-9) best = cost, s.splits_max = k;
-        }
-        if (s.splits_max > 1) {
-            const int64_t n = (int64_t)s.slots * n_kv * s.splits_max * kManyCols;
-            s.many_ml = up16(n * 8);
-            s.many_o = n * d * 4;
-        }
+        s.slots = (int)((int64_t)rows / s.tt + std::min((int64_t)batch, (int64_t)rows / (s.few_max + 1)));  // tiles, at most: as many slots
+        s.splits_max = splits_for((int64_t)s.slots * n_kv);
+        const int64_t columns = parts_upto((int64_t)s.slots * n_kv) * kManyCols;
+        s.many_ml = columns * 8;
+        s.many_o = columns * d * 4;
     }
     return s;
 }
@@ -1264,7 +1282,7 @@ extern "C" {
 int64_t chiron_row_attention_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t batch, int32_t rows, int32_t max_new) {
     if (n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads != 0 || n_q_heads / n_kv_heads > 16 || (head_dim != 64 && head_dim != 128)) return 0;
     if (batch < 1 || rows < 1 || max_new < 1) return 0;
-    int64_t most = 0;  // whatever the pool and the type are
+    int64_t most = 0;  // whatever the pool and the type are, and for smaller calls too
     for (int passes = 1; passes <= kMostPasses; passes *= 2) most = std::max(most, row_shape(n_q_heads, n_kv_heads, head_dim, batch, rows, max_new, passes).bytes());
     return most;
 }
