@@ -25,8 +25,8 @@ __device__ __forceinline__ int8_t* exps8(const Pool8Desc& p, int layer, int bloc
 __device__ __forceinline__ int k8_off(int t, int e) { return ((e >> 4) * 16 + t) * 16 + (e & 15); }
 __device__ __forceinline__ int v8_off(int t, int e) { return ((((e >> 6) * 4 + (t >> 2)) * 16 + (e & 15)) * 4 + ((e & 63) >> 4)) * 4 + (t & 3); }
 
-constexpr int kMinExp8 = -100;            // steps are not finer than this: sums of what they multiply stay clear of subnormal numbers
-constexpr float kLimit8 = 0x1p100f;       // and values not larger: sums of 2^27 of them are finite
+constexpr int kMinExp8 = -100;            // steps are not finer than this: values stay clear of subnormal numbers (their products with weights need not)
+constexpr float kLimit8 = 0x1p100f;       // and values not larger: sums of 2^27 of them are finite, with weights up to 2^8 of 2^19
 
 __device__ __forceinline__ float bounded8(float x) {
     x = x != x ? 0.f : x;

@@ -910,9 +910,11 @@ __global__ __launch_bounds__(256, F32 ? 2 : 3) void row_many_kernel(RowAttnArgs 
 
     auto compute = [&](int buf) {
         if (idle) return;
-        // int8 codes are multiplied as they are: the keys' power of two goes to the scores, the values' to the weights, and out of their sum again
-        constexpr bool INT8 = FMT == kFmtInt8, SCALED = INT8 || !F32;
-        float ks[2], ev[2], vdown[2];
+        // int8 codes are multiplied as they are: the keys' power of two goes to the scores, the values' to the weights.  fp32 rows' weights are added up before.  Those
+        // of bf16 rows get it within the exponential, and the product that adds them up takes it out: a page of zeros, whose power is 2^-100, so loses its weights
+        // below 2^-26 (of a sum of at least 1), no more than that sum does, which is off by up to 2^-24 for each.
+        constexpr bool INT8 = FMT == kFmtInt8, SCALED = INT8 || !F32, FOLDED = INT8 && !F32;
+        float ks[2], ev[2], vup[2];
         uint32_t one[2] = {0x3f803f80u, 0x3f803f80u};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -921,7 +923,7 @@ __global__ __launch_bounds__(256, F32 ? 2 : 3) void row_many_kernel(RowAttnArgs 
                 const int e = (int8_t)(cur_exps[u] >> 8);
                 ks[u] *= two_to((int8_t)(cur_exps[u] & 0xff));
                 ev[u] = (float)e;
-                vdown[u] = two_to(-e);
+                vup[u] = two_to(e);
                 one[u] = (uint32_t)(127 - e) << 23 | (uint32_t)(127 - e) << 7;
             }
         }
@@ -991,12 +993,13 @@ __global__ __launch_bounds__(256, F32 ? 2 : 3) void row_many_kernel(RowAttnArgs 
             float p[2][4];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                const float off = INT8 ? ev[y] - m_use : -m_use;
+                const float off = FOLDED ? ev[y] - m_use : -m_use;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float s = x[n][y][r];
                     p[y][r] = __builtin_amdgcn_exp2f(SCALED ? fmaf(s, ks[y], off) : s + off);
-                    if (F32) l_run[n][0] += INT8 ? p[y][r] * vdown[y] : p[y][r];
+                    if (F32) l_run[n][0] += p[y][r];
+                    if (INT8 && F32) p[y][r] *= vup[y];
                 }
             }
 #pragma unroll
