@@ -126,6 +126,7 @@ int32_t chiron_op_sparse_attention(chiron_model *m, const chiron_kvpool *p, int3
  *                one term, weights in 8 bits or more (errors of the order of out's own rounding), scores, sums and the softmax in fp32
  *     q, out     dev [rows][n_q_heads][head_dim], 16-byte aligned; q rows q_stride elements apart (16-byte multiples), heads and dims
  *                contiguous; out contiguous, not overlapping q
+ *                (over int8 pages elements of q up to 2^113: prompts multiply the codes before their power of two)
  *     n_q_heads  a multiple of the pool's KV heads, at most 16 times as many
  *     max_new    >= the rows of any request (those behind a request's first max_new are left as they were)
  *   row_starts dev int32 [batch+1], ascending from 0 to at most rows (rows behind the last request are left as they were, as are some

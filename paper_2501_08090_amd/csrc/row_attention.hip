@@ -397,7 +397,7 @@ __global__ __launch_bounds__(256, few_waves(D, FMT, F32, CW, MULTI)) void row_fe
                     top = fmaxf(top, __shfl_xor(top, 16));
                     top = fmaxf(top, __shfl_xor(top, 32));
                     // |y| <= 127 * 2^f; a head of zeros, NaN and infinities go by any power (the last two are put back below)
-                    const int f = top > 0.f && top < INFINITY ? min(max(power_of(top), -100), 120) : 0;
+                    const int f = top > 0.f && top < INFINITY ? max(power_of(top), -100) : 0;
                     const float up = two_to(-f) * 0x1p24f;
 #pragma unroll
                     for (int s = 0; s < KSTEPS; ++s)

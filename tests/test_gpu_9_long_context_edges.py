@@ -53,3 +53,28 @@ def test_small_weights_of_values_that_are_zero(fmt, dtype, new):
     err = abs(got - want[:, :, None]).max(-1)
     say("   worst error %.3f of what is allowed" % float((err / tol).max()))
     assert (err <= tol).all()
+
+
+@pytest.mark.parametrize("fmt", ("int8", "e4m3", "bf16"))
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("new,large", ((1, 2.0 ** 127 * 1.5), (3, 2.0 ** 127 * 1.5), (1, -2.0 ** 127 * 1.9), (3, 2.0 ** 126 * 1.99), (33, -2.0 ** 113), (33, 2.0 ** 113)))
+@pytest.mark.parametrize("n_q,n_kv,d", ((4, 1, 128), (8, 8, 64), (16, 2, 64)))
+def test_queries_near_the_largest_number(fmt, dtype, new, large, n_q, n_kv, d):
+    """Keys of 1 to 7 times +-2^-100 make scores of thousands and more that are whole multiples of one step: one token has all the weight, and the
+    output is its value, exactly."""
+    c = L.Cache(n_kv, d, 4, fmt)
+    c.pool.memory.zero_()
+    n = 3 * PAGE + 3
+    key = torch.zeros((n, n_kv, d), device="cuda")
+    key[:, :, 5] = ((torch.arange(n, device="cuda") % 6) - 3.0)[:, None] * 2.0 ** -100
+    key[11, :, 5], key[17, :, 5] = -7 * 2.0 ** -100, 7 * 2.0 ** -100
+    value = (torch.arange(n * n_kv * d, device="cuda") % 15 - 7.0).view(n, n_kv, d)  # held exactly by all three
+    one, zero = torch.ones((n, d // 2), device="cuda"), torch.zeros((n, d // 2), device="cuda")
+    table = ints([[2, 0, 3, 1]])
+    c.pool.append_rope(0, key, value, one, zero, table, ints([0, n]), ints([0]))
+    q = torch.zeros((new, n_q, d), dtype=dtype, device="cuda")
+    q[:, :, 5] = large
+    say("large", fmt, dtype, new, large)
+    got = B.op_row_attention(c.pool, 0, q, table, ints([0, new]), ints([18]), max_new=new)
+    want = value[17 if large > 0 else 11].repeat_interleave(n_q // n_kv, 0)
+    assert (got.float() == want).all()
