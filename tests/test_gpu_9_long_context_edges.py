@@ -78,3 +78,56 @@ def test_queries_near_the_largest_number(fmt, dtype, new, large, n_q, n_kv, d):
     got = B.op_row_attention(c.pool, 0, q, table, ints([0, new]), ints([18]), max_new=new)
     want = value[17 if large > 0 else 11].repeat_interleave(n_q // n_kv, 0)
     assert (got.float() == want).all()
+
+
+@pytest.mark.parametrize("fmt", ("bf16", "int8", "e4m3"))
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("new,window,sinks", ((1, 0, 0), (3, 0, 0), (40, 0, 0), (1, 70001, 1001), (3, 70001, 1001), (40, 70001, 1001)))
+def test_every_share_of_a_very_long_request(fmt, dtype, new, window, sinks):
+    """One request of 300000 tokens whose values say where a token is, so that a part of the pages that is lost or counted twice, or an edge that is off by a
+    token, shows: dims 0 .. 31 are 1 in one of 32 runs of tokens, the others in single tokens around the edges of what a row sees.
+
+    All values and weights are at least 0, so errors are relative.  A weight: twice the slack s of a score, twice the exponential's 2^-20, and with bf16 queries
+    2^-9 in either sum.  Sums: a part of the pages holds a sixteenth of them at most, so n/16 additions and the joins' 100, each off by 2^-23 even if it cuts, in
+    numerator and divisor.  bf16 results 2^-8."""
+    n_q, n_kv, d, n = 4, 1, 64, 300000
+    run, old = n // 32 + 1, n - new
+    c = L.Cache(n_kv, d, -(-n // PAGE), fmt)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    table = torch.randperm(-(-n // PAGE), generator=g, device="cuda").to(torch.int32)[None].contiguous()
+    key = torch.randn((n, n_kv, d), generator=g, device="cuda") * 0.5
+    at = torch.arange(n, device="cuda")
+    value = torch.zeros((n, n_kv, d), device="cuda")
+    value[at, 0, at // run] = 1.0
+    edge = at > n - 70
+    if window:
+        edge |= (abs(at - (old - window)) < 70) | (abs(at - sinks) < 20)
+    value[at[edge], 0, 32 + at[edge] % 32] = 1.0
+    one, zero = torch.ones((n, d // 2), device="cuda"), torch.zeros((n, d // 2), device="cuda")
+    c.pool.append_rope(0, key, value, one, zero, table, ints([0, n]), ints([0]))
+    k, v = (torch.from_numpy(a[:, :, 0]).cuda()[table[0].long()].reshape(-1, d)[:n] for a in c.values())
+    assert torch.equal(v.float(), value[:, 0])
+    q = (torch.randn((new, n_q, d), generator=g, device="cuda") * 1.5).to(dtype)
+    say("long", fmt, dtype, new, window, sinks)
+    got = B.op_row_attention(c.pool, 0, q, table, ints([0, new]), ints([old]), window=window, n_sinks=sinks).double()
+    worst = 0.0
+    for t in sorted({0, 1, 2, new // 2, new - 1} & set(range(new))):
+        see = at <= old + t
+        if window:
+            see &= (at > old + t - window) | (at < sinks)
+        qt = q[t].double()
+        w = torch.softmax((qt @ k.t().contiguous() / d ** 0.5).masked_fill(~see, -float("inf")), -1)
+        want = w @ v
+        slack = (d + 8) * 2.0 ** -24 * float((qt.abs() @ k.abs().t().contiguous()).max()) / d ** 0.5
+        bf16 = dtype == torch.bfloat16
+        rel = 2 * slack + 2.0 ** -19 + 2 * (int(see.sum()) / 16 + 100) * 2.0 ** -23 + (2 * 2.0 ** -9 + 2.0 ** -8 if bf16 else 0.0)
+        # what a wave takes at least, 8 pages, would show (with bf16 rows four times as much)
+        lost = 512 if bf16 else 128
+        part = w[:, n // 2 // lost * lost + lost:old // lost * lost].reshape(n_q, -1, lost).sum(-1)
+        if window:
+            part = part[:, -(window - 4 * lost) // lost:]
+        assert float(part.min()) > 1.5 * rel * float(want[:, :32].max())
+        err = (got[t] - want).abs()
+        worst = max(worst, float((err / (rel * want + 2.0 ** -60)).max()))
+        assert (err <= rel * want).all(), (t, float((err - rel * want).max()))
+    say("   worst error %.3f of what is allowed" % worst)
