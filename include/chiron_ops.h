@@ -121,12 +121,13 @@ int32_t chiron_op_sparse_attention(chiron_model *m, const chiron_kvpool *p, int3
  * is no page of the pool, or behind the table's last column, count as not there; a row that sees none gets zeros.  What other slots hold
  * (behind a request's last token, out of every window) may be anything.  NaN and infinities in a key that a row sees leave its outputs
  * of that KV head undefined, in a value the same dim of these, in q its own head's, and reach no other row.
+ * So do scores q . K / sqrt(d) beyond +-2^30 (where fp32 holds no difference below 64) and, over int8 pages, elements of q beyond 2^113 (prompts multiply
+ * the codes before their power of two) in their own row and head.
  *   in           host, read during the call
  *     dtype      CHIRON_F32: q and out fp32, products in three bf16 terms (fp32's accuracy); CHIRON_BF16: q and out bf16, q
  *                one term, weights in 8 bits or more (errors of the order of out's own rounding), scores, sums and the softmax in fp32
  *     q, out     dev [rows][n_q_heads][head_dim], 16-byte aligned; q rows q_stride elements apart (16-byte multiples), heads and dims
  *                contiguous; out contiguous, not overlapping q
- *                (over int8 pages elements of q up to 2^113: prompts multiply the codes before their power of two)
  *     n_q_heads  a multiple of the pool's KV heads, at most 16 times as many
  *     max_new    >= the rows of any request (those behind a request's first max_new are left as they were)
  *   row_starts dev int32 [batch+1], ascending from 0 to at most rows (rows behind the last request are left as they were, as are some

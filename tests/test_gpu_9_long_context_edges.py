@@ -131,3 +131,28 @@ def test_every_share_of_a_very_long_request(fmt, dtype, new, window, sinks):
         worst = max(worst, float((err / (rel * want + 2.0 ** -60)).max()))
         assert (err <= rel * want).all(), (t, float((err - rel * want).max()))
     say("   worst error %.3f of what is allowed" % worst)
+
+
+@pytest.mark.parametrize("fmt", ("int8", "e4m3", "bf16"))
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("new", (1, 3, 33))
+@pytest.mark.parametrize("sign", (1.0, -1.0))
+@pytest.mark.parametrize("n_q,n_kv,d", ((4, 1, 128), (8, 8, 64), (16, 2, 64)))
+def test_scores_as_large_as_they_may_be(fmt, dtype, new, sign, n_q, n_kv, d):
+    """Scores of one sign up to 2^29.8 whose distances are some 2^20 and more: one token has all the weight, and the output is its value, exactly."""
+    c = L.Cache(n_kv, d, 4, fmt)
+    c.pool.memory.zero_()
+    n = 3 * PAGE + 3
+    key = torch.zeros((n, n_kv, d), device="cuda")
+    key[:, :, 5] = (2.0 + (torch.arange(n, device="cuda") % 4))[:, None] * 2.0 ** -20
+    key[11, :, 5], key[17, :, 5] = 2.0 ** -20, 7 * 2.0 ** -20
+    value = (torch.arange(n * n_kv * d, device="cuda") % 15 - 7.0).view(n, n_kv, d)
+    one, zero = torch.ones((n, d // 2), device="cuda"), torch.zeros((n, d // 2), device="cuda")
+    table = ints([[2, 0, 3, 1]])
+    c.pool.append_rope(0, key, value, one, zero, table, ints([0, n]), ints([0]))
+    q = torch.zeros((new, n_q, d), dtype=dtype, device="cuda")
+    q[:, :, 5] = sign * 2.0 ** 50
+    say("scores", fmt, dtype, new, sign)
+    got = B.op_row_attention(c.pool, 0, q, table, ints([0, new]), ints([18]), max_new=new)
+    want = value[17 if sign > 0 else 11].repeat_interleave(n_q // n_kv, 0)
+    assert (got.float() == want).all()
