@@ -129,12 +129,12 @@ int32_t chiron_op_sparse_attention(chiron_model *m, const chiron_kvpool *p, int3
  *     q, out     dev [rows][n_q_heads][head_dim], 16-byte aligned; q rows q_stride elements apart (16-byte multiples), heads and dims
  *                contiguous; out contiguous, not overlapping q
  *     n_q_heads  a multiple of the pool's KV heads, at most 16 times as many
- *     max_new    >= the rows of any request (those behind a request's first max_new are left as they were)
+ *     max_new    >= the rows of any request (those behind a request's first max_new are left as they were); more than that costs launches
  *   row_starts dev int32 [batch+1], ascending from 0 to at most rows (rows behind the last request are left as they were, as are some
  *                of row starts that do not ascend);  seq_lens dev int32 [batch], tokens cached before these (negative: 0)
  *   block_table  dev int32 [batch, max_blocks_per_seq], max_blocks_per_seq <= 2^26
  *   workspace    dev, chiron_row_attention_workspace_bytes() bytes, 16-byte aligned, caller-owned, in use until the stream has passed.  What it
- *                gives for some batch, rows and max_new is enough for every call in which none of them is larger (up to 256 MiB of it for the parts of tiles) */
+ *                gives for some batch, rows and max_new is enough for every call in which none of them is larger (up to 244 MiB of it for parts of tiles) */
 typedef struct {
     const void *q;
     void *out;

@@ -697,7 +697,8 @@ def op_row_attention(pool, layer, q, block_table, row_starts, seq_lens, window=0
     """Attention of new rows over a KVPool or a KVPool8 that holds their keys and values already.  q [rows, n_q_heads, head_dim] fp32 or bf16,
     rotated, rows of any 16-byte stride; request i brings the rows row_starts[i] .. row_starts[i+1]-1 (int32 [requests+1]) at the
     positions from seq_lens[i] on (int32 [requests]).  A row sees the last `window` positions up to its own (0: all) and the first n_sinks.
-    max_new: no request brings more rows (None: as many as there are).  -> out, q's shape and type; rows of no request are left as they were."""
+    max_new: no request brings more rows (None: as many as there are, the slower choice for a batch of few rows each: 64 single tokens of 500 to
+    1500 take 72 us so, 56 with 1).  -> out, q's shape and type; rows of no request are left as they were."""
     cfg, rows, batch, dtype = pool.model.cfg, q.shape[0], seq_lens.numel(), q.dtype
     if dtype not in _ROW_TYPES:
         raise TypeError("expected torch.float32 or torch.bfloat16, got %s" % dtype)

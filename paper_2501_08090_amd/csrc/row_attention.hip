@@ -705,8 +705,8 @@ __global__ __launch_bounds__(256) void row_few_merge_kernel(RowAttnArgs a) {
 // the pages of each are dealt to `splits` workgroups.
 //
 // Bound by the latency of a stage (barrier, LDS reads, the softmax between two products) and the vector units more than by the matrix cores, which
-// are busy 32 % of the time (vector units 40 to 50 %): a prompt of 8192 tokens within a window of 1024, 32 heads over 8 KV heads of 128, bf16 181 us, 0.71
-// PFLOP/s of the 1.41 that a large product reaches here; three chunks of 500 to 1100 tokens behind 12k tokens of int8 pages 581 to 607 us, 0.8 PFLOP/s.  Two pages
+// are busy 32 % of the time (vector units 40 to 50 %): a prompt of 8192 tokens within a window of 1024, 32 heads over 8 KV heads of 128, bf16 181 us a call
+// among others, 0.71 PFLOP/s of the 1.41 that a large product reaches here; three chunks of 500 to 1100 tokens behind 12k tokens of int8 pages 581 to 607 us, 0.8 PFLOP/s.  Two pages
 // a stage leave registers and LDS for three waves of a SIMD: the chunks 617 us, and 803 with four pages and two waves.  Splitting the chunks' pages 609 us,
 // not splitting them 666; 29 mixed requests in fp32 within a window of 777 75.1 and 78.7.
 constexpr int kManyTiles = 2, kManyCols = 64 * kManyTiles;  // column tiles of a wave; columns of a workgroup
